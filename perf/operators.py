@@ -303,7 +303,7 @@ def _own(st):
     if "own" not in st:  # the handles and the workspace that a serving program keeps
         if kind in ("copy", "compact"):
             part = lambda n, i: None if st[n] is None else st[n][i]  # noqa: E731
-            pools = [ckv.PagePool(*(part(n, i) for n in POOL)) for i in range(case["layers"])]
+            pools = ckv.PageLayers([ckv.PagePool(*(part(n, i) for n in POOL)) for i in range(case["layers"])])
             ws = None
             if kind == "compact":
                 ws = torch.empty(ckv.page_compact_workspace_bytes(case["pages"]), dtype=torch.uint8, device=DEV)
