@@ -590,6 +590,125 @@ ckv_status ckv_cache_state(const ckv_cache* cache, double* importance, int64_t* 
 ckv_status ckv_cache_resident(const ckv_cache* cache, int32_t tier, int64_t* keys,
                               int64_t capacity, int64_t* n);
 
+/* ---------------------------------------------------------------------------
+ * Paged KV cache -- what serving does with a Re-Prefill's KV afterwards: decode
+ * from it, append to it, share it between requests, tidy it up.  A page is a
+ * ContiguousChunk (Def. 4.1): the K (or V) rows of page_size consecutive tokens
+ * of one sequence, [page_size][n_kv_heads][head_dim].  A pool holds the pages of
+ * one layer, and the page table of a sequence names its pages in order: token t
+ * is row t % page_size of page table[t / page_size].  A prefix [n][Hkv][d] whose n
+ * is a whole number of chunks is such a pool, and sel_idx such a table.
+ *
+ * Types: F32 (head_dim 64), BF16 and E4M3 (head_dim 64 or 128).  An E4M3 pool
+ * holds 8-bit codes (OCP e4m3: 1 sign, 4 exponent and 3 mantissa bits, no
+ * infinity, largest 448) and a scale byte e per page and KV head for K, one for
+ * V: a row's element is code * 2^(e - 127), e in [10, 247], which bf16 holds
+ * exactly.  A power of two loses nothing: the codes keep four significant bits
+ * whatever the scale.  page_size: 8, 16 or a multiple of 32.
+ * ------------------------------------------------------------------------- */
+#define CKV_DTYPE_E4M3 2 /* page pools only */
+
+typedef struct ckv_page_pool {
+  void* k;             /* device: page p's K rows begin at element p * page_stride    */
+  void* v;             /* device: page p's V rows (may interleave with the K pages)    */
+  uint8_t* k_scale;    /* device, [n_pages][n_kv_heads] scale bytes (E4M3), else NULL  */
+  uint8_t* v_scale;
+  int64_t n_pages;     /* 1 <= n_pages <= 2^31 - 1                                     */
+  int64_t page_stride; /* elements between consecutive pages, at least
+                          page_size * n_kv_heads * head_dim and a whole number of 16
+                          bytes; 0: exactly that (dense)                               */
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t dtype;       /* CKV_DTYPE_F32, CKV_DTYPE_BF16 or CKV_DTYPE_E4M3              */
+} ckv_page_pool;
+
+/* The sequences of one call.  Sequence b has lens[b] tokens in the cache, the
+ * call's own included: its n_b = tok_off[b+1] - tok_off[b] tokens, rows
+ * tok_off[b] .. tok_off[b+1]-1 of the call's token tensors, stand at positions
+ * lens[b] - n_b .. lens[b] - 1.  n_b may be 0.  tok_off must not fall and stays in
+ * [0, n_tokens]; rows outside [tok_off[0], tok_off[n_seqs]) belong to no
+ * sequence and are left as they were.  A table entry outside [0, n_pages) names no
+ * page (of a window's pages that were given back, say): its tokens are not there. */
+typedef struct ckv_page_batch {
+  const int32_t* table;   /* device, [n_seqs][table_stride], the first max_pages used   */
+  const int32_t* lens;    /* device, [n_seqs]                                           */
+  const int32_t* tok_off; /* device, [n_seqs + 1]                                       */
+  int64_t table_stride;   /* entries between consecutive sequences; 0: max_pages        */
+  int64_t n_tokens;       /* rows of the call's token tensors (0: nothing to do)        */
+  int32_t n_seqs;         /* 0: nothing to do                                           */
+  int32_t max_pages;      /* table entries per sequence                                 */
+  int32_t max_tokens;     /* about the most tokens of one sequence, and about the       */
+  int32_t max_len;        /*   greatest length: they choose kernels and splits, results
+                               hold for any; 0: not known                               */
+} ckv_page_batch;
+
+/* Writes the call's tokens into their pages: k_new and v_new [n_tokens][Hkv][d]
+ * (device, fp32 for an F32 pool, else bf16; 16-byte aligned) to the rows of
+ * their positions.  A position outside the table or without a page is dropped;
+ * every other byte of the pool is left as it was.
+ * E4M3: per page and KV head, the scale is the least power of two 2^(e-127),
+ * e >= 10, with |x| <= 448 * scale for the page's new rows; where the page
+ * already held rows of this sequence, it is no less than before, and if it rises
+ * the old codes are rounded again to it.  Codes are rounded to nearest even.
+ * An infinity becomes the largest code of its sign, a NaN stays one; neither
+ * counts for the scale.  A page must be written by one sequence of the call
+ * only (give a forked sequence a copy of the page it goes on writing:
+ * ckv_page_copy). */
+ckv_status ckv_page_append(const ckv_page_pool* pool, const ckv_page_batch* batch,
+                           const void* k_new, const void* v_new, void* stream);
+
+/* Attention of the call's tokens over their sequences' pages (causal): the query
+ * at position p sees the keys at positions j <= p that are there and, with
+ * window > 0, have j > p - window or j < n_sinks (the sequence's first tokens,
+ * which stay visible).  window = 0: no window (n_sinks is then ignored).  Append
+ * the call's own tokens first.  out[t][h] = sum softmax(sm_scale q.k) v; a row
+ * that sees no key gives zeros.  GQA as in ckv_dims.
+ *   q, out   device, [n_tokens][n_q_heads][head_dim], fp32 for an F32 pool, else
+ *            bf16 (out written); 16-byte aligned
+ *   sm_scale logit scale; 0 selects 1/sqrt(head_dim)
+ *   ws       device workspace of ckv_page_attn_workspace_bytes(...) bytes for the
+ *            same arguments; calls that share one must not overlap in time
+ * Logits, softmax and sums in fp32; bf16 MFMA products for BF16 and E4M3 pools
+ * (numerators rounded to bf16), fp32 products for F32.  What a row cannot see of
+ * rows and pages that no query of its sequence sees may be anything, NaN
+ * included; a NaN or infinity that some query sees gives unspecified output for its
+ * sequence. */
+size_t ckv_page_attn_workspace_bytes(const ckv_page_pool* pool, const ckv_page_batch* batch,
+                                     int32_t n_q_heads, int32_t window, int32_t n_sinks);
+ckv_status ckv_page_attn(const ckv_page_pool* pool, const ckv_page_batch* batch, const void* q,
+                         int32_t n_q_heads, float sm_scale, int32_t window, int32_t n_sinks,
+                         void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Copies page src[i] to page dst[i], i < count, K, V and scales, in each of the
+ * n_pools pools (one per layer; same shapes throughout).  src, dst: device,
+ * int32[count].  A pair with an index outside [0, n_pages) is skipped.  A page
+ * may be the source of many pairs; one that is written by two pairs, or by one
+ * pair and read by another, has unspecified contents afterwards.  count = 0 or
+ * n_pools = 0: nothing to do. */
+ckv_status ckv_page_copy(const ckv_page_pool* pools, int32_t n_pools, const int32_t* src,
+                         const int32_t* dst, int64_t count, void* stream);
+
+/* Moves the pages in use to the front of the pools, so that everything from page
+ * n_live on is free.  refs[p] > 0: page p is in use (by so many tables); else it
+ * has been given back.  With L pages in use, the i-th page in use from L on goes to
+ * the i-th free page below L (both ascending), in each of the n_pools pools
+ * (same shapes throughout); pages below L stay.  A page's old place keeps its
+ * contents.
+ *   refs, refs_out    device, int32[n_pages]: the use counts, and those after the
+ *                     move (0 from L on); may be the same array
+ *   table, table_out  device, int32[n_entries]: page numbers to follow the move; an
+ *                     entry that names a page given back becomes -1, one outside
+ *                     [0, n_pages) stays as it is; may be the same array
+ *   n_live            device, int32[1]: L (written)
+ *   ws                device workspace of ckv_page_compact_workspace_bytes(n_pages)
+ * n_entries = 0 (table NULL) and n_pools = 0 are allowed. */
+size_t ckv_page_compact_workspace_bytes(int64_t n_pages);
+ckv_status ckv_page_compact(const ckv_page_pool* pools, int32_t n_pools, const int32_t* refs,
+                            int32_t* refs_out, int64_t n_pages, const int32_t* table,
+                            int32_t* table_out, int64_t n_entries, int32_t* n_live, void* ws,
+                            size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

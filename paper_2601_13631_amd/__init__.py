@@ -19,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libckv.so")
 
 OK, EINVAL, EUNSUPPORTED, EHIP, ENOMEM, ESTATE = range(6)
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_E4M3 = 0, 1, 2
 CTX_HOST_PREFIX, CTX_MATERIALIZE, CTX_STAGE_TIMING, CTX_SCORE_TIMING = 0x1, 0x2, 0x4, 0x8
 CACHE_ATTENTION, CACHE_LFU, CACHE_LOADS = 0, 1, 2
 STORE_DIRECT = 0x1
@@ -80,8 +80,25 @@ class CacheCounts(ctypes.Structure):
     _fields_ = [(f, ctypes.c_int64) for f in ("hits_gpu", "hits_cpu", "misses", "demoted", "dropped")]
 
 
+class _PagePool(ctypes.Structure):
+    """``ckv_page_pool``."""
+    _fields_ = [(f, ctypes.c_void_p) for f in ("k", "v", "k_scale", "v_scale")] + [
+        (f, ctypes.c_int64) for f in ("n_pages", "page_stride")] + [
+        (f, ctypes.c_int32) for f in ("page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class _PageBatch(ctypes.Structure):
+    """``ckv_page_batch``."""
+    _fields_ = [(f, ctypes.c_void_p) for f in ("table", "lens", "tok_off")] + [
+        (f, ctypes.c_int64) for f in ("table_stride", "n_tokens")] + [
+        (f, ctypes.c_int32) for f in ("n_seqs", "max_pages", "max_tokens", "max_len")]
+
+
 _P = ctypes.c_void_p
 _DP = ctypes.POINTER(Dims)
+_PP = ctypes.POINTER(_PagePool)
+_BP = ctypes.POINTER(_PageBatch)
+_I32, _I64, _SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 _SIG = {
     "ckv_last_error": ([], ctypes.c_char_p),
     "ckv_version": ([], ctypes.c_char_p),
@@ -128,6 +145,12 @@ _SIG = {
     "ckv_cache_state": ([_P, _P, _P, _P], ctypes.c_int32),
     "ckv_cache_resident": ([_P, ctypes.c_int32, _P, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)],
                            ctypes.c_int32),
+    "ckv_page_append": ([_PP, _BP, _P, _P, _P], _I32),
+    "ckv_page_attn_workspace_bytes": ([_PP, _BP, _I32, _I32, _I32], _SZ),
+    "ckv_page_attn": ([_PP, _BP, _P, _I32, ctypes.c_float, _I32, _I32, _P, _P, _SZ, _P], _I32),
+    "ckv_page_copy": ([_PP, _I32, _P, _P, _I64, _P], _I32),
+    "ckv_page_compact_workspace_bytes": ([_I64], _SZ),
+    "ckv_page_compact": ([_PP, _I32, _P, _P, _I64, _P, _P, _I64, _P, _P, _SZ, _P], _I32),
 }
 for _name, (_args, _res) in _SIG.items():
     _f = getattr(_lib, _name)
@@ -446,3 +469,161 @@ class Store:
             self.close()
         except Exception:
             pass
+
+
+def _need(t, what: str, dtype, shape=None):
+    """``t`` if it is a contiguous tensor of the current HIP device, of this type and shape."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} must be on the current device (it is on {t.device})")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype} (it is {t.dtype})")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have shape {tuple(shape)} (it has {tuple(t.shape)})")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t
+
+
+def _int32(x, what: str) -> int:
+    """``x`` as a C int that is not negative."""
+    if not 0 <= x < 1 << 31:
+        raise ValueError(f"{what} must be in [0, 2^31) (it is {x})")
+    return int(x)
+
+
+_PAGE_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float8_e4m3fn: DTYPE_E4M3}
+
+
+class PagePool:
+    """``ckv_page_pool``: one layer's pages.
+
+    ``k`` and ``v``: float32, bfloat16 or float8_e4m3fn tensors
+    [n_pages, page_size, n_kv_heads, head_dim] of the current device, whose pages are
+    contiguous and may lie apart (``stride(0)``, the same for both); with
+    float8_e4m3fn, ``k_scale`` and ``v_scale``: contiguous uint8 tensors
+    [n_pages, n_kv_heads].  Keeps the tensors alive.
+    """
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must be of one type and shape [n_pages, page_size, n_kv_heads, head_dim]")
+        if k.dtype not in _PAGE_DTYPES:
+            raise ValueError(f"pages are float32, bfloat16 or float8_e4m3fn (not {k.dtype})")
+        n_pages, page_size, hkv, d = k.shape
+        for t in (k, v):
+            if not t.is_cuda or t.device.index != torch.cuda.current_device():
+                raise ValueError(f"pages must be on the current device (they are on {t.device})")
+            if t.stride()[1:] != (hkv * d, d, 1) or (n_pages > 1 and t.stride(0) != k.stride(0)):
+                raise ValueError("a page's rows must be contiguous, and K and V pages equally far apart")
+        if (k.dtype == torch.float8_e4m3fn) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise ValueError("k_scale and v_scale belong to float8_e4m3fn pages, and to those only")
+        for t in (k_scale, v_scale):
+            if t is not None:
+                _need(t, "a scale tensor", torch.uint8, (n_pages, hkv))
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = n_pages, page_size, hkv, d
+        self.token_dtype = torch.float32 if k.dtype == torch.float32 else torch.bfloat16
+        self._c = _PagePool(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages,
+                            k.stride(0) if n_pages > 1 else 0, page_size, hkv, d, _PAGE_DTYPES[k.dtype])
+
+
+class PageLayers:
+    """The pools of a model's layers (same shapes throughout) as one handle for
+    :func:`page_copy` and :func:`page_compact`."""
+
+    def __init__(self, pools):
+        self.pools = tuple(pools)
+        self.n_pages = self.pools[0].n_pages if self.pools else 0
+        self._c = (_PagePool * len(self.pools))(*(p._c for p in self.pools))
+
+
+class PageBatch:
+    """``ckv_page_batch``: the sequences of one call.
+
+    ``table`` (int32 [n_seqs, max_pages], rows may lie apart), ``lens`` (int32
+    [n_seqs]) and ``tok_off`` (int32 [n_seqs + 1]) are device tensors, read when the
+    call's kernels run; ``n_tokens`` is the number of rows of the call's token
+    tensors.  ``max_tokens`` and ``max_len``: about the most tokens of a sequence
+    and the greatest length (0: not known).  Keeps the tensors alive.
+    """
+
+    def __init__(self, table, lens, tok_off, n_tokens: int, max_tokens: int = 0, max_len: int = 0):
+        if table.dim() != 2 or (table.shape[0] > 0 and table.stride(1) != 1 and table.shape[1] > 1):
+            raise ValueError("table must be [n_seqs, max_pages] with contiguous rows")
+        n_seqs, width = table.shape
+        if table.dtype != torch.int32 or not table.is_cuda or table.device.index != torch.cuda.current_device():
+            raise ValueError("table must be an int32 tensor of the current device")
+        _need(lens, "lens", torch.int32, (n_seqs,))
+        _need(tok_off, "tok_off", torch.int32, (n_seqs + 1,))
+        stride = table.stride(0) if n_seqs > 1 else width
+        if stride < width:
+            raise ValueError("the table's rows must not overlap")
+        _int32(n_tokens, "n_tokens")
+        self.table, self.lens, self.tok_off = table, lens, tok_off
+        self.n_seqs, self.n_tokens = n_seqs, int(n_tokens)
+        self._c = _PageBatch(_ptr(table), _ptr(lens), _ptr(tok_off), stride, n_tokens, n_seqs, width,
+                             _int32(max_tokens, "max_tokens"), _int32(max_len, "max_len"))
+
+
+def page_append(pool: PagePool, batch: PageBatch, k_new, v_new, stream=None) -> None:
+    """``ckv_page_append``: the batch's tokens' K and V rows (``[n_tokens, n_kv_heads,
+    head_dim]``, float32 for a float32 pool, else bfloat16) into their pages."""
+    shape = (batch.n_tokens, pool.n_kv_heads, pool.head_dim)
+    _need(k_new, "k_new", pool.token_dtype, shape)
+    _need(v_new, "v_new", pool.token_dtype, shape)
+    _check(_lib.ckv_page_append(pool._c, batch._c, k_new.data_ptr(), v_new.data_ptr(), _stream(stream)),
+           "ckv_page_append")
+
+
+def page_attn_workspace_bytes(pool: PagePool, batch: PageBatch, n_q_heads: int, window: int = 0,
+                              n_sinks: int = 0) -> int:
+    return int(_lib.ckv_page_attn_workspace_bytes(pool._c, batch._c, _int32(n_q_heads, "n_q_heads"),
+                                                  _int32(window, "window"), _int32(n_sinks, "n_sinks")))
+
+
+def page_attn(pool: PagePool, batch: PageBatch, q, out, ws=None, window: int = 0, n_sinks: int = 0,
+              sm_scale: float = 0.0, stream=None) -> None:
+    """``ckv_page_attn``: attention of the batch's tokens over their sequences' pages.
+
+    ``q`` and ``out``: ``[n_tokens, n_q_heads, head_dim]``, float32 for a float32
+    pool, else bfloat16.  ``ws``: a uint8 tensor of
+    :func:`page_attn_workspace_bytes` bytes (None where that is 0).
+    """
+    if q.dim() != 3 or q.shape[0] != batch.n_tokens or q.shape[2] != pool.head_dim:
+        raise ValueError("q must be [n_tokens, n_q_heads, head_dim]")
+    _need(q, "q", pool.token_dtype)
+    _need(out, "out", pool.token_dtype, q.shape)
+    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _check(_lib.ckv_page_attn(pool._c, batch._c, q.data_ptr(), q.shape[1], sm_scale,
+                              _int32(window, "window"), _int32(n_sinks, "n_sinks"), out.data_ptr(), _ptr(ws),
+                              nbytes, _stream(stream)), "ckv_page_attn")
+
+
+def page_copy(layers: PageLayers, src, dst, stream=None) -> None:
+    """``ckv_page_copy``: page ``src[i]`` to page ``dst[i]`` (int32 device tensors) in
+    every layer."""
+    _need(src, "src", torch.int32)
+    _need(dst, "dst", torch.int32, src.shape)
+    _check(_lib.ckv_page_copy(layers._c, len(layers.pools), src.data_ptr(), dst.data_ptr(), src.numel(),
+                              _stream(stream)), "ckv_page_copy")
+
+
+def page_compact_workspace_bytes(n_pages: int) -> int:
+    return int(_lib.ckv_page_compact_workspace_bytes(n_pages))
+
+
+def page_compact(layers: PageLayers, refs, refs_out, table, table_out, n_live, ws, stream=None) -> None:
+    """``ckv_page_compact``: the pages in use (``refs`` > 0) to the front of every layer's
+    pool.  ``refs``, ``refs_out``: int32 [n_pages]; ``table``, ``table_out``: int32 tensors of
+    one shape (or None); ``n_live``: int32 [1]; ``ws``: a uint8 tensor of
+    :func:`page_compact_workspace_bytes` bytes.  The outputs may be the inputs."""
+    _need(refs, "refs", torch.int32)
+    _need(refs_out, "refs_out", torch.int32, refs.shape)
+    _need(n_live, "n_live", torch.int32, (1,))
+    if table is not None:
+        _need(table, "table", torch.int32)
+        _need(table_out, "table_out", torch.int32, table.shape)
+    _check(_lib.ckv_page_compact(layers._c, len(layers.pools), refs.data_ptr(), refs_out.data_ptr(),
+                                 refs.numel(), _ptr(table), _ptr(table_out) if table is not None else None,
+                                 table.numel() if table is not None else 0, n_live.data_ptr(), _ptr(ws),
+                                 ws.numel() * ws.element_size(), _stream(stream)), "ckv_page_compact")

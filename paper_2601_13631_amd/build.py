@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libckv.so")
 SOURCES = ["api.hip", "score.hip", "select.hip", "gather.hip", "attn.hip", "layer.hip",
-           "io_account.hip", "cache.hip", "store.hip", "noalloc.hip"]
+           "io_account.hip", "cache.hip", "store.hip", "noalloc.hip", "pages.hip", "page_attn.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # NaN and infinity keep their meaning in every file: the attention kernel finds an
 # overflowed output by the infinity or NaN that it leaves.

@@ -1,0 +1,370 @@
+"""The paged cache's operators against a host model in 64 bits: attention with and without a
+window, append, copy and compact."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from pages_common import DEV, Cache, attend, check_attention, codes_to_f64  # noqa: E402
+
+H05, H7, H14, HF, H1 = (14, 2, 64), (28, 4, 128), (40, 8, 128), (4, 1, 64), (3, 3, 64)
+
+# (cache, heads, page, (new, length) per sequence, window, sinks)
+ATTN = [
+    ("bf16", H7, 16, [(1, 1)], 0, 0),                                   # one token, one key
+    ("bf16", H7, 32, [(1, 33), (1, 32), (1, 31), (1, 1000)], 0, 0),     # page and step borders
+    ("bf16", H05, 8, [(1, 7), (1, 8), (1, 9), (1, 257)], 0, 0),
+    ("bf16", H14, 96, [(1, 95), (1, 97), (1, 777)], 0, 0),              # no power of two
+    ("bf16", H1, 64, [(1, 500), (3, 3)], 0, 0),                         # no shared heads
+    ("bf16", H7, 32, [(1, 20000)], 0, 0),                               # long: many splits
+    ("bf16", H7, 64, [(37, 37), (1, 300), (0, 90), (130, 1000), (5, 64)], 0, 0),  # ragged, one idle
+    ("bf16", H05, 16, [(200, 450), (64, 64)], 0, 0),
+    ("bf16", H7, 32, [(1, 1000), (1, 64), (1, 65), (1, 3)], 64, 0),     # window as long as two steps
+    ("bf16", H7, 16, [(1, 1000), (1, 5), (1, 70)], 1, 0),               # sees itself alone
+    ("bf16", H05, 16, [(1, 900), (1, 40), (1, 64)], 50, 4),
+    ("bf16", H14, 8, [(7, 500), (300, 700), (60, 61)], 100, 8),
+    ("bf16", H7, 64, [(150, 900), (150, 150)], 97, 70),                 # sinks past one step
+    ("bf16", H7, 32, [(40, 200), (1, 100)], 5000, 4),                   # window past everything
+    ("bf16", H7, 32, [(40, 200), (1, 100)], 10, 5000),                  # sinks past everything
+    ("bf16", H7, 16, [(4, 2), (3, 3), (2, 0)], 0, 0),                   # rows before position 0
+    ("e4m3", H7, 16, [(1, 1), (1, 17), (1, 900)], 0, 0),
+    ("e4m3", H14, 8, [(1, 333), (2, 77), (5, 5)], 0, 0),
+    ("e4m3", H05, 32, [(1, 1000), (19, 400)], 200, 3),
+    ("e4m3", H05, 8, [(4, 1000), (4, 9)], 64, 8),
+    ("e4m3", H7, 96, [(1, 15000)], 0, 0),
+    ("e4m3", H7, 64, [(140, 500), (0, 3), (70, 70)], 0, 0),
+    ("e4m3", H14, 32, [(140, 500), (33, 1000)], 130, 40),
+    ("f32", HF, 16, [(1, 1), (1, 100), (1, 1024)], 0, 0),
+    ("f32", HF, 8, [(50, 333), (20, 20)], 0, 0),
+    ("f32", (4, 2, 64), 32, [(96, 1000), (0, 5), (33, 64)], 128, 4),
+    ("f32", HF, 96, [(1, 6000)], 0, 0),
+]
+
+
+@pytest.mark.parametrize("i", range(len(ATTN)))
+def test_attention(i):
+    cache, heads, page, seqs, window, sinks = ATTN[i]
+    c = Cache(cache, heads, page, seqs, seed=i)
+    c.poison(window, sinks)
+    pool, batch = c.device()
+    check_attention(c, attend(pool, batch, c.q.to(DEV), window, sinks), window, sinks)
+
+
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("bf16", H05), ("e4m3", H7), ("e4m3", H05), ("f32", HF)])
+@pytest.mark.parametrize("new", [1, 60])
+def test_attention_layouts(cache, heads, new):
+    """Missing pages, pages and table rows that lie apart, K and V pages in turn, rows behind
+    the last sequence, hints that do not hold."""
+    seqs = [(new, 500), (1, 130), (new, new)]
+    want = None
+    for how in range(4):
+        c = Cache(cache, heads, 16, seqs, seed=5, missing=[(0, 0), (0, 3), (0, 30), (1, 7)],
+                  gap=1024 if how == 1 else 0, interleaved=how == 2)
+        c.poison()
+        hints = dict(max_tokens=0, max_len=0) if how == 0 else dict(max_tokens=1, max_len=3) if how == 3 else {}
+        after = 5 if how == 1 else 0
+        pool, batch = c.device(table_gap=9 * how, rows_after=after, **hints)
+        out = attend(pool, batch, c.q.to(DEV), rows_after=after)
+        check_attention(c, out)
+        assert (out[c.tokens:] == 7).all()
+        if how in (1, 2):
+            assert want is None or torch.equal(want, out[:c.tokens])
+            want = out[:c.tokens]
+
+
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("e4m3", H7), ("f32", HF)])
+@pytest.mark.parametrize("new", [1, 100])
+def test_rows_without_keys_are_zero(cache, heads, new):
+    c = Cache(cache, heads, 16, [(new, 300), (new, 300)], seed=9, missing=[(0, s) for s in range(19)])
+    c.poison()
+    pool, batch = c.device()
+    out = attend(pool, batch, c.q.to(DEV))
+    assert (out[:new] == 0).all()
+    check_attention(c, out)
+
+
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("e4m3", H05), ("f32", HF)])
+@pytest.mark.parametrize("new", [1, 90])
+def test_rising_logits(cache, heads, new):
+    """Logits that grow along the keys by far more than the reference's slack, and fall again."""
+    c = Cache(cache, heads, 32, [(new, 700), (1, 600)], seed=3)
+    for n in (200, 350, 690):
+        slot, row = n // 32, n % 32
+        for b in range(2):
+            if n < c.seqs[b][1]:
+                for h in range(c.hkv):
+                    q = c.q[c.off[b], h * (c.hq // c.hkv)].float()
+                    x = q * {200: 4.0, 350: 12.0, 690: 8.0}[n]
+                    if cache == "e4m3":
+                        x = (x * 16).clamp(-448, 448)
+                        c.scale["k"][c.table[b, slot], h] = 123
+                    c.raw["k"][c.table[b, slot], row, h] = x.to(c.raw["k"].dtype)
+    pool, batch = c.device()
+    check_attention(c, attend(pool, batch, c.q.to(DEV)))
+
+
+def test_attention_scale():
+    c = Cache("bf16", H7, 16, [(1, 200), (30, 90)], seed=2)
+    pool, batch = c.device()
+    check_attention(c, attend(pool, batch, c.q.to(DEV), sm=0.25), sm=0.25)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_pool_past_4_gib(cache):
+    """Pages on both sides of 2^32 bytes, for one token and for many."""
+    import paper_2601_13631_amd as ckv
+    for new in (1, 150):
+        c = Cache(cache, H7, 32, [(new, 400)], seed=6)
+        k, v, ks, vs = c.device_pages()
+        span = 32 * 4 * 128 * k.element_size()
+        far = (5 << 30) // span
+        total = far + c.n_pages
+        place = np.array([p if p % 2 else far + p for p in range(c.n_pages)])
+        big = []
+        for t in (k, v):
+            x = torch.empty((total,) + tuple(t.shape[1:]), dtype=t.dtype, device=DEV)
+            x.view(torch.uint8)[torch.from_numpy(place).to(DEV)] = t.contiguous().view(torch.uint8)
+            big.append(x)
+        scales = [None, None]
+        if cache == "e4m3":
+            scales = [torch.zeros(total, 4, dtype=torch.uint8, device=DEV) for _ in range(2)]
+            for s, t in zip(scales, (ks, vs)):
+                s[torch.from_numpy(place).to(DEV)] = t
+        pool = ckv.PagePool(*big, *scales)
+        _, small = c.device()
+        table = torch.from_numpy(place[c.table].astype(np.int32)).to(DEV)
+        batch = ckv.PageBatch(table, small.lens, small.tok_off, c.tokens)
+        check_attention(c, attend(pool, batch, c.q.to(DEV)))
+        # append writes there too
+        ckv.page_append(pool, batch, c.new_rows["k"].to(DEV), c.new_rows["v"].to(DEV))
+        c.append()
+        for x, n in zip(big, "kv"):
+            got = x.view(torch.uint8)[torch.from_numpy(place).to(DEV)].view(x.dtype)
+            assert np.array_equal(codes_to_f64(got), codes_to_f64(c.raw[n]))
+        del big, pool
+
+
+# ---- append -----------------------------------------------------------------------
+
+APPEND = [
+    (16, [(1, 1), (1, 16), (1, 17), (1, 300)]),      # a fresh page's first row, a page's last
+    (8, [(3, 3), (20, 33), (0, 12), (8, 16)]),
+    (32, [(100, 100), (31, 64), (70, 97)]),
+    (96, [(200, 205), (1, 96), (1, 97)]),
+    (64, [(500, 1000)]),
+]
+
+
+def check_pages(c: Cache, k, v, ks, vs):
+    for t, n, s in ((k, "k", ks), (v, "v", vs)):
+        got, want = codes_to_f64(t), codes_to_f64(c.raw[n])
+        assert np.array_equal(got, want, equal_nan=True), n
+        if s is not None:
+            assert torch.equal(s.cpu(), c.scale[n]), n
+
+
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("e4m3", H7), ("e4m3", H05), ("f32", (4, 2, 64))])
+@pytest.mark.parametrize("i", range(len(APPEND)))
+@pytest.mark.parametrize("magnitude", [0.01, 3.0, 1e4])
+def test_append(cache, heads, i, magnitude):
+    """Every byte of the pool: new rows, older rows rounded to a scale that rose, all others."""
+    import paper_2601_13631_amd as ckv
+    page, seqs = APPEND[i]
+    c = Cache(cache, heads, page, seqs, seed=i, missing=[(0, 0)] if i == 2 else ())
+    c.new_rows = {n: (x.float() * magnitude).to(x.dtype) for n, x in c.new_rows.items()}
+    pool, batch = c.device()
+    ckv.page_append(pool, batch, c.new_rows["k"].to(DEV), c.new_rows["v"].to(DEV))
+    c.append()
+    check_pages(c, pool.k, pool.v, pool.k_scale, pool.v_scale)
+
+
+def test_append_odd_values():
+    """Zeros, the least and largest numbers, infinities and NaN; a page of zeros that grows."""
+    import paper_2601_13631_amd as ckv
+    c = Cache("e4m3", H05, 16, [(20, 20), (3, 5), (1, 1)], seed=1)
+    big = float(torch.finfo(torch.bfloat16).max)
+    for n in "kv":
+        x = c.new_rows[n]
+        x[:16] = 0
+        x[16:20, 0] = torch.tensor([0.0, 1e-39, -1e-40, 2.0 ** -126])[:, None].to(x.dtype)
+        x[17, 1, :6] = torch.tensor([float("nan"), float("inf"), -float("inf"), 2.0, 448.0, -449.0]).to(x.dtype)
+        x[20] = big
+        x[21, 0, 5] = float("inf")
+        x[23] = float("nan")
+    pool, batch = c.device()
+    ckv.page_append(pool, batch, c.new_rows["k"].to(DEV), c.new_rows["v"].to(DEV))
+    c.append()
+    check_pages(c, pool.k, pool.v, pool.k_scale, pool.v_scale)
+
+
+def test_append_outside_the_table():
+    """Positions past the table and before position 0 are dropped; rows of no sequence too."""
+    import paper_2601_13631_amd as ckv
+    for cache, heads in (("bf16", H7), ("e4m3", H7)):
+        c = Cache(cache, heads, 16, [(20, 40), (9, 5), (4, 30)], seed=4)
+        pool, _ = c.device()
+        narrow = torch.from_numpy(np.ascontiguousarray(c.table[:, :2])).to(DEV)
+        batch = ckv.PageBatch(narrow, torch.from_numpy(c.lens).to(DEV), torch.from_numpy(c.off).to(DEV),
+                              c.tokens + 3)
+        rows = [torch.cat([c.new_rows[n], torch.full_like(c.new_rows[n][:3], 99.0)]).to(DEV) for n in "kv"]
+        ckv.page_append(pool, batch, *rows)
+        c.width, c.table = 2, c.table[:, :2]
+        c.append()
+        check_pages(c, pool.k, pool.v, pool.k_scale, pool.v_scale)
+
+
+# ---- copy and compact -----------------------------------------------------------------
+
+def layers_of(cache, n, page, pages, heads, interleaved=False):
+    cs = [Cache(cache, heads, page, [(1, page * (pages - 2))], seed=i, interleaved=interleaved) for i in range(n)]
+    import paper_2601_13631_amd as ckv
+    return cs, ckv.PageLayers([ckv.PagePool(*c.device_pages()) for c in cs])
+
+
+def bytes_of(t):
+    return t.contiguous().view(torch.uint8).cpu()
+
+
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("e4m3", H05), ("f32", HF)])
+@pytest.mark.parametrize("n,page,pages,interleaved", [(1, 16, 12, False), (3, 8, 40, True), (70, 32, 9, False),
+                                                     (2, 96, 70, False)])
+def test_copy(cache, heads, n, page, pages, interleaved):
+    import paper_2601_13631_amd as ckv
+    cs, layers = layers_of(cache, n, page, pages, heads, interleaved)
+    before = [[t if t is None else t.clone() for t in (p.k, p.v, p.k_scale, p.v_scale)] for p in layers.pools]
+    src = [2, 2, 5, -1, 3, pages, 6, 2 ** 31 - 1]
+    dst = [0, 1, 7, 3, pages, 4, 6, 3]  # (6 to itself)
+    ckv.page_copy(layers, *(torch.tensor(x, dtype=torch.int32, device=DEV) for x in (src, dst)))
+    for p, old in zip(layers.pools, before):
+        come = list(range(pages))
+        for a, b in ((2, 0), (2, 1), (5, 7)):
+            come[b] = a
+        for t, o in zip((p.k, p.v, p.k_scale, p.v_scale), old):
+            if t is not None:
+                assert torch.equal(bytes_of(t), bytes_of(o)[come])
+    ckv.page_copy(layers, *(torch.empty(0, dtype=torch.int32, device=DEV) for _ in range(2)))
+    ckv.page_copy(ckv.PageLayers([]), *(torch.zeros(4, dtype=torch.int32, device=DEV) for _ in range(2)))
+
+
+def host_compact(refs, table, n_pages):
+    live = [p for p in range(n_pages) if refs[p] > 0]
+    L = len(live)
+    name, come = {p: p for p in live}, list(range(n_pages))
+    out = [max(r, 0) for r in refs]
+    for p, hole in zip([p for p in live if p >= L], [p for p in range(L) if refs[p] <= 0]):
+        name[p], come[hole] = hole, p
+        out[hole], out[p] = refs[p], 0
+    follow = [name.get(e, -1) if 0 <= e < n_pages else e for e in table]
+    return L, come, out, follow
+
+
+@pytest.mark.parametrize("cache,heads", [("bf16", HF), ("e4m3", H05)])
+@pytest.mark.parametrize("pages", [3, 64, 2047, 2048, 2049, 5000])
+@pytest.mark.parametrize("share", [0.0, 0.02, 0.5, 0.97, 1.0])
+def test_compact(cache, heads, pages, share):
+    import paper_2601_13631_amd as ckv
+    cs, layers = layers_of(cache, 2, 8, pages, heads)
+    rng = np.random.default_rng(pages)
+    refs = np.where(rng.random(pages) < share, rng.integers(1, 4, pages), -rng.integers(0, 2, pages)).astype(np.int32)
+    table = rng.integers(-2, pages + 2, 777).astype(np.int32)
+    L, come, want_refs, want_table = host_compact(refs.tolist(), table.tolist(), pages)
+    before = [[t if t is None else bytes_of(t) for t in (p.k, p.v, p.k_scale, p.v_scale)] for p in layers.pools]
+    ws = torch.full((ckv.page_compact_workspace_bytes(pages),), 0xFF, dtype=torch.uint8, device=DEV)
+    for in_place in (False, True):  # (again from the same counts: the pages move as before)
+        r, t = (torch.from_numpy(x).to(DEV) for x in (refs, table))
+        ro, to = (r, t) if in_place else (torch.empty_like(r), torch.empty_like(t))
+        n_live = torch.full((1,), -5, dtype=torch.int32, device=DEV)
+        ckv.page_compact(layers, r, ro, t, to, n_live, ws)
+        assert n_live.item() == L
+        assert ro.tolist() == want_refs and to.tolist() == want_table
+        for p, old in zip(layers.pools, before):
+            for x, o in zip((p.k, p.v, p.k_scale, p.v_scale), old):
+                if x is not None:
+                    assert torch.equal(bytes_of(x), o[come])
+
+
+def test_compact_without_pools_or_table():
+    import paper_2601_13631_amd as ckv
+    refs = torch.tensor([0, 1, 0, 2, 1], dtype=torch.int32, device=DEV)
+    out, n = torch.empty_like(refs), torch.empty(1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(ckv.page_compact_workspace_bytes(5), dtype=torch.uint8, device=DEV)
+    ckv.page_compact(ckv.PageLayers([]), refs, out, None, None, n, ws)
+    assert out.tolist() == [2, 1, 1, 0, 0] and n.item() == 3
+
+
+# ---- together ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("e4m3", H7), ("e4m3", H05), ("f32", HF)])
+def test_serving_loop(cache, heads):
+    """Two prompts appended and attended, one forked, decoding with a window, the first freed, the
+    pool made compact: each step against the host model of the same cache."""
+    import paper_2601_13631_amd as ckv
+    page, n_pages, width = 16, 40, 12
+    hq, hkv, d = heads
+    c = Cache(cache, heads, page, [(0, page)] * 3, seed=8, extra=n_pages - 3)
+    c.width, c.table = width, np.full((3, width), -1, np.int32)
+    pool = ckv.PagePool(*c.device_pages())
+    layers = ckv.PageLayers([pool])
+    refs = np.zeros(n_pages, np.int32)
+    g = torch.Generator().manual_seed(0)
+    lens = [0, 0, 0]
+
+    def step(new, window, sinks):
+        for b, n in enumerate(new):
+            lens[b] += n
+            for s in range(-(-lens[b] // page)):
+                if n and c.table[b, s] < 0:
+                    c.table[b, s] = int(np.nonzero(refs == 0)[0][-1])  # from the back: compaction has work
+                    refs[c.table[b, s]] = 1
+        c.seqs = [(n, m) for n, m in zip(new, lens)]
+        c.new, c.lens = np.array(new), np.array(lens, np.int32)
+        c.off = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        c.tokens = int(c.off[-1])
+        wide = c.q.dtype
+        c.q = torch.randn(c.tokens, hq, d, generator=g).to(wide)
+        c.new_rows = {n: torch.randn(c.tokens, hkv, d, generator=g).to(wide) for n in "kv"}
+        batch = ckv.PageBatch(torch.from_numpy(c.table).to(DEV), torch.from_numpy(c.lens).to(DEV),
+                              torch.from_numpy(c.off).to(DEV), c.tokens, max_tokens=max(new))
+        ckv.page_append(pool, batch, c.new_rows["k"].to(DEV), c.new_rows["v"].to(DEV))
+        c.append()
+        check_pages(c, pool.k, pool.v, pool.k_scale, pool.v_scale)
+        check_attention(c, attend(pool, batch, c.q.to(DEV), window, sinks), window, sinks)
+
+    step([70, 41, 0], 0, 0)
+    # fork sequence 1: shared pages, its last one copied
+    last = c.table[1, 2]
+    own = int(np.nonzero(refs == 0)[0][-1])
+    c.table[2] = c.table[1]
+    c.table[2, 2] = own
+    lens[2] = lens[1]
+    refs[c.table[1, :2]] += 1
+    refs[own] = 1
+    ckv.page_copy(layers, *(torch.tensor([int(x)], dtype=torch.int32, device=DEV) for x in (last, own)))
+    for n in "kv":
+        c.raw[n].view(torch.uint8)[own] = c.raw[n].view(torch.uint8)[last].clone()
+        if c.scale[n] is not None:
+            c.scale[n][own] = c.scale[n][last]
+    for _ in range(3):
+        step([1, 1, 1], 0, 0)
+    step([1, 9, 1], 24, 4)
+    # the first sequence ends
+    refs[c.table[0][c.table[0] >= 0]] -= 1
+    c.table[0] = -1
+    lens[0] = 0
+    L, come, want_refs, want_table = host_compact(refs.tolist(), c.table.reshape(-1).tolist(), n_pages)
+    table = torch.from_numpy(c.table).to(DEV)
+    r = torch.from_numpy(refs).to(DEV)
+    n_live = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(ckv.page_compact_workspace_bytes(n_pages), dtype=torch.uint8, device=DEV)
+    ckv.page_compact(layers, r, r, table, table, n_live, ws)
+    assert n_live.item() == L and r.tolist() == want_refs
+    refs[:] = r.cpu().numpy()
+    c.table[:] = table.cpu().numpy()
+    assert c.table.reshape(-1).tolist() == want_table
+    for n in "kv":
+        c.raw[n] = c.raw[n].view(torch.uint8)[come].view(c.raw[n].dtype).clone()
+        if c.scale[n] is not None:
+            c.scale[n] = c.scale[n][come].clone()
+    step([30, 1, 1], 0, 0)
+    step([0, 1, 40], 33, 1)
