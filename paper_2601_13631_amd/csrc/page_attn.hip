@@ -32,9 +32,11 @@ struct PageAttnArgs {
   void* out;
   float* o_part;        // [splits][n_tokens][Hq][D]
   float2* ml_part;      // [splits][n_tokens][Hq]: (reference, sum)
+  int32_t* n_parts;     // [n_tokens]: splits that the token's sequence takes
   int c, log2c;         // log2c: -1 if c is no power of two
   int Hkv, Hq, G;
   int window, sinks, n_splits;
+  int slice;            // steps that a sequence takes another split for
   float c1;
 };
 
@@ -59,11 +61,18 @@ __device__ __forceinline__ Steps steps_of(const PageAttnArgs& a, int p0, int p1,
   return s;
 }
 
-// Page and row inside it of the key at position pos of sequence table `tab`; page -1
-// where there is none.
-__device__ __forceinline__ int page_of(const PageAttnArgs& a, const int32_t* tab, int slot) {
-  const int page = slot < a.s.max_pages ? tab[slot] : -1;
-  return page >= 0 && page < a.n_pages ? page : -1;
+// The entry of a slot of a sequence's table (past its end: of its last slot, whose
+// page then counts as not there).
+__device__ __forceinline__ int entry_of(const PageAttnArgs& a, const int32_t* tab, int slot) {
+  return tab[min(slot, a.s.max_pages - 1)];
+}
+// The same, for a slot that is one for the wave: a scalar load, which the wait for
+// rows in flight does not include.
+__device__ __forceinline__ int entry_of_uniform(const PageAttnArgs& a, const int32_t* tab, int slot) {
+  return *(const __attribute__((address_space(4))) int32_t*)(tab + min(slot, a.s.max_pages - 1));
+}
+__device__ __forceinline__ bool names_page(const PageAttnArgs& a, int entry) {
+  return entry >= 0 && entry < a.n_pages;
 }
 
 template <int T>
@@ -82,6 +91,17 @@ template <>
 struct Elem<CKV_DTYPE_E4M3> {
   static constexpr int kBytes = 1;
   using Q = __bf16;
+};
+
+// What a wave holds of a step: table entries and rows, as loaded.
+struct Pages {
+  int k0, k1, v0, v1;
+};
+template <int D, int T>
+struct Step {
+  u32x4 k[2][D * Elem<T>::kBytes / 64];
+  uint32_t v[2][4][D / 16 * Elem<T>::kBytes / 4];
+  uint32_t ks[2], vs[2];
 };
 
 __device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
@@ -109,8 +129,10 @@ __device__ __forceinline__ bf16x8 bf16_of_codes(uint32_t w0, uint32_t w1, float 
 //                  product i of D/16 takes element i of each (8 keys x D/16 elements
 //                  are turned over in registers).
 // The waves' outputs are joined through LDS, the splits' by page_combine_kernel.
-template <int D, int T>
-__global__ __launch_bounds__(64 * kWaves) void page_rows_kernel(PageAttnArgs a) {
+// kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page, and
+// the page numbers are uniform).
+template <int D, int T, bool kSmall>
+__global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs a) {
   using E = Elem<T>;
   using QT = typename E::Q;
   constexpr bool kF32 = T == CKV_DTYPE_F32, kE4 = T == CKV_DTYPE_E4M3;
@@ -118,27 +140,38 @@ __global__ __launch_bounds__(64 * kWaves) void page_rows_kernel(PageAttnArgs a) 
   constexpr int kPieces = D * E::kBytes / 64;     // 16-byte pieces of a K row per lane
   constexpr int kVWords = kVec * E::kBytes / 4;   // dwords of a V row per lane
 
-  const int split = (int)(blockIdx.x / a.Hkv) % a.n_splits, g = (int)(blockIdx.x % a.Hkv);
-  const int b = (int)(blockIdx.x / ((uint32_t)a.Hkv * a.n_splits));
+  // The KV heads of one slice of keys are neighbours on one XCD, where together they read
+  // whole token rows.  The slices go round the XCDs, every sequence's first ones before the
+  // second ones and so on, turned by one from split to split: long sequences spread.
+  const uint32_t pair = blockIdx.x / 8 / a.Hkv * 8 + (blockIdx.x & 7);
+  if (pair >= (uint32_t)a.s.n_seqs * a.n_splits) return;
+  const int g = (int)(blockIdx.x / 8 % a.Hkv), split = (int)(pair / a.s.n_seqs);
+  const int b = (int)((pair + split) % a.s.n_seqs);
   const int lane = threadIdx.x & 63, n16 = lane & 15, j4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const SeqSpan sp = seq_span(a.s, b);
   if (sp.count == 0) return;
   const int32_t* tab = a.s.table + (int64_t)b * a.s.table_stride;
   const int kv_end = (int)min<int64_t>(max(sp.len, 0), (int64_t)a.s.max_pages * a.c);
-  const int row_bytes = a.Hkv * D * E::kBytes;
+  const int row_bytes = a.Hkv * D * E::kBytes, kvh = g, g_bytes = g * D * E::kBytes;
   const int64_t rows = (int64_t)sp.count * a.G;
+  const int p_base = sp.len - sp.count;
+  // this sequence's own number of splits, by its length
+  const int all_steps = steps_of(a, p_base, p_base + sp.count - 1, kv_end).n;
+  const int n_parts = min(max((all_steps + a.slice - 1) / a.slice, 1), a.n_splits);
+  if (split >= n_parts) return;
+  if (a.n_splits > 1 && split == 0 && g == 0 && blockIdx.y == 0)
+    for (int i = threadIdx.x; i < sp.count; i += 64 * kWaves) a.n_parts[sp.first + i] = n_parts;
 
   __shared__ float lds_o[kWaves][kRows][D + 4];
   __shared__ float2 lds_ml[kWaves][kRows];
 
   for (int64_t rb = blockIdx.y; rb * kRows < rows; rb += gridDim.y) {
     const int64_t r_first = rb * kRows, r_last = min<int64_t>(rows, r_first + kRows) - 1;
-    const int p_base = sp.len - sp.count;
     const int p0 = p_base + (int)(r_first / a.G), p1 = p_base + (int)(r_last / a.G);
     const Steps steps = steps_of(a, p0, p1, kv_end);
-    const int begin = (int)((int64_t)steps.n * split / a.n_splits);
-    const int end = (int)((int64_t)steps.n * (split + 1) / a.n_splits);
+    const int begin = (int)((int64_t)steps.n * split / n_parts);
+    const int end = (int)((int64_t)steps.n * (split + 1) / n_parts);
 
     // this lane's row: its query (position p) and head
     const int64_t r = min<int64_t>(r_first + n16, r_last);
@@ -165,72 +198,89 @@ __global__ __launch_bounds__(64 * kWaves) void page_rows_kernel(PageAttnArgs a) 
     for (int i = 0; i < kVec; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float ref = kNone, l = 0.f;
 
-    for (int st = begin + wave; st < end; st += kWaves) {
-      const int tile = steps.tile(st), pos0 = tile * kTile;
-      // pages of this lane's keys: K rows 16 i + n16, V rows 16 i + 4 j4 + 0..3
-      int kp[2], vp[2], kr[2], vr[2];
+    // Pages of a step's keys: this lane's K rows 16 i + n16, V rows 16 i + 4 j4 + 0..3.
+    auto slot_of = [&](int pos) { return a.log2c >= 0 ? pos >> a.log2c : (int)((uint32_t)pos / (uint32_t)a.c); };
+    auto pages_of = [&](int st, Pages& g) __attribute__((always_inline)) {
+      const int pos0 = steps.tile(st) * kTile;
+      if constexpr (!kSmall) {
+        g.k0 = g.v0 = entry_of_uniform(a, tab, slot_of(pos0));
+        g.k1 = g.v1 = entry_of_uniform(a, tab, slot_of(pos0 + 16));
+      } else {
+        const int k = (pos0 + n16) >> 3, v = (pos0 + 4 * j4) >> 3;
+        g.k0 = entry_of(a, tab, k);
+        g.k1 = entry_of(a, tab, k + 2);
+        g.v0 = entry_of(a, tab, v);
+        g.v1 = entry_of(a, tab, v + 2);
+      }
+    };
+    // Its rows (a key that is not there reads page 0 and counts for nothing).
+    auto load = [&](int st, const Pages& g, Step<D, T>& x) __attribute__((always_inline)) {
+      const int pos0 = steps.tile(st) * kTile;
+      const int pk[2] = {names_page(a, g.k0) ? g.k0 : 0, names_page(a, g.k1) ? g.k1 : 0};
+      const int pv[2] = {names_page(a, g.v0) ? g.v0 : 0, names_page(a, g.v1) ? g.v1 : 0};
+      if constexpr (kE4) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int pos = pos0 + 16 * i;
-        if (a.c >= 16) {
-          const int slot = a.log2c >= 0 ? pos >> a.log2c : (int)((uint32_t)pos / (uint32_t)a.c);
-          kp[i] = vp[i] = page_of(a, tab, slot);
-          kr[i] = pos - slot * a.c + n16;
-          vr[i] = pos - slot * a.c + 4 * j4;
-        } else {
-          kp[i] = page_of(a, tab, (pos + n16) >> 3);
-          vp[i] = page_of(a, tab, (pos + 4 * j4) >> 3);
-          kr[i] = n16 & 7;
-          vr[i] = (4 * j4) & 7;
+        for (int i = 0; i < 2; ++i) {
+          x.ks[i] = a.k_scale[(int64_t)pk[i] * a.Hkv + kvh];
+          x.vs[i] = a.v_scale[(int64_t)pv[i] * a.Hkv + kvh];
         }
       }
-      // a key that is not there reads page 0 and counts for nothing
-      u32x4 kw[2][kPieces];
-      uint32_t vw[2][4][kVWords];
-      float ks[2], vs[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const char* kr_at = a.k + (int64_t)max(kp[i], 0) * a.page_stride +
-                            (int64_t)kr[i] * row_bytes + g * D * E::kBytes + 16 * j4;
+        int kr = n16 & 7, vr = (4 * j4) & 7;  // rows inside the page
+        if constexpr (!kSmall) {
+          const int pos = pos0 + 16 * i;
+          const int in_page = a.log2c >= 0 ? pos & (a.c - 1) : (int)((uint32_t)pos % (uint32_t)a.c);
+          kr = in_page + n16;
+          vr = in_page + 4 * j4;
+        }
+        const char* k_at = a.k + (int64_t)pk[i] * a.page_stride + (int64_t)kr * row_bytes +
+                           g_bytes + 16 * j4;
 #pragma unroll
-        for (int x = 0; x < kPieces; ++x) kw[i][x] = *reinterpret_cast<const u32x4*>(kr_at + 64 * x);
-        const char* vr_at = a.v + (int64_t)max(vp[i], 0) * a.page_stride +
-                            (int64_t)vr[i] * row_bytes + (g * D + n16 * kVec) * E::kBytes;
+        for (int y = 0; y < kPieces; ++y) x.k[i][y] = *reinterpret_cast<const u32x4*>(k_at + 64 * y);
+        const char* v_at = a.v + (int64_t)pv[i] * a.page_stride + (int64_t)vr * row_bytes +
+                           g_bytes + n16 * kVec * E::kBytes;
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           if constexpr (kVWords == 4)
-            *reinterpret_cast<u32x4*>(vw[i][y]) = *reinterpret_cast<const u32x4*>(vr_at + y * row_bytes);
+            *reinterpret_cast<u32x4*>(x.v[i][y]) = *reinterpret_cast<const u32x4*>(v_at + y * row_bytes);
           else if constexpr (kVWords == 2)
-            *reinterpret_cast<uint2*>(vw[i][y]) = *reinterpret_cast<const uint2*>(vr_at + y * row_bytes);
+            *reinterpret_cast<uint2*>(x.v[i][y]) = *reinterpret_cast<const uint2*>(v_at + y * row_bytes);
           else
-            vw[i][y][0] = *reinterpret_cast<const uint32_t*>(vr_at + y * row_bytes);
-        }
-        if constexpr (kE4) {
-          ks[i] = scale_of(a.k_scale[(int64_t)max(kp[i], 0) * a.Hkv + g]);
-          vs[i] = scale_of(a.v_scale[(int64_t)max(vp[i], 0) * a.Hkv + g]);
+            x.v[i][y][0] = *reinterpret_cast<const uint32_t*>(v_at + y * row_bytes);
         }
       }
-      // logits
+    };
+    auto attend = [&](int st, const Pages& g, Step<D, T>& x) __attribute__((always_inline)) {
+      const int pos0 = steps.tile(st) * kTile;
+      float ks[2], vs[2];
+      if constexpr (kE4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          ks[i] = scale_of(x.ks[i]);
+          vs[i] = scale_of(x.vs[i]);
+        }
+      }
       f32x4 s[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         if constexpr (kF32) {
 #pragma unroll
-          for (int x = 0; x < kPieces; ++x)
+          for (int y = 0; y < kPieces; ++y)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[i][x][e]), qf[x][e], s[i], 0, 0, 0);
+              s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.k[i][y][e]), qf[y][e], s[i], 0, 0, 0);
         } else if constexpr (kE4) {
 #pragma unroll
-          for (int x = 0; x < D / 32; ++x)
+          for (int y = 0; y < D / 32; ++y)
             s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                bf16_of_codes(kw[i][x >> 1][2 * (x & 1)], kw[i][x >> 1][2 * (x & 1) + 1], ks[i]), qb[x],
+                bf16_of_codes(x.k[i][y >> 1][2 * (y & 1)], x.k[i][y >> 1][2 * (y & 1) + 1], ks[i]), qb[y],
                 s[i], 0, 0, 0);
         } else {
 #pragma unroll
-          for (int x = 0; x < D / 32; ++x)
-            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw[i][x]), qb[x],
+          for (int y = 0; y < D / 32; ++y)
+            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[i][y]), qb[y],
                                                            s[i], 0, 0, 0);
         }
       }
@@ -238,20 +288,21 @@ __global__ __launch_bounds__(64 * kWaves) void page_rows_kernel(PageAttnArgs a) 
       const int last = pos0 + kTile;
       const bool all = last <= min(p0 + 1, kv_end) &&
                        (a.window <= 0 || pos0 > p1 - a.window || last <= a.sinks);
-      if (!all || __any(vp[0] < 0 || vp[1] < 0)) {
+      const bool there0 = names_page(a, g.v0), there1 = names_page(a, g.v1);
+      if (!all || __any(!there0 || !there1)) {
         const int lo = a.window > 0 ? p0 - a.window : -1;  // the block's first row sees keys past it
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const int pos = pos0 + 16 * i + 4 * j4 + y;
-            const bool there = vp[i] >= 0 && pos < kv_end;
+            const bool there = (i ? there1 : there0) && pos < kv_end;
             if (!(there && pos <= p && (a.window <= 0 || pos > p - a.window || pos < a.sinks)))
               s[i][y] = -INFINITY;
             // a weight of 0 does not undo a NaN: rows that no query of the block sees are cleared
             if (!(there && pos <= p1 && (pos > lo || pos < a.sinks)))
 #pragma unroll
-              for (int w = 0; w < kVWords; ++w) vw[i][y][w] = 0u;
+              for (int w = 0; w < kVWords; ++w) x.v[i][y][w] = 0u;
           }
       }
       float mx = -INFINITY;
@@ -284,32 +335,59 @@ __global__ __launch_bounds__(64 * kWaves) void page_rows_kernel(PageAttnArgs a) 
 #pragma unroll
           for (int y = 0; y < 4; ++y)
 #pragma unroll
-            for (int x = 0; x < kVec; ++x)
-              o[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[i][y][x]), s[i][y], o[x], 0, 0, 0);
+            for (int e = 0; e < kVec; ++e)
+              o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][y][e]), s[i][y], o[e], 0, 0, 0);
       } else {
         u32x4 pb;
 #pragma unroll
         for (int i = 0; i < 4; ++i) pb[i] = bf16_pair(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
 #pragma unroll
-        for (int x = 0; x < kVec; ++x) {
-          u32x4 vt;  // element x of the 8 keys
+        for (int e = 0; e < kVec; ++e) {
+          u32x4 vt;  // element e of the 8 keys
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t* r0 = vw[i >> 1][2 * (i & 1)];
-            const uint32_t* r1 = vw[i >> 1][2 * (i & 1) + 1];
+            const uint32_t* r0 = x.v[i >> 1][2 * (i & 1)];
+            const uint32_t* r1 = x.v[i >> 1][2 * (i & 1) + 1];
             if constexpr (kE4) {
-              // codes of elements 2 (x / 2) and + 1 of both keys, then the pair of element x
-              const uint32_t w = __builtin_amdgcn_perm(r1[x >> 2], r0[x >> 2], x & 2 ? 0x07030602u : 0x05010400u);
+              // codes of elements 2 (e / 2) and + 1 of both keys, then the pair of element e
+              const uint32_t w = __builtin_amdgcn_perm(r1[e >> 2], r0[e >> 2], e & 2 ? 0x07030602u : 0x05010400u);
               vt[i] = __builtin_bit_cast(
-                  uint32_t, x & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, vs[i >> 1], true)
+                  uint32_t, e & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, vs[i >> 1], true)
                                   : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, vs[i >> 1], false));
             } else {
-              vt[i] = __builtin_amdgcn_perm(r1[x >> 1], r0[x >> 1], x & 1 ? 0x07060302u : 0x05040100u);
+              vt[i] = __builtin_amdgcn_perm(r1[e >> 1], r0[e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
             }
           }
-          o[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt),
-                                                         __builtin_bit_cast(bf16x8, pb), o[x], 0, 0, 0);
+          o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt),
+                                                         __builtin_bit_cast(bf16x8, pb), o[e], 0, 0, 0);
         }
+      }
+    };
+
+    // Each step's rows load during the step before, its table entries two steps before
+    // (and ahead of the rows that load meanwhile, for which they need not wait then).
+    // Past the end a wave reads its last step's rows once more.
+    int st = begin + wave;
+    if (st < end) {
+      Pages ga, gb;
+      Step<D, T> xa, xb;
+      pages_of(st, ga);
+      pages_of(min(st + kWaves, end - 1), gb);
+      load(st, ga, xa);
+      auto turn = [&](Pages& g, Step<D, T>& x, const Pages& gn, Step<D, T>& xn)
+          __attribute__((always_inline)) {
+        Pages after;
+        pages_of(min(st + 2 * kWaves, end - 1), after);
+        load(min(st + kWaves, end - 1), gn, xn);
+        attend(st, g, x);
+        g = after;
+        st += kWaves;
+      };
+      while (true) {
+        turn(ga, xa, gb, xb);
+        if (st >= end) break;
+        turn(gb, xb, ga, xa);
+        if (st >= end) break;
       }
     }
 
@@ -342,7 +420,7 @@ __global__ __launch_bounds__(64 * kWaves) void page_rows_kernel(PageAttnArgs a) 
         for (int w = 0; w < kWaves; ++w) acc[x] += f[w] * lds_o[w][row][col + x];
       }
       const int64_t at = (sp.first + rr / a.G) * a.Hq + g * a.G + rr % a.G;
-      if (a.n_splits > 1) {
+      if (n_parts > 1) {
         const int64_t prow = (int64_t)split * a.s.n_tokens * a.Hq + at;
         float* dst = a.o_part + prow * D + col;
 #pragma unroll
@@ -364,35 +442,59 @@ __global__ __launch_bounds__(64 * kWaves) void page_rows_kernel(PageAttnArgs a) 
   }
 }
 
-// Joins the splits of each row in split order.  D / 4 threads per row.
+// Joins a row's splits, a workgroup per row: 256 / (D / 4) groups of threads take the
+// splits in turn, 4 elements a thread, and meet in LDS (in a fixed order).
 template <int D, class QT>
 __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (D / 4);
-  const int col = (int)(i % (D / 4)) * 4;
-  const int64_t n_rows = a.s.n_tokens * a.Hq, tok = row / a.Hq;
-  if (row >= n_rows) return;
+  constexpr int kCols = D / 4, kGroups = 256 / kCols, kBatch = 8;
+  const int64_t row = blockIdx.x, n_rows = a.s.n_tokens * a.Hq, tok = row / a.Hq;
   if (tok < a.s.tok_off[0] || tok >= a.s.tok_off[a.s.n_seqs]) return;  // of no sequence
+  const int n_parts = min(a.n_parts[tok], a.n_splits);
+  if (n_parts <= 1) return;  // written already
+  const int col = threadIdx.x % kCols * 4, grp = threadIdx.x / kCols;
   float M = kNone, L = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  constexpr int kBatch = 8;  // splits whose loads are in flight together
-  for (int s0 = 0; s0 < a.n_splits; s0 += kBatch) {
+  for (int s0 = grp; s0 < n_parts; s0 += kGroups * kBatch) {
     float2 ml[kBatch];
     f32x4 x[kBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int64_t at = (int64_t)min(s0 + k, a.n_splits - 1) * n_rows + row;
+    for (int k = 0; k < kBatch; ++k) {  // all in flight together
+      const int64_t at = (int64_t)min(s0 + k * kGroups, n_parts - 1) * n_rows + row;
       ml[k] = a.ml_part[at];
       x[k] = *reinterpret_cast<const f32x4*>(a.o_part + at * D + col);
     }
+    float to = M;
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      if (s0 + k >= a.n_splits || !(ml[k].y > 0.f)) continue;
-      const float to = fmaxf(M, ml[k].x);
-      const float f = __builtin_amdgcn_exp2f(M - to), w = __builtin_amdgcn_exp2f(ml[k].x - to);
-      M = to;
-      L = L * f + ml[k].y * w;
-      acc = acc * f + x[k] * w;
+      if (s0 + k * kGroups >= n_parts) ml[k] = make_float2(kNone, 0.f);
+      to = fmaxf(to, ml[k].x);
     }
+    const float f = __builtin_amdgcn_exp2f(M - to);
+    M = to;
+    L *= f;
+    acc *= f;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const float w = __builtin_amdgcn_exp2f(ml[k].x - to);
+      L += ml[k].y * w;
+      acc += x[k] * w;  // (a split that saw no key wrote zeros)
+    }
+  }
+  __shared__ f32x4 part[kGroups][kCols];
+  __shared__ float2 part_ml[kGroups];
+  part[grp][threadIdx.x % kCols] = acc;
+  if (col == 0) part_ml[grp] = make_float2(M, L);
+  __syncthreads();
+  if (grp > 0) return;
+#pragma unroll
+  for (int k = 1; k < kGroups; ++k) M = fmaxf(M, part_ml[k].x);
+  L = 0.f;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kGroups; ++k) {
+    const float w = __builtin_amdgcn_exp2f(part_ml[k].x - M);
+    L += part_ml[k].y * w;
+    acc += part[k][threadIdx.x] * w;
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
   QT y[4];
@@ -406,9 +508,9 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
 }
 
 struct PageAttnPlan {
-  int n_splits;
+  int n_splits, slice;
   int row_blocks;  // grid y
-  size_t off_ml, bytes;
+  size_t off_ml, off_n, bytes;
 };
 
 PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq, int window, int sinks) {
@@ -420,11 +522,14 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
   if (b->max_len > 0) len = std::min<int64_t>(len, b->max_len);
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + most + sinks + 2 * kTile);
   const int64_t steps = ceil_div(len, kTile), wgs = (int64_t)b->n_seqs * pool->n_kv_heads * p.row_blocks;
-  p.n_splits = (int)std::max<int64_t>(1, std::min(1024 / std::max<int64_t>(wgs, 1), steps / 8));
+  p.n_splits = (int)std::max<int64_t>(1, std::min(4096 / std::max<int64_t>(wgs, 1), steps / 16));
+  p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
   const size_t rows = (size_t)b->n_tokens * Hq;
+  if (rows >= (size_t)kMaxGrid) p.n_splits = 1;  // (the join has a workgroup per row)
   if (p.n_splits > 1) {
     p.off_ml = align_up((size_t)p.n_splits * rows * pool->head_dim * sizeof(float), 256);
-    p.bytes = align_up(p.off_ml + (size_t)p.n_splits * rows * sizeof(float2), 256);
+    p.off_n = align_up(p.off_ml + (size_t)p.n_splits * rows * sizeof(float2), 256);
+    p.bytes = align_up(p.off_n + (size_t)b->n_tokens * sizeof(int32_t), 256);
   }
   return p;
 }
@@ -445,13 +550,14 @@ ckv_status check_attn(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq
 
 template <int D, int T>
 ckv_status launch_page_attn(const PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) {
-  const int64_t wgs = (int64_t)a.s.n_seqs * a.Hkv * a.n_splits;
+  const int64_t wgs = (int64_t)align_up((size_t)a.s.n_seqs * a.n_splits, 8) * a.Hkv;
   if (wgs >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
-  hipLaunchKernelGGL((page_rows_kernel<D, T>), dim3((unsigned)wgs, (unsigned)p.row_blocks),
+  const auto kernel = a.c == 8 ? page_rows_kernel<D, T, true> : page_rows_kernel<D, T, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)p.row_blocks),
                      dim3(64 * kWaves), 0, st, a);
   CKV_HIP(hipGetLastError());
   if (a.n_splits > 1) {
-    const int64_t blocks = ceil_div(a.s.n_tokens * a.Hq * (D / 4), 256);
+    const int64_t blocks = a.s.n_tokens * a.Hq;
     hipLaunchKernelGGL((page_combine_kernel<D, typename Elem<T>::Q>), dim3((unsigned)blocks), dim3(256),
                        0, st, a);
     CKV_HIP(hipGetLastError());
@@ -499,6 +605,8 @@ ckv_status ckv_page_attn(const ckv_page_pool* pool, const ckv_page_batch* batch,
   a.out = out;
   a.o_part = static_cast<float*>(ws);
   a.ml_part = p.bytes ? reinterpret_cast<float2*>(static_cast<char*>(ws) + p.off_ml) : nullptr;
+  a.n_parts = p.bytes ? reinterpret_cast<int32_t*>(static_cast<char*>(ws) + p.off_n) : nullptr;
+  a.slice = p.slice;
   a.c = pool->page_size;
   a.log2c = (a.c & (a.c - 1)) == 0 ? __builtin_ctz(a.c) : -1;
   a.Hkv = pool->n_kv_heads;
