@@ -6,6 +6,7 @@
 // for any reference m.  A key is seen if j <= p, its page is there, and (window > 0)
 // j > p - window or j < n_sinks.
 
+#include "attn_tile.h"
 #include "pages_internal.h"
 
 namespace ckv {
@@ -36,17 +37,19 @@ struct PageAttnArgs {
   int c, log2c;         // log2c: -1 if c is no power of two
   int Hkv, Hq, G;
   int window, sinks, n_splits;
+  uint32_t n_blocks;    // blocks of 128 rows, at most (page_tile_kernel)
   int slice;            // steps that a sequence takes another split for
   float c1;
 };
 
-// The keys of a block of rows as steps of kTile: those that hold the sinks, then those
-// from the window's begin on.
+// The keys of a block of rows as steps of some tile of keys: those that hold the sinks,
+// then those from the window's begin on.
 struct Steps {
   int n_sink, first, n;  // step i: tile i < n_sink ? i : first + i - n_sink
   __device__ __forceinline__ int tile(int i) const { return i < n_sink ? i : first + (i - n_sink); }
 };
 // For queries at positions p0 .. p1 of a sequence with keys below kv_end.
+template <int kTile>
 __device__ __forceinline__ Steps steps_of(const PageAttnArgs& a, int p0, int p1, int kv_end) {
   Steps s{0, 0, 0};
   const int hi = min(p1 + 1, kv_end);
@@ -157,7 +160,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
   const int64_t rows = (int64_t)sp.count * a.G;
   const int p_base = sp.len - sp.count;
   // this sequence's own number of splits, by its length
-  const int all_steps = steps_of(a, p_base, p_base + sp.count - 1, kv_end).n;
+  const int all_steps = steps_of<kTile>(a, p_base, p_base + sp.count - 1, kv_end).n;
   const int n_parts = min(max((all_steps + a.slice - 1) / a.slice, 1), a.n_splits);
   if (split >= n_parts) return;
   if (a.n_splits > 1 && split == 0 && g == 0 && blockIdx.y == 0)
@@ -169,7 +172,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
   for (int64_t rb = blockIdx.y; rb * kRows < rows; rb += gridDim.y) {
     const int64_t r_first = rb * kRows, r_last = min<int64_t>(rows, r_first + kRows) - 1;
     const int p0 = p_base + (int)(r_first / a.G), p1 = p_base + (int)(r_last / a.G);
-    const Steps steps = steps_of(a, p0, p1, kv_end);
+    const Steps steps = steps_of<kTile>(a, p0, p1, kv_end);
     const int begin = (int)((int64_t)steps.n * split / n_parts);
     const int end = (int)((int64_t)steps.n * (split + 1) / n_parts);
 
@@ -442,6 +445,358 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
   }
 }
 
+// Many rows: a workgroup owns 128 query rows (4 waves x 32) of one KV head and one split
+// of their 64-key stages; K and V go through LDS as bf16, two stages of buffers:
+//   S^T = K Q^T   MFMA 32x32x16 in two halves of 32 keys: a lane owns one row, 16 keys
+//   O^T += V^T P^T  V^T by transposing LDS reads, P^T from the softmax registers
+// bf16 rows go from memory straight to LDS, a page per load (8 keys of a stage lie in
+// one page).  8-bit rows come through registers, a stage further ahead, and are written
+// as bf16.  A row's reference is the ceiling of its maximum so far, followed once a half's
+// logits pass it by kSlack: rescalings are rare, and powers of two, so that numerators
+// already rounded lose nothing.
+template <int D, int T>
+__global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
+  using namespace tile;
+  using St = Stage<D>;
+  constexpr int kKeys = tile::kTile;
+  constexpr bool kE4 = T == CKV_DTYPE_E4M3;
+  __shared__ __attribute__((aligned(16))) uint16_t k0[kKeys * D], k1[kKeys * D];
+  __shared__ __attribute__((aligned(16))) uint16_t v0[kKeys * D], v1[kKeys * D];
+
+  // Blocks of rows that read the same keys (of one head and split: a stream) share an
+  // XCD's L2.  Streams go to the XCDs in turn; where there are fewer of them (1, 2, 4),
+  // a stream's blocks go to its XCDs in turn.  The last rows see the most keys: first.
+  const uint32_t streams = a.Hkv * a.n_splits, xcd = blockIdx.x & 7, idx = blockIdx.x >> 3;
+  uint32_t stream, blk;
+  if (8 % streams == 0) {
+    stream = xcd % streams;
+    blk = idx * (8 / streams) + xcd / streams;
+  } else {
+    stream = idx / a.n_blocks * 8 + xcd;
+    blk = idx % a.n_blocks;
+  }
+  if (stream >= streams || blk >= a.n_blocks) return;
+  const int g = (int)(stream % a.Hkv), split = (int)(stream / a.Hkv);
+  int64_t rb = a.n_blocks - 1 - blk;
+  SeqSpan sp{};
+  const int b = find_part(
+      a.s, [&](const SeqSpan& q) { return (int)(((int64_t)q.count * a.G + kBlockRows - 1) / kBlockRows); }, rb, sp);
+  if (b < 0) return;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t* tab = a.s.table + (int64_t)b * a.s.table_stride;
+  const int kv_end = (int)min<int64_t>(max(sp.len, 0), (int64_t)a.s.max_pages * a.c);
+  const int rows = sp.count * a.G, r_first = (int)rb * kBlockRows, r_last = min(rows, r_first + kBlockRows) - 1;
+  const int p_base = sp.len - sp.count;
+  const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
+  const int all_steps = steps_of<kKeys>(a, p_base, p_base + sp.count - 1, kv_end).n;
+  const int n_parts = min(max((all_steps + a.slice - 1) / a.slice, 1), a.n_splits);
+  if (split >= n_parts) return;
+  if (a.n_splits > 1 && split == 0 && g == 0)
+    for (int i = r_first / a.G + (int)threadIdx.x; i <= r_last / a.G; i += 256) a.n_parts[sp.first + i] = n_parts;
+  const Steps steps = steps_of<kKeys>(a, p0, p1, kv_end);
+  const int begin = (int)((int64_t)steps.n * split / n_parts);
+  const int end = (int)((int64_t)steps.n * (split + 1) / n_parts);
+
+  // this lane's row
+  const int row = r_first + wave * kWaveRows + (lane & 31);
+  const bool row_ok = row <= r_last;
+  const int rt = (row_ok ? row : r_last) / a.G;
+  const int p = row_ok ? p_base + rt : INT32_MIN / 2;
+  const int64_t out_row = (sp.first + rt) * a.Hq + g * a.G + (row_ok ? row : r_last) % a.G;
+  bf16x8 qf[D / 16];
+  {
+    const __bf16* q = static_cast<const __bf16*>(a.q) + out_row * D + 8 * half;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(q + 16 * i);
+  }
+
+  // Table entries of a stage: lane l has that of keys 8 (l % 8) .. + 7.
+  auto entries = [&](int st) __attribute__((always_inline)) {
+    const int pos = steps.tile(min(st, end - 1)) * kKeys + 8 * (lane & 7);
+    return entry_of(a, tab, a.log2c >= 0 ? pos >> a.log2c : (int)((uint32_t)pos / (uint32_t)a.c));
+  };
+  // Row of its page that the key at pos is.
+  auto in_page = [&](int pos) { return a.log2c >= 0 ? pos & (a.c - 1) : (int)((uint32_t)pos % (uint32_t)a.c); };
+  const int row_bytes = a.Hkv * D * Elem<T>::kBytes;
+
+  // bf16: this lane's byte of the rows that a load moves (the LDS permutation undone)
+  const int key0 = wave * St::kRowsPerLoad + lane / St::kSegs;
+  const uint32_t kcol = (uint32_t)(lane / St::kSegs * row_bytes + 2 * (g * D + ((lane % St::kSegs ^ k_swz<D>(key0)) << 3)));
+  const uint32_t vcol = (uint32_t)(lane / St::kSegs * row_bytes + 2 * (g * D + ((lane % St::kSegs ^ v_swz<D>(key0)) << 3)));
+  auto load_direct = [&](int st, int ent, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
+    const int pos0 = steps.tile(st) * kKeys;
+    ent = names_page(a, ent) ? ent : 0;
+#pragma unroll
+    for (int i = 0; i < St::kPer; ++i) {
+      const int key = i * St::kKeyStep + wave * St::kRowsPerLoad;
+      const int64_t off = (int64_t)__builtin_amdgcn_readlane(ent, key >> 3) * a.page_stride +
+                          (int64_t)in_page(pos0 + key) * row_bytes;
+      buffer_to_lds(raw_rsrc(a.k + off, 0xffffffffu), kcol, 0, dk + key * D);
+      buffer_to_lds(raw_rsrc(a.v + off, 0xffffffffu), vcol, 0, dv + key * D);
+    }
+  };
+  // 8 bits: 16 codes of a row per lane and load, kLoads loads of kERows rows per wave
+  constexpr int kELanes = D / 16, kERows = 64 / kELanes, kLoads = kKeys / (4 * kERows);
+  struct Codes {
+    u32x4 k[kLoads], v[kLoads];
+    uint32_t ks, vs;  // scale bytes of the stage, as its entries
+  };
+  auto load_codes = [&](int st, int ent, Codes& x) __attribute__((always_inline)) {
+    const int pos0 = steps.tile(min(st, end - 1)) * kKeys;
+    ent = names_page(a, ent) ? ent : 0;
+    x.ks = a.k_scale[(int64_t)ent * a.Hkv + g];
+    x.vs = a.v_scale[(int64_t)ent * a.Hkv + g];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int key = (4 * i + wave) * kERows;
+      // (at D = 64 a load has rows of two groups of 8 keys)
+      int page, r;
+      if constexpr (kERows == 8) {
+        page = __builtin_amdgcn_readlane(ent, key >> 3);
+        r = in_page(pos0 + key) + lane / kELanes;
+      } else {
+        const int up = lane >> 5;
+        const int e0 = __builtin_amdgcn_readlane(ent, key >> 3), e1 = __builtin_amdgcn_readlane(ent, (key >> 3) + 1);
+        const int r0 = in_page(pos0 + key), r1 = in_page(pos0 + key + 8);
+        page = up ? e1 : e0;
+        r = (up ? r1 : r0) + (lane / kELanes & 7);
+      }
+      const int64_t off = (int64_t)page * a.page_stride + (int64_t)r * row_bytes + g * D + lane % kELanes * 16;
+      x.k[i] = *reinterpret_cast<const u32x4*>(a.k + off);
+      x.v[i] = *reinterpret_cast<const u32x4*>(a.v + off);
+    }
+  };
+  auto write_codes = [&](const Codes& x, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int first = (4 * i + wave) * kERows, key = first + lane / kELanes, seg = 2 * (lane % kELanes);
+      float ks, vs;
+      if constexpr (kERows == 8) {
+        ks = scale_of(__builtin_amdgcn_readlane(x.ks, first >> 3));
+        vs = scale_of(__builtin_amdgcn_readlane(x.vs, first >> 3));
+      } else {
+        const int a0 = __builtin_amdgcn_readlane(x.ks, first >> 3), a1 = __builtin_amdgcn_readlane(x.ks, (first >> 3) + 1);
+        const int b0 = __builtin_amdgcn_readlane(x.vs, first >> 3), b1 = __builtin_amdgcn_readlane(x.vs, (first >> 3) + 1);
+        ks = scale_of(lane >> 5 ? a1 : a0);
+        vs = scale_of(lane >> 5 ? b1 : b0);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        *reinterpret_cast<bf16x8*>(dk + key * D + (((seg + h) ^ k_swz<D>(key)) << 3)) =
+            bf16_of_codes(x.k[i][2 * h], x.k[i][2 * h + 1], ks);
+        *reinterpret_cast<bf16x8*>(dv + key * D + (((seg + h) ^ v_swz<D>(key)) << 3)) =
+            bf16_of_codes(x.v[i][2 * h], x.v[i][2 * h + 1], vs);
+      }
+    }
+  };
+
+  // byte offsets of the operand reads (the same for every stage)
+  const int kr = kappa(lane & 31);
+  const uint32_t kfo = 2 * (kr * D + ((half ^ k_swz<D>(kr)) << 3));
+  const int s16 = lane & 15, g4 = (lane >> 4) & 1;
+  const uint32_t voff = 2 * (v_off<D>(8 * half + (s16 >> 2), 2 * g4 + ((s16 & 3) >> 1)) + 4 * (s16 & 1));
+
+  constexpr int kG = D / 16;  // MFMAs of one 32-key product, and of one O update
+  constexpr int kE = 256 / D; // logits per numerator step: kG + 2 steps per half
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
+  float l[2] = {0.f, 0.f}, ref = kNone;
+
+  // -inf where this lane's row must not see a key of half `sub`; `there`: bit i, the page
+  // of the stage's keys 8 i .. + 7.
+  auto mask = [&](int pos0, int sub, uint32_t there, f32x16& s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {  // 4 keys of one group of 8
+      int key = kSub * sub + 16 * (q >> 1) + 4 * (q & 1) + 8 * half;
+      asm volatile("" : "+v"(key));  // nothing of this (rare) path is kept across stages
+      const int pos = pos0 + key;
+      const bool page = there >> (key >> 3) & 1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = pos + e;
+        const bool see = page && j <= p && j < kv_end && (a.window <= 0 || j > p - a.window || j < a.sinks);
+        s[4 * q + e] = see ? s[4 * q + e] : -INFINITY;
+      }
+    }
+  };
+  // The reference follows the logits of a half; pb: numerators rounded against the old one.
+  auto follow = [&](const f32x16& s, u32x4* pb) __attribute__((always_inline)) {
+    float mx = max16(s) * a.c1;
+    if (__any(mx > ref + kSlack)) {
+      mx = fmaxf(mx, partner_f(mx));
+      const float to = fmaxf(ceilf(mx), ref), f = __builtin_amdgcn_exp2f(ref - to);
+      ref = to;
+      l[0] *= f;
+      l[1] *= f;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[db][v] *= f;
+      if (pb) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t w = pb[i >> 2][i & 3];
+          const uint32_t lo = __float_as_uint(__uint_as_float(w << 16) * f);
+          const uint32_t hi = __float_as_uint(__uint_as_float(w & 0xffff0000u) * f);
+          pb[i >> 2][i & 3] = (hi & 0xffff0000u) | lo >> 16;
+        }
+      }
+    }
+  };
+
+  if (begin < end) {
+    // entries of the current stage and of the ones after it
+    int ent = entries(begin), ent1 = entries(begin + 1), ent2 = 0;
+    Codes codes;
+    if constexpr (kE4) {
+      ent2 = entries(begin + 2);
+      load_codes(begin, ent, codes);
+      write_codes(codes, k0, v0);
+      load_codes(begin + 1, ent1, codes);
+    } else {
+      load_direct(begin, ent, k0, v0);
+    }
+    stage_barrier();
+    bf16x8 ka[kG];  // K fragments of the current stage's first 32 keys
+#pragma unroll
+    for (int i = 0; i < kG; ++i) ka[i] = read_k<D>(k0, kfo, 0, i);
+
+    auto stage = [&](int st, uint16_t* lk, uint16_t* lv, uint16_t* nk, uint16_t* nv)
+        __attribute__((always_inline)) {
+      uint32_t ko = kfo, vo = voff;
+      asm volatile("" : "+v"(ko), "+v"(vo));
+      const int pos0 = steps.tile(st) * kKeys, last = pos0 + kKeys;
+      // what some row of the block must not see, and which pages are there
+      const uint32_t there = (uint32_t)__ballot(names_page(a, ent)) & 0xffu;
+      const bool edge = there != 0xffu || last > min(p0 + 1, kv_end) ||
+                        (a.window > 0 && pos0 <= p1 - a.window && last > a.sinks);
+      int after;
+      if constexpr (kE4) {
+        if (st + 1 < end) write_codes(codes, nk, nv);
+        after = entries(st + 3);
+        if (st + 2 < end) load_codes(st + 2, ent2, codes);
+      } else {
+        after = entries(st + 2);
+        if (st + 1 < end) load_direct(st + 1, ent1, nk, nv);
+      }
+      if (edge) {
+        // a weight of 0 does not undo a NaN: V rows that no query of the block sees are cleared
+        for (int i = threadIdx.x; i < kKeys * (D / 8); i += 256) {
+          const int key = i / (D / 8), pos = pos0 + key;
+          if (!((there >> (key >> 3) & 1) && pos < kv_end && pos <= p1 &&
+                (a.window <= 0 || pos > p0 - a.window || pos < a.sinks)))
+            *reinterpret_cast<u32x4*>(lv + i * 8) = u32x4{0u, 0u, 0u, 0u};
+        }
+        __syncthreads();
+      }
+      bf16x8 kb[kG], va[2][D / 32], vb[2][D / 32];
+      f32x16 s0, s1;
+      u32x4 p0b[2], p1b[2];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<kG>([&](auto i) __attribute__((always_inline)) {
+        kb[i] = read_k<D>(lk, ko, 1, i);
+        s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[i], qf[i], s0, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if (edge) mask(pos0, 0, there, s0);
+      follow(s0, nullptr);
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<kG>([&](auto i) __attribute__((always_inline)) {
+        constexpr int kk = i / (D / 32), db = i % (D / 32);
+        va[kk][db] = read_v<D>(lv, vo, 0, kk, db);
+        s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[i], qf[i], s1, 0, 0, 0);
+        numerator_step<kE, i>(s0, a.c1, ref, l, p0b);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      numerator_step<kE, kG>(s0, a.c1, ref, l, p0b);
+      numerator_step<kE, kG + 1>(s0, a.c1, ref, l, p0b);
+      if (edge) mask(pos0, 1, there, s1);
+      follow(s1, p0b);
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<kG>([&](auto i) __attribute__((always_inline)) {
+        constexpr int kk = i / (D / 32), db = i % (D / 32);
+        vb[kk][db] = read_v<D>(lv, vo, 1, kk, db);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[kk][db], __builtin_bit_cast(bf16x8, p0b[kk]),
+                                                        o[db], 0, 0, 0);
+        numerator_step<kE, i>(s1, a.c1, ref, l, p1b);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (kE4) {  // the next stage's rows are written; loads stay in flight
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+      } else {
+        stage_barrier();  // the next stage has landed; this one's buffers are read
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<kG>([&](auto i) __attribute__((always_inline)) {
+        constexpr int kk = i / (D / 32), db = i % (D / 32);
+        ka[i] = read_k<D>(nk, ko, 0, i);  // (after the last stage: read and not used)
+        if constexpr (i < 2) numerator_step<kE, kG + i>(s1, a.c1, ref, l, p1b);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[kk][db], __builtin_bit_cast(bf16x8, p1b[kk]),
+                                                        o[db], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      ent = ent1;
+      if constexpr (kE4) {
+        ent1 = ent2;
+        ent2 = after;
+      } else {
+        ent1 = after;
+      }
+    };
+    for (int st = begin; st < end; st += 2) {
+      stage(st, k0, v0, k1, v1);
+      if (st + 1 >= end) break;
+      stage(st + 1, k1, v1, k0, v0);
+    }
+  }
+  l[0] += l[1];
+  l[0] += partner_f(l[0]);
+
+  // o[db][v] holds d = 32*db + 8*(v/4) + 4*half + v%4 of this lane's row
+  if (n_parts > 1) {
+    if (!row_ok) return;
+    const int64_t prow = (int64_t)split * a.s.n_tokens * a.Hq + out_row;
+    float* dst = a.o_part + prow * D + 4 * half;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(dst + 32 * db + 8 * q) =
+            f32x4{o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
+    if (half == 0) a.ml_part[prow] = make_float2(ref, l[0]);
+    return;
+  }
+  // Output rows through LDS, so that a store is a whole 16-byte piece of a row and 16 lanes
+  // cover a row: the wave's rows go to a stage buffer of its own, which no wave reads for
+  // its values any more.
+  const float inv = l[0] > 0.f ? 1.f / l[0] : 0.f;
+  constexpr int kRow = D + 8, kSegs = D / 8, kRowsPerPass = 64 / kSegs;
+  uint16_t* rows_of = wave == 0 ? k0 : wave == 1 ? k1 : wave == 2 ? v0 : v1;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<uint2*>(rows_of + (lane & 31) * kRow + 32 * db + 8 * q + 4 * half) =
+          make_uint2(bf16_pair(o[db][4 * q] * inv, o[db][4 * q + 1] * inv),
+                     bf16_pair(o[db][4 * q + 2] * inv, o[db][4 * q + 3] * inv));
+#pragma unroll
+  for (int r0 = 0; r0 < kWaveRows; r0 += kRowsPerPass) {
+    const int rr = r0 + lane / kSegs;
+    const uint4 x = *reinterpret_cast<const uint4*>(rows_of + rr * kRow + lane % kSegs * 8);
+    const int64_t at = __shfl(out_row, rr);
+    if (r_first + wave * kWaveRows + rr <= r_last)
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * D + lane % kSegs * 8) = x;
+  }
+}
+
 // Joins a row's splits, a workgroup per row: 256 / (D / 4) groups of threads take the
 // splits in turn, 4 elements a thread, and meet in LDS (in a fixed order).
 template <int D, class QT>
@@ -508,8 +863,10 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
 }
 
 struct PageAttnPlan {
+  bool wide;       // page_tile_kernel
   int n_splits, slice;
-  int row_blocks;  // grid y
+  int row_blocks;  // page_rows_kernel: grid y
+  int64_t blocks;  // page_tile_kernel: blocks of rows, at most
   size_t off_ml, off_n, bytes;
 };
 
@@ -517,13 +874,24 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
   PageAttnPlan p{};
   const int G = Hq / pool->n_kv_heads;
   const int64_t most = b->max_tokens > 0 ? std::min<int64_t>(b->max_tokens, b->n_tokens) : b->n_tokens;
-  p.row_blocks = (int)std::min<int64_t>(65535, std::max<int64_t>(1, ceil_div(most * G, kRows)));
   int64_t len = (int64_t)b->max_pages * pool->page_size;
   if (b->max_len > 0) len = std::min<int64_t>(len, b->max_len);
-  if (window > 0) len = std::min<int64_t>(len, (int64_t)window + most + sinks + 2 * kTile);
-  const int64_t steps = ceil_div(len, kTile), wgs = (int64_t)b->n_seqs * pool->n_kv_heads * p.row_blocks;
-  p.n_splits = (int)std::max<int64_t>(1, std::min(4096 / std::max<int64_t>(wgs, 1), steps / 16));
-  p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
+  p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32;
+  if (p.wide) {
+    p.blocks = b->n_tokens * G / tile::kBlockRows + b->n_seqs;
+    if (window > 0) len = std::min<int64_t>(len, (int64_t)window + ceil_div(tile::kBlockRows, G) + sinks + 2 * tile::kTile);
+    const int64_t steps = ceil_div(len, tile::kTile);
+    const int64_t wgs = (b->n_tokens * G / tile::kBlockRows + 1) * pool->n_kv_heads;
+    p.n_splits = (int)std::max<int64_t>(1, std::min(512 / wgs, steps / 16));
+    p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
+  } else {
+    p.row_blocks = (int)std::min<int64_t>(65535, std::max<int64_t>(1, ceil_div(most * G, kRows)));
+    if (window > 0) len = std::min<int64_t>(len, (int64_t)window + most + sinks + 2 * kTile);
+    const int64_t steps = ceil_div(len, kTile);
+    const int64_t wgs = (int64_t)b->n_seqs * pool->n_kv_heads * p.row_blocks;
+    p.n_splits = (int)std::max<int64_t>(1, std::min(4096 / std::max<int64_t>(wgs, 1), steps / 16));
+    p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
+  }
   const size_t rows = (size_t)b->n_tokens * Hq;
   if (rows >= (size_t)kMaxGrid) p.n_splits = 1;  // (the join has a workgroup per row)
   if (p.n_splits > 1) {
@@ -549,12 +917,21 @@ ckv_status check_attn(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq
 }
 
 template <int D, int T>
-ckv_status launch_page_attn(const PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) {
-  const int64_t wgs = (int64_t)align_up((size_t)a.s.n_seqs * a.n_splits, 8) * a.Hkv;
-  if (wgs >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
-  const auto kernel = a.c == 8 ? page_rows_kernel<D, T, true> : page_rows_kernel<D, T, false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)p.row_blocks),
-                     dim3(64 * kWaves), 0, st, a);
+ckv_status launch_page_attn(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) {
+  if (p.wide) {
+    if constexpr (T != CKV_DTYPE_F32) {
+      const int64_t streams = (int64_t)a.Hkv * a.n_splits;
+      const int64_t grid = 8 % streams == 0 ? 8 * ceil_div(p.blocks, 8 / streams) : 8 * ceil_div(streams, 8) * p.blocks;
+      if (grid >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
+      a.n_blocks = (uint32_t)p.blocks;
+      hipLaunchKernelGGL((page_tile_kernel<D, T>), dim3((unsigned)grid), dim3(256), 0, st, a);
+    }
+  } else {
+    const int64_t wgs = (int64_t)align_up((size_t)a.s.n_seqs * a.n_splits, 8) * a.Hkv;
+    if (wgs >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
+    const auto kernel = a.c == 8 ? page_rows_kernel<D, T, true> : page_rows_kernel<D, T, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)p.row_blocks), dim3(64 * kWaves), 0, st, a);
+  }
   CKV_HIP(hipGetLastError());
   if (a.n_splits > 1) {
     const int64_t blocks = a.s.n_tokens * a.Hq;

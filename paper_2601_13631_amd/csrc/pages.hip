@@ -128,41 +128,20 @@ __device__ __forceinline__ uint32_t codes2(float x, float y) {
 // scale, rounds the page's older rows again if that rose, and writes the new rows.
 // Lanes hold 8 elements each, D / 8 lanes per row.
 //
-// The pages of the batch are numbered sequence by sequence, page slots in order, and
-// a wave finds its own by a running sum over the sequences, 64 at a time.
+// The pages of the batch are numbered sequence by sequence, page slots in order.
 template <int D>
 __global__ __launch_bounds__(64) void append_e4m3_kernel(AppendArgs a) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes;
   const int lane = threadIdx.x, g = blockIdx.y;
   int64_t want = blockIdx.x;
-  int b = -1;
   SeqSpan sp{};
-  for (int b0 = 0; b0 < a.s.n_seqs; b0 += 64) {
-    SeqSpan mine{0, 0, 0};
-    int pages = 0;
-    if (b0 + lane < a.s.n_seqs) {
-      mine = seq_span(a.s, b0 + lane);
-      const int64_t start = max<int64_t>((int64_t)mine.len - mine.count, 0), end = mine.len;
-      if (mine.count > 0 && end > start) pages = (int)((end - 1) / a.c - start / a.c) + 1;
-    }
-    int sum = pages;  // inclusive over the lanes
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const int y = __shfl_up(sum, x);
-      if (lane >= x) sum += y;
-    }
-    const uint64_t past = __ballot((int64_t)sum > want);
-    if (past) {
-      const int at = __builtin_ctzll(past);
-      want -= __shfl(sum - pages, at);
-      sp.first = __shfl(mine.first, at);
-      sp.count = __shfl(mine.count, at);
-      sp.len = __shfl(mine.len, at);
-      b = b0 + at;
-      break;
-    }
-    want -= __shfl(sum, 63);
-  }
+  const int b = find_part(
+      a.s,
+      [&](const SeqSpan& q) {  // pages that its tokens lie in
+        const int64_t start = max<int64_t>((int64_t)q.len - q.count, 0), end = q.len;
+        return end > start ? (int)((end - 1) / a.c - start / a.c) + 1 : 0;
+      },
+      want, sp);
   if (b < 0) return;  // more waves than pages
   const int64_t start = (int64_t)sp.len - sp.count;  // position of the call's first token
   const int64_t slot = max<int64_t>(start, 0) / a.c + want;

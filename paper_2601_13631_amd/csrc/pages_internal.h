@@ -49,6 +49,40 @@ __device__ __forceinline__ SeqSpan seq_span(const PageSeqs& s, int b) {
   return SeqSpan{lo, (int32_t)max<int64_t>(hi - lo, 0), s.lens[b]};
 }
 
+// Work that the sequences have in parts, parts(span) of them each, numbered sequence by
+// sequence: the sequence b of part `want`, its span, and the part's number inside it (in
+// want).  b = -1 past the last part.  A whole wave calls it: 64 sequences at a time, by a
+// running sum over the lanes.
+template <class F>
+__device__ __forceinline__ int find_part(const PageSeqs& s, F&& parts, int64_t& want, SeqSpan& span) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < s.n_seqs; b0 += 64) {
+    SeqSpan mine{0, 0, 0};
+    int n = 0;
+    if (b0 + lane < s.n_seqs) {
+      mine = seq_span(s, b0 + lane);
+      if (mine.count > 0) n = parts(mine);
+    }
+    int sum = n;  // up to this lane
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const int y = __shfl_up(sum, x);
+      if (lane >= x) sum += y;
+    }
+    const uint64_t past = __ballot((int64_t)sum > want);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      want -= __builtin_amdgcn_readlane(sum - n, at);
+      span.first = (int64_t)__builtin_amdgcn_readlane((int)mine.first, at);  // (below 2^31)
+      span.count = __builtin_amdgcn_readlane(mine.count, at);
+      span.len = __builtin_amdgcn_readlane(mine.len, at);
+      return b0 + at;
+    }
+    want -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  return -1;
+}
+
 // The scale of an E4M3 page from its byte: 2^(e - 127), finite whatever the byte (a page
 // that no query sees may hold any; its cleared rows then stay 0).
 __device__ __forceinline__ float scale_of(uint32_t byte) {
