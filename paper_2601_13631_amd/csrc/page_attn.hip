@@ -797,30 +797,36 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   }
 }
 
-// Joins a row's splits, a workgroup per row: 256 / (D / 4) groups of threads take the
-// splits in turn, 4 elements a thread, and meet in LDS (in a fixed order).
-template <int D, class QT>
+// Joins the splits of a row: kGroups groups of D / 4 threads take them in turn, 4 elements
+// a thread, and meet in LDS, all in a fixed order.  One group (and several rows per
+// workgroup) up to kJoinBatch splits, whose loads are all in flight together; else the
+// whole workgroup.
+constexpr int kJoinBatch = 8;
+template <int D, class QT, int kGroups>
 __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
-  constexpr int kCols = D / 4, kGroups = 256 / kCols, kBatch = 8;
-  const int64_t row = blockIdx.x, n_rows = a.s.n_tokens * a.Hq, tok = row / a.Hq;
-  if (tok < a.s.tok_off[0] || tok >= a.s.tok_off[a.s.n_seqs]) return;  // of no sequence
+  constexpr int kCols = D / 4, kRowsPer = 256 / kCols / kGroups;
+  const int64_t n_rows = a.s.n_tokens * a.Hq;
+  const int64_t row = (int64_t)blockIdx.x * kRowsPer + threadIdx.x / (kCols * kGroups);
+  const int64_t tok = row / a.Hq;
+  // (with several groups, a workgroup has one row: it leaves as a whole)
+  if (row >= n_rows || tok < a.s.tok_off[0] || tok >= a.s.tok_off[a.s.n_seqs]) return;  // of no sequence
   const int n_parts = min(a.n_parts[tok], a.n_splits);
   if (n_parts <= 1) return;  // written already
-  const int col = threadIdx.x % kCols * 4, grp = threadIdx.x / kCols;
+  const int col = threadIdx.x % kCols * 4, grp = threadIdx.x / kCols % kGroups;
   float M = kNone, L = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = grp; s0 < n_parts; s0 += kGroups * kBatch) {
-    float2 ml[kBatch];
-    f32x4 x[kBatch];
+  for (int s0 = grp; s0 < n_parts; s0 += kGroups * kJoinBatch) {
+    float2 ml[kJoinBatch];
+    f32x4 x[kJoinBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {  // all in flight together
+    for (int k = 0; k < kJoinBatch; ++k) {
       const int64_t at = (int64_t)min(s0 + k * kGroups, n_parts - 1) * n_rows + row;
       ml[k] = a.ml_part[at];
       x[k] = *reinterpret_cast<const f32x4*>(a.o_part + at * D + col);
     }
     float to = M;
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
+    for (int k = 0; k < kJoinBatch; ++k) {
       if (s0 + k * kGroups >= n_parts) ml[k] = make_float2(kNone, 0.f);
       to = fmaxf(to, ml[k].x);
     }
@@ -829,27 +835,29 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
     L *= f;
     acc *= f;
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
+    for (int k = 0; k < kJoinBatch; ++k) {
       const float w = __builtin_amdgcn_exp2f(ml[k].x - to);
       L += ml[k].y * w;
       acc += x[k] * w;  // (a split that saw no key wrote zeros)
     }
   }
-  __shared__ f32x4 part[kGroups][kCols];
-  __shared__ float2 part_ml[kGroups];
-  part[grp][threadIdx.x % kCols] = acc;
-  if (col == 0) part_ml[grp] = make_float2(M, L);
-  __syncthreads();
-  if (grp > 0) return;
+  if constexpr (kGroups > 1) {
+    __shared__ f32x4 part[kGroups][kCols];
+    __shared__ float2 part_ml[kGroups];
+    part[grp][threadIdx.x % kCols] = acc;
+    if (col == 0) part_ml[grp] = make_float2(M, L);
+    __syncthreads();
+    if (grp > 0) return;
 #pragma unroll
-  for (int k = 1; k < kGroups; ++k) M = fmaxf(M, part_ml[k].x);
-  L = 0.f;
-  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 1; k < kGroups; ++k) M = fmaxf(M, part_ml[k].x);
+    L = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int k = 0; k < kGroups; ++k) {
-    const float w = __builtin_amdgcn_exp2f(part_ml[k].x - M);
-    L += part_ml[k].y * w;
-    acc += part[k][threadIdx.x] * w;
+    for (int k = 0; k < kGroups; ++k) {
+      const float w = __builtin_amdgcn_exp2f(part_ml[k].x - M);
+      L += part_ml[k].y * w;
+      acc += part[k][threadIdx.x] * w;
+    }
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
   QT y[4];
@@ -934,9 +942,13 @@ ckv_status launch_page_attn(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t 
   }
   CKV_HIP(hipGetLastError());
   if (a.n_splits > 1) {
-    const int64_t blocks = a.s.n_tokens * a.Hq;
-    hipLaunchKernelGGL((page_combine_kernel<D, typename Elem<T>::Q>), dim3((unsigned)blocks), dim3(256),
-                       0, st, a);
+    using QT = typename Elem<T>::Q;
+    constexpr int kUnits = 256 / (D / 4);
+    const int64_t rows = a.s.n_tokens * a.Hq;
+    if (a.n_splits <= kJoinBatch)
+      hipLaunchKernelGGL((page_combine_kernel<D, QT, 1>), dim3((unsigned)ceil_div(rows, kUnits)), dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((page_combine_kernel<D, QT, kUnits>), dim3((unsigned)rows), dim3(256), 0, st, a);
     CKV_HIP(hipGetLastError());
   }
   return CKV_OK;
