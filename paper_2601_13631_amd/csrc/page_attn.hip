@@ -451,9 +451,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
 //   O^T += V^T P^T  V^T by transposing LDS reads, P^T from the softmax registers
 // bf16 rows go from memory straight to LDS, a page per load (8 keys of a stage lie in
 // one page).  8-bit rows come through registers, a stage further ahead, and are written
-// as bf16.  A row's reference is the ceiling of its maximum so far, followed once a half's
-// logits pass it by kSlack: rescalings are rare, and powers of two, so that numerators
-// already rounded lose nothing.
+// as bf16.  A row's reference is the ceiling of its maximum at some time before: where it is
+// followed the scaling is a power of two, so that numerators already rounded lose nothing.
 template <int D, int T>
 __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   using namespace tile;
@@ -530,6 +529,12 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < St::kPer; ++i) {
       const int key = i * St::kKeyStep + wave * St::kRowsPerLoad;
+      if (a.c % kKeys == 0) {  // the stage lies in one page
+        const int64_t off = (int64_t)__builtin_amdgcn_readfirstlane(ent) * a.page_stride + (int64_t)in_page(pos0) * row_bytes;
+        buffer_to_lds(raw_rsrc(a.k + off, 0xffffffffu), kcol, (uint32_t)(key * row_bytes), dk + key * D);
+        buffer_to_lds(raw_rsrc(a.v + off, 0xffffffffu), vcol, (uint32_t)(key * row_bytes), dv + key * D);
+        continue;
+      }
       const int64_t off = (int64_t)__builtin_amdgcn_readlane(ent, key >> 3) * a.page_stride +
                           (int64_t)in_page(pos0 + key) * row_bytes;
       buffer_to_lds(raw_rsrc(a.k + off, 0xffffffffu), kcol, 0, dk + key * D);
@@ -542,6 +547,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
     u32x4 k[kLoads], v[kLoads];
     uint32_t ks, vs;  // scale bytes of the stage, as its entries
   };
+  const uint32_t ecol = (uint32_t)((lane / kELanes & 7) * row_bytes + g * D + lane % kELanes * 16);
   auto load_codes = [&](int st, int ent, Codes& x) __attribute__((always_inline)) {
     const int pos0 = steps.tile(min(st, end - 1)) * kKeys;
     ent = names_page(a, ent) ? ent : 0;
@@ -550,45 +556,34 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int key = (4 * i + wave) * kERows;
-      // (at D = 64 a load has rows of two groups of 8 keys)
-      int page, r;
+      const auto at = [&](int k) {  // where the 8 keys from k on begin
+        return (int64_t)__builtin_amdgcn_readlane(ent, k >> 3) * a.page_stride + (int64_t)in_page(pos0 + k) * row_bytes;
+      };
       if constexpr (kERows == 8) {
-        page = __builtin_amdgcn_readlane(ent, key >> 3);
-        r = in_page(pos0 + key) + lane / kELanes;
-      } else {
-        const int up = lane >> 5;
-        const int e0 = __builtin_amdgcn_readlane(ent, key >> 3), e1 = __builtin_amdgcn_readlane(ent, (key >> 3) + 1);
-        const int r0 = in_page(pos0 + key), r1 = in_page(pos0 + key + 8);
-        page = up ? e1 : e0;
-        r = (up ? r1 : r0) + (lane / kELanes & 7);
+        const int64_t off = at(key);
+        x.k[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(raw_rsrc(a.k + off, 0xffffffffu), ecol, 0, 0));
+        x.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(raw_rsrc(a.v + off, 0xffffffffu), ecol, 0, 0));
+      } else {  // (at D = 64 a load has rows of two groups of 8 keys)
+        const int64_t lo = at(key), hi = at(key + 8), off = (lane >> 5 ? hi : lo) + ecol;
+        x.k[i] = *reinterpret_cast<const u32x4*>(a.k + off);
+        x.v[i] = *reinterpret_cast<const u32x4*>(a.v + off);
       }
-      const int64_t off = (int64_t)page * a.page_stride + (int64_t)r * row_bytes + g * D + lane % kELanes * 16;
-      x.k[i] = *reinterpret_cast<const u32x4*>(a.k + off);
-      x.v[i] = *reinterpret_cast<const u32x4*>(a.v + off);
     }
   };
-  auto write_codes = [&](const Codes& x, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int first = (4 * i + wave) * kERows, key = first + lane / kELanes, seg = 2 * (lane % kELanes);
-      float ks, vs;
-      if constexpr (kERows == 8) {
-        ks = scale_of(__builtin_amdgcn_readlane(x.ks, first >> 3));
-        vs = scale_of(__builtin_amdgcn_readlane(x.vs, first >> 3));
-      } else {
-        const int a0 = __builtin_amdgcn_readlane(x.ks, first >> 3), a1 = __builtin_amdgcn_readlane(x.ks, (first >> 3) + 1);
-        const int b0 = __builtin_amdgcn_readlane(x.vs, first >> 3), b1 = __builtin_amdgcn_readlane(x.vs, (first >> 3) + 1);
-        ks = scale_of(lane >> 5 ? a1 : a0);
-        vs = scale_of(lane >> 5 ? b1 : b0);
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        *reinterpret_cast<bf16x8*>(dk + key * D + (((seg + h) ^ k_swz<D>(key)) << 3)) =
-            bf16_of_codes(x.k[i][2 * h], x.k[i][2 * h + 1], ks);
-        *reinterpret_cast<bf16x8*>(dv + key * D + (((seg + h) ^ v_swz<D>(key)) << 3)) =
-            bf16_of_codes(x.v[i][2 * h], x.v[i][2 * h + 1], vs);
-      }
+  // Piece n < 4 kLoads of a stage's codes as bf16 in LDS: half n % 2 of load n / 4, K then V.
+  auto write_codes = [&](auto n, const Codes& x, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
+    constexpr int i = n / 4, kv = n / 2 % 2, h = n % 2;
+    const int first = (4 * i + wave) * kERows, key = first + lane / kELanes;
+    const uint32_t bytes = kv ? x.vs : x.ks;
+    uint32_t byte = (uint32_t)__builtin_amdgcn_readlane(bytes, first >> 3);
+    if constexpr (kERows == 16) {
+      const uint32_t up = (uint32_t)__builtin_amdgcn_readlane(bytes, (first >> 3) + 1);
+      byte = lane >> 5 ? up : byte;
     }
+    const int seg = (2 * (lane % kELanes) + h) ^ (kv ? v_swz<D>(key) : k_swz<D>(key));
+    const u32x4& w = kv ? x.v[i] : x.k[i];
+    *reinterpret_cast<bf16x8*>((kv ? dv : dk) + key * D + (seg << 3)) =
+        bf16_of_codes(w[2 * h], w[2 * h + 1], scale_of(byte));
   };
 
   // byte offsets of the operand reads (the same for every stage)
@@ -599,12 +594,9 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
 
   constexpr int kG = D / 16;  // MFMAs of one 32-key product, and of one O update
   constexpr int kE = 256 / D; // logits per numerator step: kG + 2 steps per half
+  static_assert(!kE4 || 4 * kLoads == kG);
   f32x16 o[D / 32];
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
-  float l[2] = {0.f, 0.f}, ref = kNone;
+  float l[2], ref;
 
   // -inf where this lane's row must not see a key of half `sub`; `there`: bit i, the page
   // of the stage's keys 8 i .. + 7.
@@ -623,146 +615,173 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
       }
     }
   };
-  // The reference follows the logits of a half; pb: numerators rounded against the old one.
-  auto follow = [&](const f32x16& s, u32x4* pb) __attribute__((always_inline)) {
+  // The reference follows the logits of a half.  `before`: the half whose numerators are
+  // under way, pb where they go; of its groups of kE the last has only its exponents, the
+  // one before it is not yet added or packed.
+  auto follow = [&](const f32x16& s, f32x16* before, u32x4* pb) __attribute__((always_inline)) {
     float mx = max16(s) * a.c1;
-    if (__any(mx > ref + kSlack)) {
-      mx = fmaxf(mx, partner_f(mx));
-      const float to = fmaxf(ceilf(mx), ref), f = __builtin_amdgcn_exp2f(ref - to);
-      ref = to;
-      l[0] *= f;
-      l[1] *= f;
+    if (!__any(mx > ref + kSlack)) return;
+    mx = fmaxf(mx, partner_f(mx));
+    const float to = fmaxf(ceilf(mx), ref), by = ref - to, f = __builtin_amdgcn_exp2f(by);
+    ref = to;
+    l[0] *= f;
+    l[1] *= f;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
+    for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[db][v] *= f;
-      if (pb) {
+      for (int v = 0; v < 16; ++v) o[db][v] *= f;
+    if (!before) return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t w = pb[i >> 2][i & 3];
-          const uint32_t lo = __float_as_uint(__uint_as_float(w << 16) * f);
-          const uint32_t hi = __float_as_uint(__uint_as_float(w & 0xffff0000u) * f);
-          pb[i >> 2][i & 3] = (hi & 0xffff0000u) | lo >> 16;
-        }
-      }
+    for (int e = 0; e < kE; ++e) {
+      (*before)[kE * (kG - 1) + e] += by;
+      (*before)[kE * (kG - 2) + e] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w = pb[i >> 2][i & 3];
+      const uint32_t lo = __float_as_uint(__uint_as_float(w << 16) * f);
+      const uint32_t hi = __float_as_uint(__uint_as_float(w & 0xffff0000u) * f);
+      pb[i >> 2][i & 3] = (hi & 0xffff0000u) | lo >> 16;
     }
   };
 
-  if (begin < end) {
-    // entries of the current stage and of the ones after it
-    int ent = entries(begin), ent1 = entries(begin + 1), ent2 = 0;
-    Codes codes;
-    if constexpr (kE4) {
-      ent2 = entries(begin + 2);
-      load_codes(begin, ent, codes);
-      write_codes(codes, k0, v0);
-      load_codes(begin + 1, ent1, codes);
-    } else {
-      load_direct(begin, ent, k0, v0);
-    }
-    stage_barrier();
-    bf16x8 ka[kG];  // K fragments of the current stage's first 32 keys
+  // The reference is looked at in the first stage and in those where some row sees only a
+  // part: the first keys that a row sees are in one of them.  In the others it is left: only
+  // a logit 120 log2 units above all earlier ones does harm, which the sums then show, and
+  // the split is done again with every stage looked at.
+  for (bool look = false;; look = true) {
 #pragma unroll
-    for (int i = 0; i < kG; ++i) ka[i] = read_k<D>(k0, kfo, 0, i);
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
+    l[0] = l[1] = 0.f;
+    ref = kNone;
+    if (begin < end) {
+      // entries of the current stage and of the ones after it
+      int ent = entries(begin), ent1 = entries(begin + 1), ent2 = 0;
+      Codes codes;
+      if constexpr (kE4) {
+        ent2 = entries(begin + 2);
+        load_codes(begin, ent, codes);
+        static_for<4 * kLoads>([&](auto n) { write_codes(n, codes, k0, v0); });
+        load_codes(begin + 1, ent1, codes);
+      } else {
+        load_direct(begin, ent, k0, v0);
+      }
+      stage_barrier();
+      bf16x8 ka[kG];  // K fragments of the current stage's first 32 keys
+#pragma unroll
+      for (int i = 0; i < kG; ++i) ka[i] = read_k<D>(k0, kfo, 0, i);
 
-    auto stage = [&](int st, uint16_t* lk, uint16_t* lv, uint16_t* nk, uint16_t* nv)
-        __attribute__((always_inline)) {
-      uint32_t ko = kfo, vo = voff;
-      asm volatile("" : "+v"(ko), "+v"(vo));
-      const int pos0 = steps.tile(st) * kKeys, last = pos0 + kKeys;
-      // what some row of the block must not see, and which pages are there
-      const uint32_t there = (uint32_t)__ballot(names_page(a, ent)) & 0xffu;
-      const bool edge = there != 0xffu || last > min(p0 + 1, kv_end) ||
-                        (a.window > 0 && pos0 <= p1 - a.window && last > a.sinks);
-      int after;
-      if constexpr (kE4) {
-        if (st + 1 < end) write_codes(codes, nk, nv);
-        after = entries(st + 3);
-        if (st + 2 < end) load_codes(st + 2, ent2, codes);
-      } else {
-        after = entries(st + 2);
-        if (st + 1 < end) load_direct(st + 1, ent1, nk, nv);
-      }
-      if (edge) {
-        // a weight of 0 does not undo a NaN: V rows that no query of the block sees are cleared
-        for (int i = threadIdx.x; i < kKeys * (D / 8); i += 256) {
-          const int key = i / (D / 8), pos = pos0 + key;
-          if (!((there >> (key >> 3) & 1) && pos < kv_end && pos <= p1 &&
-                (a.window <= 0 || pos > p0 - a.window || pos < a.sinks)))
-            *reinterpret_cast<u32x4*>(lv + i * 8) = u32x4{0u, 0u, 0u, 0u};
+      auto stage = [&](int st, uint16_t* lk, uint16_t* lv, uint16_t* nk, uint16_t* nv)
+          __attribute__((always_inline)) {
+        uint32_t ko = kfo, vo = voff;
+        asm volatile("" : "+v"(ko), "+v"(vo));
+        const int pos0 = steps.tile(st) * kKeys, last = pos0 + kKeys;
+        // what some row of the block must not see, and which pages are there
+        const uint32_t there = (uint32_t)__ballot(names_page(a, ent)) & 0xffu;
+        const bool edge = there != 0xffu || last > min(p0 + 1, kv_end) ||
+                          (a.window > 0 && pos0 <= p1 - a.window && last > a.sinks);
+        const bool check = edge || st == begin || look;
+        const int after = entries(st + (kE4 ? 3 : 2));
+        if constexpr (!kE4)
+          if (st + 1 < end) load_direct(st + 1, ent1, nk, nv);
+        if (edge) {
+          // a weight of 0 does not undo a NaN: V rows that no query of the block sees are cleared
+          for (int i = threadIdx.x; i < kKeys * (D / 8); i += 256) {
+            const int key = i / (D / 8), pos = pos0 + key;
+            if (!((there >> (key >> 3) & 1) && pos < kv_end && pos <= p1 &&
+                  (a.window <= 0 || pos > p0 - a.window || pos < a.sinks)))
+              *reinterpret_cast<u32x4*>(lv + i * 8) = u32x4{0u, 0u, 0u, 0u};
+          }
+          __syncthreads();
         }
-        __syncthreads();
-      }
-      bf16x8 kb[kG], va[2][D / 32], vb[2][D / 32];
-      f32x16 s0, s1;
-      u32x4 p0b[2], p1b[2];
+        bf16x8 kb[kG], va[2][D / 32], vb[2][D / 32];
+        f32x16 s0, s1;
+        u32x4 p0b[2], p1b[2];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
-      __builtin_amdgcn_sched_barrier(0);
-      static_for<kG>([&](auto i) __attribute__((always_inline)) {
-        kb[i] = read_k<D>(lk, ko, 1, i);
-        s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[i], qf[i], s0, 0, 0, 0);
+        for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
         __builtin_amdgcn_sched_barrier(0);
-      });
-      if (edge) mask(pos0, 0, there, s0);
-      follow(s0, nullptr);
-      __builtin_amdgcn_sched_barrier(0);
-      static_for<kG>([&](auto i) __attribute__((always_inline)) {
-        constexpr int kk = i / (D / 32), db = i % (D / 32);
-        va[kk][db] = read_v<D>(lv, vo, 0, kk, db);
-        s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[i], qf[i], s1, 0, 0, 0);
-        numerator_step<kE, i>(s0, a.c1, ref, l, p0b);
+        static_for<kG>([&](auto i) __attribute__((always_inline)) {
+          kb[i] = read_k<D>(lk, ko, 1, i);
+          s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[i], qf[i], s0, 0, 0, 0);
+          // (kG pieces: the stage after the last one is written as well, and not used)
+          if constexpr (kE4) write_codes(i, codes, nk, nv);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (kE4) load_codes(st + 2, ent2, codes);
+        if (edge) mask(pos0, 0, there, s0);
+        if (check) follow(s0, nullptr, nullptr);
         __builtin_amdgcn_sched_barrier(0);
-      });
-      numerator_step<kE, kG>(s0, a.c1, ref, l, p0b);
-      numerator_step<kE, kG + 1>(s0, a.c1, ref, l, p0b);
-      if (edge) mask(pos0, 1, there, s1);
-      follow(s1, p0b);
-      __builtin_amdgcn_sched_barrier(0);
-      static_for<kG>([&](auto i) __attribute__((always_inline)) {
-        constexpr int kk = i / (D / 32), db = i % (D / 32);
-        vb[kk][db] = read_v<D>(lv, vo, 1, kk, db);
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[kk][db], __builtin_bit_cast(bf16x8, p0b[kk]),
-                                                        o[db], 0, 0, 0);
-        numerator_step<kE, i>(s1, a.c1, ref, l, p1b);
+        static_for<kG>([&](auto i) __attribute__((always_inline)) {
+          constexpr int kk = i / (D / 32), db = i % (D / 32);
+          va[kk][db] = read_v<D>(lv, vo, 0, kk, db);
+          s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[i], qf[i], s1, 0, 0, 0);
+          numerator_step<kE, i>(s0, a.c1, ref, l, p0b);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if (edge) mask(pos0, 1, there, s1);
+        if (check) follow(s1, &s0, p0b);
         __builtin_amdgcn_sched_barrier(0);
-      });
-      if constexpr (kE4) {  // the next stage's rows are written; loads stay in flight
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-      } else {
-        stage_barrier();  // the next stage has landed; this one's buffers are read
+        static_for<kG>([&](auto i) __attribute__((always_inline)) {
+          constexpr int kk = i / (D / 32), db = i % (D / 32);
+          vb[kk][db] = read_v<D>(lv, vo, 1, kk, db);
+          if constexpr (i < 2) numerator_step<kE, kG + i>(s0, a.c1, ref, l, p0b);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[kk][db], __builtin_bit_cast(bf16x8, p0b[kk]),
+                                                          o[db], 0, 0, 0);
+          numerator_step<kE, i>(s1, a.c1, ref, l, p1b);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (kE4) {  // the next stage's rows are written; loads stay in flight
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+          __builtin_amdgcn_s_barrier();
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        } else {
+          stage_barrier();  // the next stage has landed; this one's buffers are read
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<kG>([&](auto i) __attribute__((always_inline)) {
+          constexpr int kk = i / (D / 32), db = i % (D / 32);
+          ka[i] = read_k<D>(nk, ko, 0, i);  // (after the last stage: read and not used)
+          if constexpr (i < 2) numerator_step<kE, kG + i>(s1, a.c1, ref, l, p1b);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[kk][db], __builtin_bit_cast(bf16x8, p1b[kk]),
+                                                          o[db], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        ent = ent1;
+        if constexpr (kE4) {
+          ent1 = ent2;
+          ent2 = after;
+        } else {
+          ent1 = after;
+        }
+      };
+      for (int st = begin; st < end; st += 2) {
+        stage(st, k0, v0, k1, v1);
+        if (st + 1 >= end) break;
+        stage(st + 1, k1, v1, k0, v0);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      static_for<kG>([&](auto i) __attribute__((always_inline)) {
-        constexpr int kk = i / (D / 32), db = i % (D / 32);
-        ka[i] = read_k<D>(nk, ko, 0, i);  // (after the last stage: read and not used)
-        if constexpr (i < 2) numerator_step<kE, kG + i>(s1, a.c1, ref, l, p1b);
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[kk][db], __builtin_bit_cast(bf16x8, p1b[kk]),
-                                                        o[db], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      ent = ent1;
-      if constexpr (kE4) {
-        ent1 = ent2;
-        ent2 = after;
-      } else {
-        ent1 = after;
-      }
-    };
-    for (int st = begin; st < end; st += 2) {
-      stage(st, k0, v0, k1, v1);
-      if (st + 1 >= end) break;
-      stage(st + 1, k1, v1, k0, v0);
     }
+    l[0] += l[1];
+    l[0] += partner_f(l[0]);
+    if (look) break;
+    float any[4] = {0.f, 0.f, 0.f, 0.f};  // (a sum over the outputs is inf or NaN if one of them is)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) any[v & 3] += o[db][v];
+    const uint32_t total = __float_as_uint((any[0] + any[1]) + (any[2] + any[3]));
+    const bool bad = (total & 0x7f800000u) == 0x7f800000u ||
+                     (__float_as_uint(l[0]) & 0x7fffffffu) > __float_as_uint(0x1p120f);
+    if (!__syncthreads_or(bad)) break;
   }
-  l[0] += l[1];
-  l[0] += partner_f(l[0]);
 
   // o[db][v] holds d = 32*db + 8*(v/4) + 4*half + v%4 of this lane's row
   if (n_parts > 1) {
     if (!row_ok) return;
+    // The sum in [1, 2), so that outputs are of V's size whatever the reference was.
+    const int e = l[0] > 0.f ? (int)(__float_as_uint(l[0]) >> 23) - 127 : 0;
+    const float f = __uint_as_float((uint32_t)(127 - e) << 23);
     const int64_t prow = (int64_t)split * a.s.n_tokens * a.Hq + out_row;
     float* dst = a.o_part + prow * D + 4 * half;
 #pragma unroll
@@ -770,8 +789,8 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<f32x4*>(dst + 32 * db + 8 * q) =
-            f32x4{o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
-    if (half == 0) a.ml_part[prow] = make_float2(ref, l[0]);
+            f32x4{o[db][4 * q] * f, o[db][4 * q + 1] * f, o[db][4 * q + 2] * f, o[db][4 * q + 3] * f};
+    if (half == 0) a.ml_part[prow] = make_float2(ref + (float)e, l[0] * f);
     return;
   }
   // Output rows through LDS, so that a store is a whole 16-byte piece of a row and 16 lanes
