@@ -463,16 +463,23 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t v0[kKeys * D], v1[kKeys * D];
 
   // Blocks of rows that read the same keys (of one head and split: a stream) share an
-  // XCD's L2.  Streams go to the XCDs in turn; where there are fewer of them (1, 2, 4),
-  // a stream's blocks go to its XCDs in turn.  The last rows see the most keys: first.
+  // XCD's L2: eight streams at a time, one per XCD.  Of the streams left over, 1, 2 or 4
+  // have 8, 4 or 2 XCDs each, their blocks in turn; 3, 5, 6 or 7 are cut into eight runs of
+  // blocks.  The last rows see the most keys: first.
   const uint32_t streams = a.Hkv * a.n_splits, xcd = blockIdx.x & 7, idx = blockIdx.x >> 3;
+  const uint32_t whole = streams / 8 * a.n_blocks, rest = streams % 8;
   uint32_t stream, blk;
-  if (8 % streams == 0) {
-    stream = xcd % streams;
-    blk = idx * (8 / streams) + xcd / streams;
-  } else {
+  if (idx < whole) {
     stream = idx / a.n_blocks * 8 + xcd;
     blk = idx % a.n_blocks;
+  } else if (8 % rest == 0) {
+    stream = streams - rest + xcd % rest;
+    blk = (idx - whole) * (8 / rest) + xcd / rest;
+  } else {
+    const uint32_t run = (rest * a.n_blocks + 7) / 8, j = xcd * run + (idx - whole);
+    stream = streams - rest + j / a.n_blocks;
+    blk = j % a.n_blocks;
+    if (idx - whole >= run) return;
   }
   if (stream >= streams || blk >= a.n_blocks) return;
   const int g = (int)(stream % a.Hkv), split = (int)(stream / a.Hkv);
@@ -598,21 +605,33 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   f32x16 o[D / 32];
   float l[2], ref;
 
-  // -inf where this lane's row must not see a key of half `sub`; `there`: bit i, the page
-  // of the stage's keys 8 i .. + 7.
-  auto mask = [&](int pos0, int sub, uint32_t there, f32x16& s) __attribute__((always_inline)) {
+  // -inf where this lane's row must not see a key of half `sub` of the stage at pos0: keys
+  // past its own position or the sequence's end, keys before its window, keys of a missing
+  // page (`there`: bit i, the page of the stage's keys 8 i .. + 7), as far as the stage has
+  // any.  Register v holds key 16 (v / 8) + v % 8 + 8 half of the half.
+  const int upper = min(p, kv_end - 1);
+  auto mask = [&](int pos0, int sub, uint32_t there, bool up, bool low, f32x16& s) __attribute__((always_inline)) {
+    const int base = pos0 + kSub * sub + 8 * half;
+    if (up) {
+      const int most = upper - base;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {  // 4 keys of one group of 8
-      int key = kSub * sub + 16 * (q >> 1) + 4 * (q & 1) + 8 * half;
-      asm volatile("" : "+v"(key));  // nothing of this (rare) path is kept across stages
-      const int pos = pos0 + key;
-      const bool page = there >> (key >> 3) & 1;
+      for (int v = 0; v < 16; ++v) s[v] = 16 * (v >> 3) + (v & 7) <= most ? s[v] : -INFINITY;
+    }
+    if (low) {
+      const int least = p - a.window - base, first = a.sinks - base;  // sees above, and below
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = pos + e;
-        const bool see = page && j <= p && j < kv_end && (a.window <= 0 || j > p - a.window || j < a.sinks);
-        s[4 * q + e] = see ? s[4 * q + e] : -INFINITY;
+      for (int v = 0; v < 16; ++v) {
+        const int key = 16 * (v >> 3) + (v & 7);
+        s[v] = key > least || key < first ? s[v] : -INFINITY;
       }
+    }
+    if (there != 0xffu) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (!(there >> (4 * sub + 2 * i + half) & 1)) {
+#pragma unroll
+          for (int v = 0; v < 8; ++v) s[8 * i + v] = -INFINITY;
+        }
     }
   };
   // The reference follows the logits of a half.  `before`: the half whose numerators are
@@ -680,20 +699,22 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
         const int pos0 = steps.tile(st) * kKeys, last = pos0 + kKeys;
         // what some row of the block must not see, and which pages are there
         const uint32_t there = (uint32_t)__ballot(names_page(a, ent)) & 0xffu;
-        const bool edge = there != 0xffu || last > min(p0 + 1, kv_end) ||
-                          (a.window > 0 && pos0 <= p1 - a.window && last > a.sinks);
+        const bool up = last > min(p0 + 1, kv_end);
+        const bool low = a.window > 0 && pos0 <= p1 - a.window && last > a.sinks;
+        const bool edge = up || low || there != 0xffu;
         const bool check = edge || st == begin || look;
         const int after = entries(st + (kE4 ? 3 : 2));
         if constexpr (!kE4)
           if (st + 1 < end) load_direct(st + 1, ent1, nk, nv);
-        if (edge) {
+        if (there != 0xffu || last > min(p1 + 1, kv_end) ||
+            (a.window > 0 && pos0 <= p0 - a.window && last > a.sinks)) {
           // a weight of 0 does not undo a NaN: V rows that no query of the block sees are cleared
-          for (int i = threadIdx.x; i < kKeys * (D / 8); i += 256) {
-            const int key = i / (D / 8), pos = pos0 + key;
-            if (!((there >> (key >> 3) & 1) && pos < kv_end && pos <= p1 &&
-                  (a.window <= 0 || pos > p0 - a.window || pos < a.sinks)))
-              *reinterpret_cast<u32x4*>(lv + i * 8) = u32x4{0u, 0u, 0u, 0u};
-          }
+          const int key = (int)threadIdx.x >> 2, pos = pos0 + key;  // four threads a row
+          if (!((there >> (key >> 3) & 1) && pos < kv_end && pos <= p1 &&
+                (a.window <= 0 || pos > p0 - a.window || pos < a.sinks)))
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+              *reinterpret_cast<u32x4*>(lv + key * D + ((int)(threadIdx.x & 3) * (D / 32) + i) * 8) = u32x4{0u, 0u, 0u, 0u};
           __syncthreads();
         }
         bf16x8 kb[kG], va[2][D / 32], vb[2][D / 32];
@@ -710,7 +731,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (kE4) load_codes(st + 2, ent2, codes);
-        if (edge) mask(pos0, 0, there, s0);
+        if (edge) mask(pos0, 0, there, up, low, s0);
         if (check) follow(s0, nullptr, nullptr);
         __builtin_amdgcn_sched_barrier(0);
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
@@ -720,7 +741,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           numerator_step<kE, i>(s0, a.c1, ref, l, p0b);
           __builtin_amdgcn_sched_barrier(0);
         });
-        if (edge) mask(pos0, 1, there, s1);
+        if (edge) mask(pos0, 1, there, up, low, s1);
         if (check) follow(s1, &s0, p0b);
         __builtin_amdgcn_sched_barrier(0);
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
@@ -908,9 +929,28 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
     p.blocks = b->n_tokens * G / tile::kBlockRows + b->n_seqs;
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + ceil_div(tile::kBlockRows, G) + sinks + 2 * tile::kTile);
     const int64_t steps = ceil_div(len, tile::kTile);
+    // The splits that cost least by a model of the launch, in cycles at 1.85 GHz: 512
+    // workgroups run at once, two per CU, each for its stages (3,440 cycles a stage for two,
+    // 2,100 for one alone on its CU) and a fixed part; a split's partials are written and
+    // read again.  (2,341 tokens x 28 heads, 516 blocks, after 30,427 others: 1,543 us in
+    // one split, 1,148 in 4, 1,125 in 6; after a window of 1,000: 67 us in one, 86 in 2.)
+    constexpr double kFixed = 15000, kStage = 3440, kFixedAlone = 12500, kStageAlone = 2100;
+    constexpr double kJoin = 5500, kJoinBytes = 2500;
     const int64_t wgs = (b->n_tokens * G / tile::kBlockRows + 1) * pool->n_kv_heads;
-    p.n_splits = (int)std::max<int64_t>(1, std::min(512 / wgs, steps / 16));
-    p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
+    const double join = (double)b->n_tokens * Hq * pool->head_dim * 2 * sizeof(float) / kJoinBytes;
+    double best = 0;
+    for (int64_t n0 = 1; n0 <= 64 && n0 * 4 <= std::max<int64_t>(steps, 4); ++n0) {
+      const int64_t per = ceil_div(steps, n0), n = ceil_div(steps, per), rem = wgs * n % 512;
+      double cost = (double)(wgs * n / 512) * (kFixed + kStage * (double)per);
+      if (rem > 0)
+        cost += rem <= 256 ? kFixedAlone + kStageAlone * (double)per : kFixed + kStage * (double)per;
+      if (n > 1) cost += kJoin + join * (double)n;
+      if (n0 == 1 || cost < best) {
+        best = cost;
+        p.n_splits = (int)n;
+        p.slice = (int)per;
+      }
+    }
   } else {
     p.row_blocks = (int)std::min<int64_t>(65535, std::max<int64_t>(1, ceil_div(most * G, kRows)));
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + most + sinks + 2 * kTile);
@@ -948,7 +988,8 @@ ckv_status launch_page_attn(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t 
   if (p.wide) {
     if constexpr (T != CKV_DTYPE_F32) {
       const int64_t streams = (int64_t)a.Hkv * a.n_splits;
-      const int64_t grid = 8 % streams == 0 ? 8 * ceil_div(p.blocks, 8 / streams) : 8 * ceil_div(streams, 8) * p.blocks;
+      const int64_t rest = streams % 8;
+      const int64_t grid = 8 * (streams / 8 * p.blocks + ceil_div(rest * p.blocks, 8));
       if (grid >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
       a.n_blocks = (uint32_t)p.blocks;
       hipLaunchKernelGGL((page_tile_kernel<D, T>), dim3((unsigned)grid), dim3(256), 0, st, a);

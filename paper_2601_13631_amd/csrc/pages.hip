@@ -160,15 +160,22 @@ __global__ __launch_bounds__(64) void append_e4m3_kernel(AppendArgs a) {
     return *reinterpret_cast<const bf16x8*>(src + ((t * a.Hkv + g) * D + col) * 2);
   };
 
+  // the first kBatch rows per lane stay in registers, all in flight together
+  constexpr int kBatch = 8;
+  bf16x8 x[kBatch];
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i) x[i] = new_row(min(r0 + sub + i * kRows, r1 - 1));
   float amax = 0.f;
-  for (int r = r0 + sub; r < r1; r += kRows) {
-    const bf16x8 x = new_row(r);
+  auto look = [&](const bf16x8& y) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float y = fabsf((float)x[e]);
-      if (y < INFINITY) amax = fmaxf(amax, y);
+      const float z = fabsf((float)y[e]);
+      if (z < INFINITY) amax = fmaxf(amax, z);
     }
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i) look(x[i]);  // (a row past the end is the last one again)
+  for (int r = r0 + sub + kBatch * kRows; r < r1; r += kRows) look(new_row(r));
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) amax = fmaxf(amax, __shfl_xor(amax, x));
   uint32_t to = scale_byte(amax);
@@ -194,15 +201,18 @@ __global__ __launch_bounds__(64) void append_e4m3_kernel(AppendArgs a) {
   }
   // 1 / scale is a power of two of its own (a byte of 10 to 247 gives 2^117 to 2^-120)
   const float inv = scale_of(254 - to);
-  for (int r = r0 + sub; r < r1; r += kRows) {
-    const bf16x8 x = new_row(r);
+  auto write = [&](int r, const bf16x8& y) {
     uint32_t z[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      z[i] = codes2((float)x[4 * i] * inv, (float)x[4 * i + 1] * inv) |
-             codes2((float)x[4 * i + 2] * inv, (float)x[4 * i + 3] * inv) << 16;
+      z[i] = codes2((float)y[4 * i] * inv, (float)y[4 * i + 1] * inv) |
+             codes2((float)y[4 * i + 2] * inv, (float)y[4 * i + 3] * inv) << 16;
     *reinterpret_cast<uint2*>(dst + (int64_t)r * a.row_bytes + col) = make_uint2(z[0], z[1]);
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i)
+    if (const int r = r0 + sub + i * kRows; r < r1) write(r, x[i]);
+  for (int r = r0 + sub + kBatch * kRows; r < r1; r += kRows) write(r, new_row(r));
   // every lane has read the old scale: the wave runs in step
   if (lane == 0) *scale = (uint8_t)to;
 }
@@ -306,13 +316,28 @@ __global__ __launch_bounds__(kPlanThreads) void compact_count_kernel(PlanArgs a)
   if (threadIdx.x == 0) a.counts[blockIdx.x] = n;
 }
 
+// kCount: no counts yet, every workgroup goes over all use counts itself.
+template <bool kCount>
 __global__ __launch_bounds__(kPlanThreads) void compact_rank_kernel(PlanArgs a) {
   __shared__ int waves[kPlanThreads / 64];
   int below = 0, all = 0;
-  for (int i = threadIdx.x; i < (int)gridDim.x; i += kPlanThreads) {
-    const int n = a.counts[i];
-    all += n;
-    if (i < (int)blockIdx.x) below += n;
+  if constexpr (kCount) {
+    for (int64_t p0 = threadIdx.x; p0 < a.n_pages; p0 += kPlan) {
+      int32_t refs[kPlanPer];
+#pragma unroll
+      for (int i = 0; i < kPlanPer; ++i) refs[i] = a.refs[min<int64_t>(p0 + i * kPlanThreads, a.n_pages - 1)];
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kPlanPer; ++i) n += p0 + i * kPlanThreads < a.n_pages && refs[i] > 0;
+      all += n;
+      if (p0 < (int64_t)blockIdx.x * kPlan) below += n;
+    }
+  } else {
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kPlanThreads) {
+      const int n = a.counts[i];
+      all += n;
+      if (i < (int)blockIdx.x) below += n;
+    }
   }
   below = block_sum(below);
   const int64_t L = block_sum(all);
@@ -545,9 +570,15 @@ ckv_status ckv_page_compact(const ckv_page_pool* pools, int32_t n_pools, const i
                     at(l.mover_refs), at(l.head), n_live};
   const hipStream_t st = (hipStream_t)stream;
   const unsigned blocks = (unsigned)ceil_div(n_pages, kPlan);
-  hipLaunchKernelGGL(compact_count_kernel, dim3(blocks), dim3(kPlanThreads), 0, st, pl);
-  CKV_HIP(hipGetLastError());
-  hipLaunchKernelGGL(compact_rank_kernel, dim3(blocks), dim3(kPlanThreads), 0, st, pl);
+  // Up to 4 workgroups each count all pages themselves: 4,000 pages in one launch of 6.2 us
+  // instead of two of 5.2 and 5.4; more of them go by the counts.
+  if (blocks <= 4) {
+    hipLaunchKernelGGL(compact_rank_kernel<true>, dim3(blocks), dim3(kPlanThreads), 0, st, pl);
+  } else {
+    hipLaunchKernelGGL(compact_count_kernel, dim3(blocks), dim3(kPlanThreads), 0, st, pl);
+    CKV_HIP(hipGetLastError());
+    hipLaunchKernelGGL(compact_rank_kernel<false>, dim3(blocks), dim3(kPlanThreads), 0, st, pl);
+  }
   CKV_HIP(hipGetLastError());
   for (int p0 = 0; p0 == 0 || p0 < n_pools; p0 += kMaxPools) {
     PoolTable t;

@@ -260,7 +260,7 @@ def host_compact(refs, table, n_pages):
 
 
 @pytest.mark.parametrize("cache,heads", [("bf16", HF), ("e4m3", H05)])
-@pytest.mark.parametrize("pages", [3, 64, 2047, 2048, 2049, 5000])
+@pytest.mark.parametrize("pages", [3, 64, 2047, 2048, 2049, 5000, 8192, 8193, 20000])
 @pytest.mark.parametrize("share", [0.0, 0.02, 0.5, 0.97, 1.0])
 def test_compact(cache, heads, pages, share):
     import paper_2601_13631_amd as ckv
