@@ -42,14 +42,13 @@ struct PageAttnArgs {
   float c1;
 };
 
-// The keys of a block of rows as steps of some tile of keys: those that hold the sinks,
-// then those from the window's begin on.
+// The keys of a block of rows as steps of kTile: those that hold the sinks, then those
+// from the window's begin on.
 struct Steps {
   int n_sink, first, n;  // step i: tile i < n_sink ? i : first + i - n_sink
   __device__ __forceinline__ int tile(int i) const { return i < n_sink ? i : first + (i - n_sink); }
 };
 // For queries at positions p0 .. p1 of a sequence with keys below kv_end.
-template <int kTile>
 __device__ __forceinline__ Steps steps_of(const PageAttnArgs& a, int p0, int p1, int kv_end) {
   Steps s{0, 0, 0};
   const int hi = min(p1 + 1, kv_end);
@@ -61,6 +60,25 @@ __device__ __forceinline__ Steps steps_of(const PageAttnArgs& a, int p0, int p1,
     s.first = max(lo / kTile, s.n_sink);
   }
   s.n = s.n_sink + max(tiles - s.first, 0);
+  return s;
+}
+
+// The same keys as groups of 8, which lie in one page each: those that hold the sinks, then
+// those from the window's begin on, without a gap between.
+struct Groups {
+  int n_sink, first, n;
+  __device__ __forceinline__ int pos(int i) const { return 8 * (i < n_sink ? i : first + (i - n_sink)); }
+};
+__device__ __forceinline__ Groups groups_of(const PageAttnArgs& a, int p0, int p1, int kv_end) {
+  Groups s{0, 0, 0};
+  const int hi = min(p1 + 1, kv_end);
+  if (hi <= 0) return s;
+  if (a.window > 0) {
+    const int lo = max(p0 - a.window + 1, 0);
+    s.n_sink = (min(min(a.sinks, lo), hi) + 7) / 8;
+    s.first = max(lo / 8, s.n_sink);
+  }
+  s.n = s.n_sink + max((hi + 7) / 8 - s.first, 0);
   return s;
 }
 
@@ -160,7 +178,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
   const int64_t rows = (int64_t)sp.count * a.G;
   const int p_base = sp.len - sp.count;
   // this sequence's own number of splits, by its length
-  const int all_steps = steps_of<kTile>(a, p_base, p_base + sp.count - 1, kv_end).n;
+  const int all_steps = steps_of(a, p_base, p_base + sp.count - 1, kv_end).n;
   const int n_parts = min(max((all_steps + a.slice - 1) / a.slice, 1), a.n_splits);
   if (split >= n_parts) return;
   if (a.n_splits > 1 && split == 0 && g == 0 && blockIdx.y == 0)
@@ -172,7 +190,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
   for (int64_t rb = blockIdx.y; rb * kRows < rows; rb += gridDim.y) {
     const int64_t r_first = rb * kRows, r_last = min<int64_t>(rows, r_first + kRows) - 1;
     const int p0 = p_base + (int)(r_first / a.G), p1 = p_base + (int)(r_last / a.G);
-    const Steps steps = steps_of<kTile>(a, p0, p1, kv_end);
+    const Steps steps = steps_of(a, p0, p1, kv_end);
     const int begin = (int)((int64_t)steps.n * split / n_parts);
     const int end = (int)((int64_t)steps.n * (split + 1) / n_parts);
 
@@ -495,14 +513,15 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   const int rows = sp.count * a.G, r_first = (int)rb * kBlockRows, r_last = min(rows, r_first + kBlockRows) - 1;
   const int p_base = sp.len - sp.count;
   const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
-  const int all_steps = steps_of<kKeys>(a, p_base, p_base + sp.count - 1, kv_end).n;
+  const int all_steps = (groups_of(a, p_base, p_base + sp.count - 1, kv_end).n + 7) / 8;
   const int n_parts = min(max((all_steps + a.slice - 1) / a.slice, 1), a.n_splits);
   if (split >= n_parts) return;
   if (a.n_splits > 1 && split == 0 && g == 0)
     for (int i = r_first / a.G + (int)threadIdx.x; i <= r_last / a.G; i += 256) a.n_parts[sp.first + i] = n_parts;
-  const Steps steps = steps_of<kKeys>(a, p0, p1, kv_end);
-  const int begin = (int)((int64_t)steps.n * split / n_parts);
-  const int end = (int)((int64_t)steps.n * (split + 1) / n_parts);
+  const Groups groups = groups_of(a, p0, p1, kv_end);  // a stage: 8 of them
+  const int stages = (groups.n + 7) / 8;
+  const int begin = (int)((int64_t)stages * split / n_parts);
+  const int end = (int)((int64_t)stages * (split + 1) / n_parts);
 
   // this lane's row
   const int row = r_first + wave * kWaveRows + (lane & 31);
@@ -519,31 +538,32 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
 
   // Table entries of a stage: lane l has that of keys 8 (l % 8) .. + 7.
   auto entries = [&](int st) __attribute__((always_inline)) {
-    const int pos = steps.tile(min(st, end - 1)) * kKeys + 8 * (lane & 7);
+    const int pos = groups.pos(8 * min(st, end - 1) + (lane & 7));
     return entry_of(a, tab, a.log2c >= 0 ? pos >> a.log2c : (int)((uint32_t)pos / (uint32_t)a.c));
   };
-  // Row of its page that the key at pos is.
-  auto in_page = [&](int pos) { return a.log2c >= 0 ? pos & (a.c - 1) : (int)((uint32_t)pos % (uint32_t)a.c); };
   const int row_bytes = a.Hkv * D * Elem<T>::kBytes;
+  // Where a stage's groups begin in the pool: lane l has group l % 8 (a missing page: page 0).
+  // Found by the lanes at once; a load takes its group's by readlane.
+  auto places = [&](int st, int ent) __attribute__((always_inline)) {
+    const int pos = groups.pos(8 * st + (lane & 7));
+    const int r = a.log2c >= 0 ? pos & (a.c - 1) : (int)((uint32_t)pos % (uint32_t)a.c);
+    return (int64_t)(names_page(a, ent) ? ent : 0) * a.page_stride + (int64_t)r * row_bytes;
+  };
+  auto place = [&](int64_t of, int group) __attribute__((always_inline)) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(of >> 32), group) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int)of, group));
+  };
 
   // bf16: this lane's byte of the rows that a load moves (the LDS permutation undone)
   const int key0 = wave * St::kRowsPerLoad + lane / St::kSegs;
-  const uint32_t kcol = (uint32_t)(lane / St::kSegs * row_bytes + 2 * (g * D + ((lane % St::kSegs ^ k_swz<D>(key0)) << 3)));
-  const uint32_t vcol = (uint32_t)(lane / St::kSegs * row_bytes + 2 * (g * D + ((lane % St::kSegs ^ v_swz<D>(key0)) << 3)));
-  auto load_direct = [&](int st, int ent, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
-    const int pos0 = steps.tile(st) * kKeys;
-    ent = names_page(a, ent) ? ent : 0;
+  const uint32_t rcol = (uint32_t)(((wave * St::kRowsPerLoad & 7) + lane / St::kSegs) * row_bytes);
+  const uint32_t kcol = rcol + (uint32_t)(2 * (g * D + ((lane % St::kSegs ^ k_swz<D>(key0)) << 3)));
+  const uint32_t vcol = rcol + (uint32_t)(2 * (g * D + ((lane % St::kSegs ^ v_swz<D>(key0)) << 3)));
+  auto load_direct = [&](int64_t of, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < St::kPer; ++i) {
       const int key = i * St::kKeyStep + wave * St::kRowsPerLoad;
-      if (a.c % kKeys == 0) {  // the stage lies in one page
-        const int64_t off = (int64_t)__builtin_amdgcn_readfirstlane(ent) * a.page_stride + (int64_t)in_page(pos0) * row_bytes;
-        buffer_to_lds(raw_rsrc(a.k + off, 0xffffffffu), kcol, (uint32_t)(key * row_bytes), dk + key * D);
-        buffer_to_lds(raw_rsrc(a.v + off, 0xffffffffu), vcol, (uint32_t)(key * row_bytes), dv + key * D);
-        continue;
-      }
-      const int64_t off = (int64_t)__builtin_amdgcn_readlane(ent, key >> 3) * a.page_stride +
-                          (int64_t)in_page(pos0 + key) * row_bytes;
+      const int64_t off = place(of, key >> 3);
       buffer_to_lds(raw_rsrc(a.k + off, 0xffffffffu), kcol, 0, dk + key * D);
       buffer_to_lds(raw_rsrc(a.v + off, 0xffffffffu), vcol, 0, dv + key * D);
     }
@@ -555,23 +575,19 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
     uint32_t ks, vs;  // scale bytes of the stage, as its entries
   };
   const uint32_t ecol = (uint32_t)((lane / kELanes & 7) * row_bytes + g * D + lane % kELanes * 16);
-  auto load_codes = [&](int st, int ent, Codes& x) __attribute__((always_inline)) {
-    const int pos0 = steps.tile(min(st, end - 1)) * kKeys;
+  auto load_codes = [&](int64_t of, int ent, Codes& x) __attribute__((always_inline)) {
     ent = names_page(a, ent) ? ent : 0;
     x.ks = a.k_scale[(int64_t)ent * a.Hkv + g];
     x.vs = a.v_scale[(int64_t)ent * a.Hkv + g];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int key = (4 * i + wave) * kERows;
-      const auto at = [&](int k) {  // where the 8 keys from k on begin
-        return (int64_t)__builtin_amdgcn_readlane(ent, k >> 3) * a.page_stride + (int64_t)in_page(pos0 + k) * row_bytes;
-      };
+      const int group = (4 * i + wave) * kERows >> 3;
       if constexpr (kERows == 8) {
-        const int64_t off = at(key);
+        const int64_t off = place(of, group);
         x.k[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(raw_rsrc(a.k + off, 0xffffffffu), ecol, 0, 0));
         x.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(raw_rsrc(a.v + off, 0xffffffffu), ecol, 0, 0));
-      } else {  // (at D = 64 a load has rows of two groups of 8 keys)
-        const int64_t lo = at(key), hi = at(key + 8), off = (lane >> 5 ? hi : lo) + ecol;
+      } else {  // (at D = 64 a load has rows of two groups)
+        const int64_t lo = place(of, group), hi = place(of, group + 1), off = (lane >> 5 ? hi : lo) + ecol;
         x.k[i] = *reinterpret_cast<const u32x4*>(a.k + off);
         x.v[i] = *reinterpret_cast<const u32x4*>(a.v + off);
       }
@@ -605,33 +621,29 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   f32x16 o[D / 32];
   float l[2], ref;
 
-  // -inf where this lane's row must not see a key of half `sub` of the stage at pos0: keys
-  // past its own position or the sequence's end, keys before its window, keys of a missing
-  // page (`there`: bit i, the page of the stage's keys 8 i .. + 7), as far as the stage has
-  // any.  Register v holds key 16 (v / 8) + v % 8 + 8 half of the half.
+  // -inf where this lane's row must not see a key of half `sub` of stage st: keys past its
+  // own position or the sequence's end, keys before its window, keys of a missing page
+  // (`there`: bit i, the page of the stage's group i), as far as the stage has any.
+  // Registers 8 i .. + 7 hold the keys of group 4 sub + 2 i + half.
   const int upper = min(p, kv_end - 1);
-  auto mask = [&](int pos0, int sub, uint32_t there, bool up, bool low, f32x16& s) __attribute__((always_inline)) {
-    const int base = pos0 + kSub * sub + 8 * half;
-    if (up) {
-      const int most = upper - base;
+  auto mask = [&](int st, int sub, uint32_t there, bool up, bool low, f32x16& s) __attribute__((always_inline)) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = 16 * (v >> 3) + (v & 7) <= most ? s[v] : -INFINITY;
-    }
-    if (low) {
-      const int least = p - a.window - base, first = a.sinks - base;  // sees above, and below
+    for (int i = 0; i < 2; ++i) {
+      const int group = 4 * sub + 2 * i + half, pos = groups.pos(8 * st + group);
+      if (up) {
+        const int most = upper - pos;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int key = 16 * (v >> 3) + (v & 7);
-        s[v] = key > least || key < first ? s[v] : -INFINITY;
+        for (int v = 0; v < 8; ++v) s[8 * i + v] = v <= most ? s[8 * i + v] : -INFINITY;
       }
-    }
-    if (there != 0xffu) {
+      if (low) {
+        const int least = p - a.window - pos, first = a.sinks - pos;  // sees above, and below
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (!(there >> (4 * sub + 2 * i + half) & 1)) {
+        for (int v = 0; v < 8; ++v) s[8 * i + v] = v > least || v < first ? s[8 * i + v] : -INFINITY;
+      }
+      if (there != 0xffu && !(there >> group & 1)) {
 #pragma unroll
-          for (int v = 0; v < 8; ++v) s[8 * i + v] = -INFINITY;
-        }
+        for (int v = 0; v < 8; ++v) s[8 * i + v] = -INFINITY;
+      }
     }
   };
   // The reference follows the logits of a half.  `before`: the half whose numerators are
@@ -681,11 +693,11 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
       Codes codes;
       if constexpr (kE4) {
         ent2 = entries(begin + 2);
-        load_codes(begin, ent, codes);
+        load_codes(places(begin, ent), ent, codes);
         static_for<4 * kLoads>([&](auto n) { write_codes(n, codes, k0, v0); });
-        load_codes(begin + 1, ent1, codes);
+        load_codes(places(min(begin + 1, end - 1), ent1), ent1, codes);
       } else {
-        load_direct(begin, ent, k0, v0);
+        load_direct(places(begin, ent), k0, v0);
       }
       stage_barrier();
       bf16x8 ka[kG];  // K fragments of the current stage's first 32 keys
@@ -696,20 +708,21 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           __attribute__((always_inline)) {
         uint32_t ko = kfo, vo = voff;
         asm volatile("" : "+v"(ko), "+v"(vo));
-        const int pos0 = steps.tile(st) * kKeys, last = pos0 + kKeys;
+        const int pos0 = groups.pos(8 * st), last = groups.pos(8 * st + 7) + 8;
+        const bool sinks = 8 * st < groups.n_sink;  // the first groups are of the sinks
         // what some row of the block must not see, and which pages are there
         const uint32_t there = (uint32_t)__ballot(names_page(a, ent)) & 0xffu;
         const bool up = last > min(p0 + 1, kv_end);
-        const bool low = a.window > 0 && pos0 <= p1 - a.window && last > a.sinks;
+        const bool low = a.window > 0 && (sinks || pos0 <= p1 - a.window) && last > a.sinks;
         const bool edge = up || low || there != 0xffu;
         const bool check = edge || st == begin || look;
         const int after = entries(st + (kE4 ? 3 : 2));
         if constexpr (!kE4)
-          if (st + 1 < end) load_direct(st + 1, ent1, nk, nv);
+          if (st + 1 < end) load_direct(places(st + 1, ent1), nk, nv);
         if (there != 0xffu || last > min(p1 + 1, kv_end) ||
-            (a.window > 0 && pos0 <= p0 - a.window && last > a.sinks)) {
+            (a.window > 0 && (sinks || pos0 <= p0 - a.window) && last > a.sinks)) {
           // a weight of 0 does not undo a NaN: V rows that no query of the block sees are cleared
-          const int key = (int)threadIdx.x >> 2, pos = pos0 + key;  // four threads a row
+          const int key = (int)threadIdx.x >> 2, pos = groups.pos(8 * st + (key >> 3)) + (key & 7);  // four threads a row
           if (!((there >> (key >> 3) & 1) && pos < kv_end && pos <= p1 &&
                 (a.window <= 0 || pos > p0 - a.window || pos < a.sinks)))
 #pragma unroll
@@ -723,6 +736,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) s0[v] = s1[v] = 0.f;
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
           kb[i] = read_k<D>(lk, ko, 1, i);
           s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[i], qf[i], s0, 0, 0, 0);
@@ -730,8 +744,9 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           if constexpr (kE4) write_codes(i, codes, nk, nv);
           __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (kE4) load_codes(st + 2, ent2, codes);
-        if (edge) mask(pos0, 0, there, up, low, s0);
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (kE4) load_codes(places(min(st + 2, end - 1), ent2), ent2, codes);
+        if (edge) mask(st, 0, there, up, low, s0);
         if (check) follow(s0, nullptr, nullptr);
         __builtin_amdgcn_sched_barrier(0);
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
@@ -741,7 +756,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           numerator_step<kE, i>(s0, a.c1, ref, l, p0b);
           __builtin_amdgcn_sched_barrier(0);
         });
-        if (edge) mask(pos0, 1, there, up, low, s1);
+        if (edge) mask(st, 1, there, up, low, s1);
         if (check) follow(s1, &s0, p0b);
         __builtin_amdgcn_sched_barrier(0);
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
@@ -761,6 +776,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           stage_barrier();  // the next stage has landed; this one's buffers are read
         }
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
           constexpr int kk = i / (D / 32), db = i % (D / 32);
           ka[i] = read_k<D>(nk, ko, 0, i);  // (after the last stage: read and not used)
@@ -769,6 +785,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
                                                           o[db], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
         });
+        __builtin_amdgcn_s_setprio(0);
         ent = ent1;
         if constexpr (kE4) {
           ent1 = ent2;
@@ -927,7 +944,7 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
   p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32;
   if (p.wide) {
     p.blocks = b->n_tokens * G / tile::kBlockRows + b->n_seqs;
-    if (window > 0) len = std::min<int64_t>(len, (int64_t)window + ceil_div(tile::kBlockRows, G) + sinks + 2 * tile::kTile);
+    if (window > 0) len = std::min<int64_t>(len, (int64_t)window + ceil_div(tile::kBlockRows, G) + sinks + 16);
     const int64_t steps = ceil_div(len, tile::kTile);
     // The splits that cost least by a model of the launch, in cycles at 1.85 GHz: 512
     // workgroups run at once, two per CU, each for its stages (3,440 cycles a stage for two,
