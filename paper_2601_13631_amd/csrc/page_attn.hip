@@ -938,7 +938,9 @@ struct PageAttnPlan {
 PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq, int window, int sinks) {
   PageAttnPlan p{};
   const int G = Hq / pool->n_kv_heads;
-  const int64_t most = b->max_tokens > 0 ? std::min<int64_t>(b->max_tokens, b->n_tokens) : b->n_tokens;
+  // (some sequence has at least the mean, whatever max_tokens says)
+  const int64_t most = b->max_tokens > 0 ? std::min(std::max<int64_t>(b->max_tokens, ceil_div(b->n_tokens, std::max(b->n_seqs, 1))), b->n_tokens)
+                                         : b->n_tokens;
   int64_t len = (int64_t)b->max_pages * pool->page_size;
   if (b->max_len > 0) len = std::min<int64_t>(len, b->max_len);
   p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32;

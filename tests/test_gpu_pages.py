@@ -104,6 +104,54 @@ def test_rising_logits(cache, heads, new):
     check_attention(c, attend(pool, batch, c.q.to(DEV)))
 
 
+def draw_attention(seed):
+    """A random case: heads, page, ragged lengths, window, missing pages, layout, hints."""
+    rng = np.random.default_rng(1000 + seed)
+    cache = ("bf16", "e4m3", "bf16", "e4m3", "f32")[seed % 5]
+    d = 64 if cache == "f32" else int(rng.choice((64, 128)))
+    hkv = int(rng.integers(1, 8))
+    heads = (hkv * int(rng.integers(1, 9)), hkv, d)
+    page = int(rng.choice((8, 16, 32, 64, 96, 128)))
+    top = int(np.exp(rng.uniform(0, np.log(3000))))
+    many = int(np.exp(rng.uniform(0, np.log(300)))) if rng.random() < 0.6 else 1
+    seqs = []
+    for _ in range(int(rng.integers(1, 7))):
+        n = int(rng.integers(0, many + 1))
+        seqs.append((n, n + int(rng.integers(0, top + 1))))
+    seqs[0] = (many, many + top)
+    window = int(np.exp(rng.uniform(0, np.log(800)))) if rng.random() < 0.6 else 0
+    sinks = int(rng.choice((0, 1, 4, 7, 64, 100)))
+    missing = [(b, int(rng.integers(0, -(-m // page)))) for b, (n, m) in enumerate(seqs) if m and rng.random() < 0.4]
+    return cache, heads, page, seqs, window, sinks, missing, rng
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_attention_random(seed):
+    cache, heads, page, seqs, window, sinks, missing, rng = draw_attention(seed)
+    c = Cache(cache, heads, page, seqs, seed=seed, missing=missing, interleaved=bool(rng.random() < 0.3))
+    c.poison(window, sinks)
+    hints = {} if rng.random() < 0.6 else dict(max_tokens=int(rng.integers(0, 50)), max_len=int(rng.integers(0, 2000)))
+    after = int(rng.integers(0, 3))
+    pool, batch = c.device(table_gap=int(rng.integers(0, 4)), rows_after=after, **hints)
+    out = attend(pool, batch, c.q.to(DEV), window, sinks, rows_after=after)
+    check_attention(c, out, window, sinks)
+    assert (out[c.tokens:] == 7).all()
+    assert torch.equal(out, attend(pool, batch, c.q.to(DEV), window, sinks, rows_after=after))  # bit for bit
+
+
+def test_lengths_past_the_table():
+    """A sequence longer than its table: its queries see what the table holds."""
+    import paper_2601_13631_amd as ckv
+    for cache, heads in (("bf16", H7), ("e4m3", H05), ("f32", HF)):
+        for new in (1, 70):
+            c = Cache(cache, heads, 16, [(new, 200), (new, 90)], seed=3)
+            c.table = np.ascontiguousarray(c.table[:, :4])
+            c.width = 4
+            pool = ckv.PagePool(*c.device_pages())
+            batch = ckv.PageBatch(*(torch.from_numpy(x).to(DEV) for x in (c.table, c.lens, c.off)), c.tokens)
+            check_attention(c, attend(pool, batch, c.q.to(DEV)))
+
+
 def test_attention_scale():
     c = Cache("bf16", H7, 16, [(1, 200), (30, 90)], seed=2)
     pool, batch = c.device()
@@ -368,3 +416,127 @@ def test_serving_loop(cache, heads):
             c.scale[n] = c.scale[n][come].clone()
     step([30, 1, 1], 0, 0)
     step([0, 1, 40], 33, 1)
+
+
+# ---- streams, graphs, refusals -------------------------------------------------------------
+
+def serving_step(ckv, c, pool, layers, batch, q, out, ws, window):
+    ckv.page_append(pool, batch, c["k"], c["v"])
+    ckv.page_attn(pool, batch, q, out, ws, window=window, n_sinks=4)
+    ckv.page_copy(layers, c["src"], c["dst"])
+    ckv.page_compact(layers, c["refs"], c["refs_out"], c["table"], c["table_out"], c["live"], c["cws"])
+
+
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("e4m3", H7), ("f32", HF)])
+@pytest.mark.parametrize("new", [1, 80])
+@pytest.mark.parametrize("window", [0, 100])
+def test_graphs(cache, heads, new, window):
+    """Two captured graphs with workspaces of their own, replayed in turn with other inputs and
+    lengths, against eager calls on a copy."""
+    import paper_2601_13631_amd as ckv
+    sides = []
+    for g in range(2):
+        c = Cache(cache, heads, 16, [(new, 2000 - 300 * g), (new, 100 + new)], seed=20 + g)
+        two = []
+        for _ in range(2):  # the graph's and the eager calls' own
+            pool, batch = c.device(max_len=2000)
+            x = {"k": c.new_rows["k"].to(DEV), "v": c.new_rows["v"].to(DEV)}
+            x["src"], x["dst"] = (torch.tensor(i, dtype=torch.int32, device=DEV) for i in ([0, 1], [c.n_pages - 1, c.n_pages - 2]))
+            refs = torch.ones(c.n_pages, dtype=torch.int32, device=DEV)
+            refs[3::4] = 0
+            x["refs"], x["refs_out"] = refs, torch.zeros_like(refs)
+            x["table"] = batch.table.contiguous()
+            x["table_out"] = torch.zeros_like(x["table"])
+            x["live"] = torch.zeros(1, dtype=torch.int32, device=DEV)
+            x["cws"] = torch.empty(ckv.page_compact_workspace_bytes(c.n_pages), dtype=torch.uint8, device=DEV)
+            q = c.q.to(DEV)
+            out = torch.zeros_like(q)
+            ws = torch.empty(ckv.page_attn_workspace_bytes(pool, batch, q.shape[1], window, 4), dtype=torch.uint8, device=DEV)
+            two.append((x, pool, ckv.PageLayers([pool]), batch, q, out, ws, window))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            serving_step(ckv, *two[0])
+        sides.append((graph, *two))
+    for i in range(4):
+        for graph, a, b in sides:
+            g = torch.Generator(DEV).manual_seed(i)
+            fresh = torch.randn(a[4].shape, generator=g, device=DEV).to(a[4].dtype)
+            for s in (a, b):
+                s[4].copy_(fresh)
+                s[3].lens.sub_(i)
+            graph.replay()
+            serving_step(ckv, *b)
+            torch.cuda.synchronize()
+            assert torch.equal(a[5], b[5])
+            for n in ("k", "v", "k_scale", "v_scale"):
+                u, v = getattr(a[1], n), getattr(b[1], n)
+                assert u is None or torch.equal(bytes_of(u), bytes_of(v))
+            for n in ("refs_out", "table_out", "live"):
+                assert torch.equal(a[0][n], b[0][n])
+
+
+def test_streams():
+    """Calls on two streams at once, each with a workspace of its own, and a stream that is given."""
+    import paper_2601_13631_amd as ckv
+    cs = [Cache("bf16", H7, 32, [(1, 9000), (1, 500)], seed=i) for i in range(2)]
+    made = [c.device() for c in cs]
+    qs = [c.q.to(DEV) for c in cs]
+    outs = [torch.zeros_like(q) for q in qs]
+    wss = [torch.empty(ckv.page_attn_workspace_bytes(*m, 28), dtype=torch.uint8, device=DEV) for m in made]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for i in range(2):
+            if i:
+                ckv.page_attn(*made[i], qs[i], outs[i], wss[i], stream=streams[i])
+            else:
+                with torch.cuda.stream(streams[i]):
+                    ckv.page_attn(*made[i], qs[i], outs[i], wss[i])
+    torch.cuda.synchronize()
+    for c, out in zip(cs, outs):
+        check_attention(c, out)
+
+
+def test_wrappers_refuse():
+    import paper_2601_13631_amd as ckv
+    c = Cache("bf16", H7, 16, [(3, 50)], seed=0)
+    pool, batch = c.device()
+    q = c.q.to(DEV)
+    k = c.new_rows["k"].to(DEV)
+    for bad in (q[:2], q.float(), q.cpu(), q.transpose(0, 1), q[..., :64]):
+        with pytest.raises(ValueError):
+            ckv.page_attn(pool, batch, bad, torch.empty_like(q))
+    for bad in (q[:, :14], q.float(), torch.empty(q.shape[::-1], dtype=q.dtype, device=DEV).permute(2, 1, 0)):
+        with pytest.raises(ValueError):
+            ckv.page_attn(pool, batch, q, bad)
+    with pytest.raises(ckv.CkvError):
+        ckv.page_attn(pool, batch, q[:, :27].contiguous(), q[:, :27].contiguous())
+    for bad in (dict(window=-1), dict(n_sinks=-1), dict(window=1 << 32)):
+        with pytest.raises(ValueError):
+            ckv.page_attn(pool, batch, q, torch.empty_like(q), **bad)
+    for bad in (k[:2], k.float(), k[:, :2]):
+        with pytest.raises(ValueError):
+            ckv.page_append(pool, batch, bad, k)
+    with pytest.raises(ValueError):
+        ckv.PagePool(pool.k, pool.v, torch.zeros(c.n_pages, 4, dtype=torch.uint8, device=DEV))
+    e = pool.k.to(torch.float8_e4m3fn)
+    s = torch.zeros(c.n_pages, 4, dtype=torch.uint8, device=DEV)
+    ckv.PagePool(e, e, s, s)
+    for bad in ((None, None), (s, None), (s.int(), s), (s[:-1], s), (s.t().contiguous().t(), s)):
+        with pytest.raises(ValueError):
+            ckv.PagePool(e, e, *bad)
+    with pytest.raises(ValueError):
+        ckv.PagePool(pool.k.transpose(1, 2), pool.v.transpose(1, 2))
+    with pytest.raises(ValueError):
+        ckv.PagePool(pool.k[::2], pool.v[:pool.k[::2].shape[0]])
+    for bad in (batch.table.long(), batch.table.t(), batch.table[0]):
+        with pytest.raises(ValueError):
+            ckv.PageBatch(bad, batch.lens, batch.tok_off, 3)
+    with pytest.raises(ValueError):
+        ckv.PageBatch(batch.table, batch.lens, batch.tok_off[:1], 3)
+    i = torch.zeros(3, dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError):
+        ckv.page_copy(ckv.PageLayers([pool]), i, i[:2])
+    with pytest.raises(ValueError):
+        ckv.page_copy(ckv.PageLayers([pool]), i.long(), i)
