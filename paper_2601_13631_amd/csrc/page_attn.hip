@@ -114,13 +114,15 @@ struct Elem<CKV_DTYPE_E4M3> {
   using Q = __bf16;
 };
 
-// What a wave holds of a step: table entries and rows, as loaded.
+// What a wave holds of a step: the table entries of its 16-key (kSmall: 8-key) groups and
+// where these begin in the pool, and its V rows and scales as loaded.
+template <bool kSmall>
 struct Pages {
-  int k0, k1, v0, v1;
+  __attribute__((ext_vector_type(kSmall ? 4 : 2))) int e;
+  __attribute__((ext_vector_type(kSmall ? 4 : 2))) int64_t at;
 };
 template <int D, int T>
 struct Step {
-  u32x4 k[2][D * Elem<T>::kBytes / 64];
   uint32_t v[2][4][D / 16 * Elem<T>::kBytes / 4];
   uint32_t ks[2], vs[2];
 };
@@ -140,8 +142,12 @@ __device__ __forceinline__ bf16x8 bf16_of_codes(uint32_t w0, uint32_t w1, float 
   return __builtin_bit_cast(bf16x8, r);
 }
 
+// s_waitcnt: vmcnt(0); lgkmcnt(0).
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }
+
 // Few rows: a workgroup owns 16 query rows of one KV head and one split of their
-// steps, each wave every fourth step of it, straight from memory to registers:
+// steps, each wave every fourth step of it:
 //   S^T = K Q^T    MFMA 16x16 (bf16: x32, fp32: x4), two groups of 16 keys; lane l
 //                  then holds row l % 16 and keys 4 (l / 16) + 0..3 of each group
 //   O^T += V^T P^T the contraction's 8 (bf16) keys per lane are those it holds, so
@@ -149,16 +155,19 @@ __device__ __forceinline__ bf16x8 bf16_of_codes(uint32_t w0, uint32_t w1, float 
 //                  loads D/16 elements from l % 16 * D/16 on of its 8 keys' V rows, and
 //                  product i of D/16 takes element i of each (8 keys x D/16 elements
 //                  are turned over in registers).
-// The waves' outputs are joined through LDS, the splits' by page_combine_kernel.
-// kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page, and
-// the page numbers are uniform).
+// V rows go straight to registers, 16 lanes a row.  The K operand wants neighbouring
+// lanes in different rows, which read so cost the cache an access per 16 bytes: K rows go
+// whole to LDS, a step ahead, into a buffer of the wave's own.  The waves' outputs are
+// joined through LDS, the splits' by page_combine_kernel.
+// kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page).
 template <int D, int T, bool kSmall>
 __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs a) {
   using E = Elem<T>;
   using QT = typename E::Q;
   constexpr bool kF32 = T == CKV_DTYPE_F32, kE4 = T == CKV_DTYPE_E4M3;
   constexpr int kVec = D / 16;                    // elements of a V row per lane, and products of O
-  constexpr int kPieces = D * E::kBytes / 64;     // 16-byte pieces of a K row per lane
+  constexpr int kRow = D * E::kBytes;             // bytes of a K row in LDS
+  constexpr int kPieces = kRow / 64;              // 16-byte pieces of a K row per lane
   constexpr int kVWords = kVec * E::kBytes / 4;   // dwords of a V row per lane
 
   // The KV heads of one slice of keys are neighbours on one XCD, where together they read
@@ -174,8 +183,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
   if (sp.count == 0) return;
   const int32_t* tab = a.s.table + (int64_t)b * a.s.table_stride;
   const int kv_end = (int)min<int64_t>(max(sp.len, 0), (int64_t)a.s.max_pages * a.c);
-  const int row_bytes = a.Hkv * D * E::kBytes, kvh = g, g_bytes = g * D * E::kBytes;
-  const int64_t rows = (int64_t)sp.count * a.G;
+  const int row_bytes = a.Hkv * kRow, kvh = g, g_bytes = g * kRow;
+  const int rows = sp.count * a.G;
   const int p_base = sp.len - sp.count;
   // this sequence's own number of splits, by its length
   const int all_steps = steps_of(a, p_base, p_base + sp.count - 1, kv_end).n;
@@ -184,20 +193,37 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
   if (a.n_splits > 1 && split == 0 && g == 0 && blockIdx.y == 0)
     for (int i = threadIdx.x; i < sp.count; i += 64 * kWaves) a.n_parts[sp.first + i] = n_parts;
 
-  __shared__ float lds_o[kWaves][kRows][D + 4];
-  __shared__ float2 lds_ml[kWaves][kRows];
+  // the waves' K buffers, and after the last step their outputs
+  struct Joined {
+    float o[kWaves][kRows][D + 4];
+    float2 ml[kWaves][kRows];
+  };
+  constexpr int kLds = sizeof(Joined) > kWaves * kTile * kRow ? sizeof(Joined) : kWaves * kTile * kRow;
+  __shared__ __attribute__((aligned(16))) char lds[kLds];
+  Joined& joined = *reinterpret_cast<Joined*>(lds);
+  char* lds_k = lds + wave * kTile * kRow;
+  // A load to LDS moves kLoadRows rows, lane l 16 bytes of row l / kSegs: the segment at
+  // position s of row r is segment s ^ swz(r), so that 16 lanes that read one piece of 16
+  // rows each meet 64 different banks.
+  constexpr int kSegs = kRow / 16, kLoadRows = 64 / kSegs, kLoads = kTile / kLoadRows;
+  constexpr auto swz = [](int r) { return kSegs == 16 ? r & 15 : kSegs == 8 ? r >> 1 & 7 : r >> 2 & 3; };
+  const uint32_t k_col = (uint32_t)(lane / kSegs * row_bytes + g_bytes + ((lane % kSegs) ^ swz(lane / kSegs)) * 16);
+  uint32_t k_at[kPieces];  // this lane's pieces of row n16
+#pragma unroll
+  for (int y = 0; y < kPieces; ++y) k_at[y] = (uint32_t)(n16 * kRow + (((j4 + 4 * y) ^ swz(n16)) * 16));
+  const uint32_t v_col = (uint32_t)(4 * j4 * row_bytes + g_bytes + n16 * kVec * E::kBytes);
 
-  for (int64_t rb = blockIdx.y; rb * kRows < rows; rb += gridDim.y) {
-    const int64_t r_first = rb * kRows, r_last = min<int64_t>(rows, r_first + kRows) - 1;
-    const int p0 = p_base + (int)(r_first / a.G), p1 = p_base + (int)(r_last / a.G);
+  for (int rb = blockIdx.y; rb * kRows < rows; rb += gridDim.y) {
+    const int r_first = rb * kRows, r_last = min(rows, r_first + kRows) - 1;
+    const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
     const Steps steps = steps_of(a, p0, p1, kv_end);
-    const int begin = (int)((int64_t)steps.n * split / n_parts);
-    const int end = (int)((int64_t)steps.n * (split + 1) / n_parts);
+    const int per = steps.n / n_parts, over = steps.n % n_parts;  // the first `over` splits: one more
+    const int begin = split * per + min(split, over), end = begin + per + (split < over ? 1 : 0);
 
     // this lane's row: its query (position p) and head
-    const int64_t r = min<int64_t>(r_first + n16, r_last);
+    const int r = min(r_first + n16, r_last);
     const int64_t tok = sp.first + r / a.G;
-    const int head = g * a.G + (int)(r % a.G), p = p_base + (int)(r / a.G);
+    const int head = g * a.G + r % a.G, p = p_base + r / a.G;
     const QT* q = static_cast<const QT*>(a.q) + (tok * a.Hq + head) * D;
     // Q^T operands in the order of the K pieces
     f32x4 qf[kF32 ? kPieces : 1];
@@ -219,60 +245,89 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
     for (int i = 0; i < kVec; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float ref = kNone, l = 0.f;
 
-    // Pages of a step's keys: this lane's K rows 16 i + n16, V rows 16 i + 4 j4 + 0..3.
-    auto slot_of = [&](int pos) { return a.log2c >= 0 ? pos >> a.log2c : (int)((uint32_t)pos / (uint32_t)a.c); };
-    auto pages_of = [&](int st, Pages& g) __attribute__((always_inline)) {
+    // The table entries of a step's groups of keys.
+    constexpr int kGroup = kSmall ? 8 : 16;
+    auto pages_of = [&](int st, Pages<kSmall>& x) __attribute__((always_inline)) {
       const int pos0 = steps.tile(st) * kTile;
-      if constexpr (!kSmall) {
-        g.k0 = g.v0 = entry_of_uniform(a, tab, slot_of(pos0));
-        g.k1 = g.v1 = entry_of_uniform(a, tab, slot_of(pos0 + 16));
-      } else {
-        const int k = (pos0 + n16) >> 3, v = (pos0 + 4 * j4) >> 3;
-        g.k0 = entry_of(a, tab, k);
-        g.k1 = entry_of(a, tab, k + 2);
-        g.v0 = entry_of(a, tab, v);
-        g.v1 = entry_of(a, tab, v + 2);
+#pragma unroll
+      for (int i = 0; i < kTile / kGroup; ++i) {
+        const int pos = pos0 + kGroup * i;
+        x.e[i] = entry_of_uniform(a, tab, kSmall ? pos >> 3 : a.log2c >= 0 ? pos >> a.log2c
+                                                                           : (int)((uint32_t)pos / (uint32_t)a.c));
       }
     };
-    // Its rows (a key that is not there reads page 0 and counts for nothing).
-    auto load = [&](int st, const Pages& g, Step<D, T>& x) __attribute__((always_inline)) {
+    // (a missing page: page 0, and its keys count for nothing)
+    auto locate = [&](int st, Pages<kSmall>& x) __attribute__((always_inline)) {
       const int pos0 = steps.tile(st) * kTile;
-      const int pk[2] = {names_page(a, g.k0) ? g.k0 : 0, names_page(a, g.k1) ? g.k1 : 0};
-      const int pv[2] = {names_page(a, g.v0) ? g.v0 : 0, names_page(a, g.v1) ? g.v1 : 0};
-      if constexpr (kE4) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          x.ks[i] = a.k_scale[(int64_t)pk[i] * a.Hkv + kvh];
-          x.vs[i] = a.v_scale[(int64_t)pv[i] * a.Hkv + kvh];
+      for (int i = 0; i < kTile / kGroup; ++i) {
+        const int pos = pos0 + kGroup * i;
+        const int r0 = kSmall ? 0 : a.log2c >= 0 ? pos & (a.c - 1) : (int)((uint32_t)pos % (uint32_t)a.c);
+        x.at[i] = (int64_t)(names_page(a, x.e[i]) ? x.e[i] : 0) * a.page_stride + (int64_t)r0 * row_bytes;
+      }
+    };
+    auto load_k = [&](const Pages<kSmall>& x) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        constexpr int kPer = kLoadRows > kGroup ? kLoadRows / kGroup : 1;  // groups of a load: 2 at most
+        const uint32_t col = k_col ^ (uint32_t)(64 * (i & (kSegs / 4 - 1)));
+#pragma unroll
+        for (int h = 0; h < kPer; ++h) {
+          const int key = i * kLoadRows + h * kGroup;
+          const __amdgpu_buffer_rsrc_t rsrc = tile::raw_rsrc(a.k + x.at[key / kGroup], 0xffffffffu);
+          // (the second half of a load has the second group: 8 rows back in the lanes' offsets)
+          const uint32_t in_group = (uint32_t)(key % kGroup * row_bytes);
+          if (kPer == 1 || lane >> 5 == h)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (tile::LdsPtr)(lds_k + i * kLoadRows * kRow), 16,
+                                                     col - (uint32_t)(h * kGroup * row_bytes), in_group, 0, 0);
+        }
+      }
+    };
+    auto load_v = [&](const Pages<kSmall>& x, Step<D, T>& y) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (kE4) {  // pages of K row 16 i + n16, V rows 16 i + 4 j4 ..
+          int pk = x.e[kSmall ? 2 * i : i], pv = pk;
+          if constexpr (kSmall) {
+            pk = n16 & 8 ? x.e[2 * i + 1] : pk;
+            pv = j4 & 2 ? x.e[2 * i + 1] : pv;
+          }
+          y.ks[i] = a.k_scale[(int64_t)(names_page(a, pk) ? pk : 0) * a.Hkv + kvh];
+          y.vs[i] = a.v_scale[(int64_t)(names_page(a, pv) ? pv : 0) * a.Hkv + kvh];
         }
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        int kr = n16 & 7, vr = (4 * j4) & 7;  // rows inside the page
-        if constexpr (!kSmall) {
-          const int pos = pos0 + 16 * i;
-          const int in_page = a.log2c >= 0 ? pos & (a.c - 1) : (int)((uint32_t)pos % (uint32_t)a.c);
-          kr = in_page + n16;
-          vr = in_page + 4 * j4;
-        }
-        const char* k_at = a.k + (int64_t)pk[i] * a.page_stride + (int64_t)kr * row_bytes +
-                           g_bytes + 16 * j4;
+        if constexpr (kSmall) {
+          const int64_t lo = x.at[2 * i], hi = x.at[2 * i + 1] - 8 * (int64_t)row_bytes;
+          const char* at = a.v + (j4 & 2 ? hi : lo) + v_col;
 #pragma unroll
-        for (int y = 0; y < kPieces; ++y) x.k[i][y] = *reinterpret_cast<const u32x4*>(k_at + 64 * y);
-        const char* v_at = a.v + (int64_t)pv[i] * a.page_stride + (int64_t)vr * row_bytes +
-                           g_bytes + n16 * kVec * E::kBytes;
+          for (int k = 0; k < 4; ++k) {
+            if constexpr (kVWords == 4)
+              *reinterpret_cast<u32x4*>(y.v[i][k]) = *reinterpret_cast<const u32x4*>(at + k * row_bytes);
+            else if constexpr (kVWords == 2)
+              *reinterpret_cast<uint2*>(y.v[i][k]) = *reinterpret_cast<const uint2*>(at + k * row_bytes);
+            else
+              y.v[i][k][0] = *reinterpret_cast<const uint32_t*>(at + k * row_bytes);
+          }
+        } else {
+          const __amdgpu_buffer_rsrc_t rsrc = tile::raw_rsrc(a.v + x.at[i], 0xffffffffu);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          if constexpr (kVWords == 4)
-            *reinterpret_cast<u32x4*>(x.v[i][y]) = *reinterpret_cast<const u32x4*>(v_at + y * row_bytes);
-          else if constexpr (kVWords == 2)
-            *reinterpret_cast<uint2*>(x.v[i][y]) = *reinterpret_cast<const uint2*>(v_at + y * row_bytes);
-          else
-            x.v[i][y][0] = *reinterpret_cast<const uint32_t*>(v_at + y * row_bytes);
+          for (int k = 0; k < 4; ++k) {
+            if constexpr (kVWords == 4)
+              *reinterpret_cast<u32x4*>(y.v[i][k]) =
+                  __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, v_col, k * row_bytes, 0));
+            else if constexpr (kVWords == 2)
+              *reinterpret_cast<uint2*>(y.v[i][k]) =
+                  __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, v_col, k * row_bytes, 0));
+            else
+              y.v[i][k][0] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, v_col, k * row_bytes, 0);
+          }
         }
       }
     };
-    auto attend = [&](int st, const Pages& g, Step<D, T>& x) __attribute__((always_inline)) {
+    auto attend = [&](int st, const Pages<kSmall>& e, const u32x4 (&kw)[2][kPieces], Step<D, T>& x)
+        __attribute__((always_inline)) {
       const int pos0 = steps.tile(st) * kTile;
       float ks[2], vs[2];
       if constexpr (kE4) {
@@ -284,40 +339,47 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
       }
       f32x4 s[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (kF32) {
+      for (int i = 0; i < 2; ++i) s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (kF32) {
 #pragma unroll
-          for (int y = 0; y < kPieces; ++y)
+        for (int y = 0; y < kPieces; ++y)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.k[i][y][e]), qf[y][e], s[i], 0, 0, 0);
-        } else if constexpr (kE4) {
+          for (int z = 0; z < 4; ++z)
 #pragma unroll
-          for (int y = 0; y < D / 32; ++y)
+            for (int i = 0; i < 2; ++i)
+              s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[i][y][z]), qf[y][z], s[i], 0, 0, 0);
+      } else if constexpr (kE4) {
+#pragma unroll
+        for (int y = 0; y < D / 32; ++y)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
             s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                bf16_of_codes(x.k[i][y >> 1][2 * (y & 1)], x.k[i][y >> 1][2 * (y & 1) + 1], ks[i]), qb[y],
+                bf16_of_codes(kw[i][y >> 1][2 * (y & 1)], kw[i][y >> 1][2 * (y & 1) + 1], ks[i]), qb[y],
                 s[i], 0, 0, 0);
-        } else {
+      } else {
 #pragma unroll
-          for (int y = 0; y < D / 32; ++y)
-            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[i][y]), qb[y],
+        for (int y = 0; y < D / 32; ++y)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw[i][y]), qb[y],
                                                            s[i], 0, 0, 0);
-        }
       }
       // what some row of the block must not see
       const int last = pos0 + kTile;
-      const bool all = last <= min(p0 + 1, kv_end) &&
-                       (a.window <= 0 || pos0 > p1 - a.window || last <= a.sinks);
-      const bool there0 = names_page(a, g.v0), there1 = names_page(a, g.v1);
-      if (!all || __any(!there0 || !there1)) {
+      bool all = last <= min(p0 + 1, kv_end) &&
+                 (a.window <= 0 || pos0 > p1 - a.window || last <= a.sinks);
+#pragma unroll
+      for (int i = 0; i < kTile / kGroup; ++i) all = all && names_page(a, e.e[i]);
+      if (!all) {
         const int lo = a.window > 0 ? p0 - a.window : -1;  // the block's first row sees keys past it
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i) {
+          int page = e.e[kSmall ? 2 * i : i];
+          if constexpr (kSmall) page = j4 & 2 ? e.e[2 * i + 1] : page;
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const int pos = pos0 + 16 * i + 4 * j4 + y;
-            const bool there = (i ? there1 : there0) && pos < kv_end;
+            const bool there = names_page(a, page) && pos < kv_end;
             if (!(there && pos <= p && (a.window <= 0 || pos > p - a.window || pos < a.sinks)))
               s[i][y] = -INFINITY;
             // a weight of 0 does not undo a NaN: rows that no query of the block sees are cleared
@@ -325,6 +387,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
 #pragma unroll
               for (int w = 0; w < kVWords; ++w) x.v[i][y][w] = 0u;
           }
+        }
       }
       float mx = -INFINITY;
 #pragma unroll
@@ -385,24 +448,40 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
       }
     };
 
-    // Each step's rows load during the step before, its table entries two steps before
-    // (and ahead of the rows that load meanwhile, for which they need not wait then).
-    // Past the end a wave reads its last step's rows once more.
+    // A step's rows load during the step before, its table entries two steps before.
     int st = begin + wave;
     if (st < end) {
-      Pages ga, gb;
+      Pages<kSmall> ga, gb;
       Step<D, T> xa, xb;
       pages_of(st, ga);
       pages_of(min(st + kWaves, end - 1), gb);
-      load(st, ga, xa);
-      auto turn = [&](Pages& g, Step<D, T>& x, const Pages& gn, Step<D, T>& xn)
+      locate(st, ga);
+      load_k(ga);
+      load_v(ga, xa);
+      __builtin_amdgcn_sched_barrier(0);
+      auto turn = [&](Pages<kSmall>& g, Step<D, T>& x, Pages<kSmall>& gn, Step<D, T>& xn)
           __attribute__((always_inline)) {
-        Pages after;
+        wait_loads();  // the K rows are in LDS
+        __builtin_amdgcn_sched_barrier(0);
+        u32x4 kw[2][kPieces];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int y = 0; y < kPieces; ++y)
+            kw[i][y] = *reinterpret_cast<const u32x4*>(lds_k + i * 16 * kRow + k_at[y]);
+        wait_lds();  // read: the next step's may come
+        __builtin_amdgcn_sched_barrier(0);
+        locate(min(st + kWaves, end - 1), gn);
+        if (st + kWaves < end) {
+          load_k(gn);
+          load_v(gn, xn);
+        }
+        Pages<kSmall> after;
         pages_of(min(st + 2 * kWaves, end - 1), after);
-        load(min(st + kWaves, end - 1), gn, xn);
-        attend(st, g, x);
+        attend(st, g, kw, x);
         g = after;
         st += kWaves;
+        __builtin_amdgcn_sched_barrier(0);
       };
       while (true) {
         turn(ga, xa, gb, xb);
@@ -414,31 +493,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
 
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (rb > (int64_t)blockIdx.y) __syncthreads();  // the last block's rows have been read
+    __syncthreads();  // every wave is through with its K rows
     // o[x][v] holds element kVec (4 j4 + v) + x of row n16
 #pragma unroll
     for (int v = 0; v < 4; ++v)
 #pragma unroll
-      for (int x = 0; x < kVec; ++x) lds_o[wave][n16][kVec * (4 * j4 + v) + x] = o[x][v];
-    if (lane < kRows) lds_ml[wave][lane] = make_float2(ref, l);
+      for (int x = 0; x < kVec; ++x) joined.o[wave][n16][kVec * (4 * j4 + v) + x] = o[x][v];
+    if (lane < kRows) joined.ml[wave][lane] = make_float2(ref, l);
     __syncthreads();
     // 16 threads per row, D / 16 elements each
     const int row = threadIdx.x >> 4, col = (threadIdx.x & 15) * kVec;
-    const int64_t rr = r_first + row;
+    const int rr = r_first + row;
     if (rr <= r_last) {
       float M = kNone, L = 0.f, f[kWaves], acc[kVec];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, lds_ml[w][row].x);
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, joined.ml[w][row].x);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(lds_ml[w][row].x - M);
-        L += f[w] * lds_ml[w][row].y;
+        f[w] = __builtin_amdgcn_exp2f(joined.ml[w][row].x - M);
+        L += f[w] * joined.ml[w][row].y;
       }
 #pragma unroll
       for (int x = 0; x < kVec; ++x) {
         acc[x] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) acc[x] += f[w] * lds_o[w][row][col + x];
+        for (int w = 0; w < kWaves; ++w) acc[x] += f[w] * joined.o[w][row][col + x];
       }
       const int64_t at = (sp.first + rr / a.G) * a.Hq + g * a.G + rr % a.G;
       if (n_parts > 1) {
@@ -460,6 +539,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
           *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(y);
       }
     }
+    if (rb + (int)gridDim.y < (rows + kRows - 1) / kRows) __syncthreads();  // read, before the next block's K rows come
   }
 }
 
@@ -504,7 +584,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   int64_t rb = a.n_blocks - 1 - blk;
   SeqSpan sp{};
   const int b = find_part(
-      a.s, [&](const SeqSpan& q) { return (int)(((int64_t)q.count * a.G + kBlockRows - 1) / kBlockRows); }, rb, sp);
+      a.s, [&](const SeqSpan& q) { return (q.count * a.G + kBlockRows - 1) / kBlockRows; }, rb, sp);
   if (b < 0) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -520,8 +600,8 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
     for (int i = r_first / a.G + (int)threadIdx.x; i <= r_last / a.G; i += 256) a.n_parts[sp.first + i] = n_parts;
   const Groups groups = groups_of(a, p0, p1, kv_end);  // a stage: 8 of them
   const int stages = (groups.n + 7) / 8;
-  const int begin = (int)((int64_t)stages * split / n_parts);
-  const int end = (int)((int64_t)stages * (split + 1) / n_parts);
+  const int per = stages / n_parts, over = stages % n_parts;  // the first `over` splits: one more
+  const int begin = split * per + min(split, over), end = begin + per + (split < over ? 1 : 0);
 
   // this lane's row
   const int row = r_first + wave * kWaveRows + (lane & 31);
@@ -864,7 +944,7 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
   constexpr int kCols = D / 4, kRowsPer = 256 / kCols / kGroups;
   const int64_t n_rows = a.s.n_tokens * a.Hq;
   const int64_t row = (int64_t)blockIdx.x * kRowsPer + threadIdx.x / (kCols * kGroups);
-  const int64_t tok = row / a.Hq;
+  const int tok = (int)row / a.Hq;  // (at most 2^26 rows)
   // (with several groups, a workgroup has one row: it leaves as a whole)
   if (row >= n_rows || tok < a.s.tok_off[0] || tok >= a.s.tok_off[a.s.n_seqs]) return;  // of no sequence
   const int n_parts = min(a.n_parts[tok], a.n_splits);
@@ -975,6 +1055,9 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + most + sinks + 2 * kTile);
     const int64_t steps = ceil_div(len, kTile);
     const int64_t wgs = (int64_t)b->n_seqs * pool->n_kv_heads * p.row_blocks;
+    // Splits of 16 steps or more (a sequence of 1,026 steps: 14.0 us; of 12: 15.8, of 24: 14.5),
+    // up to 4,096 workgroups, so that sequences of unequal lengths spread over the chip (64
+    // of 1,024 to 16,384 tokens: 165 us; up to 2,048: 183, up to 8,192: 170).
     p.n_splits = (int)std::max<int64_t>(1, std::min(4096 / std::max<int64_t>(wgs, 1), steps / 16));
     p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
   }
