@@ -232,19 +232,23 @@ struct PoolTable {
 struct MoveArgs {
   int64_t n_pages, page_stride, page_bytes;
   int Hkv;
-  int pieces;  // of kPiece bytes per page
+  int pieces;  // of piece_bytes(kUnroll) per page
 };
-constexpr int kUnroll = 4;
-constexpr int64_t kPiece = kThreads * kUnroll * 16;
+constexpr int64_t piece_bytes(int unroll) { return (int64_t)kThreads * unroll * 16; }
+// 16-byte loads per thread and piece: 1, 2 or 4, the most that a page has for all threads.
+inline int unroll_of(int64_t page_bytes) {
+  return page_bytes >= piece_bytes(4) ? 4 : page_bytes >= piece_bytes(2) ? 2 : 1;
+}
 
 // Piece w of a page moved from src to dst: w counts pieces, then K and V, then pools.
+template <int kUnroll>
 __device__ __forceinline__ void move_piece(const PoolTable& t, const MoveArgs& a, int64_t src,
                                            int64_t dst, int w) {
   const int piece = w % a.pieces, kv = w / a.pieces & 1, pool = w / a.pieces / 2;
   char* base = kv ? t.v[pool] : t.k[pool];
   const char* s = base + src * a.page_stride;
   char* d = base + dst * a.page_stride;
-  const int64_t at = piece * kPiece + (int64_t)threadIdx.x * 16;
+  const int64_t at = piece * piece_bytes(kUnroll) + (int64_t)threadIdx.x * 16;
   u32x4 x[kUnroll];
   // unconditional loads at offsets clamped into the page, so that all are in flight
 #pragma unroll
@@ -260,6 +264,7 @@ __device__ __forceinline__ void move_piece(const PoolTable& t, const MoveArgs& a
     for (int g = threadIdx.x; g < a.Hkv; g += kThreads) scale[dst * a.Hkv + g] = scale[src * a.Hkv + g];
 }
 
+template <int kUnroll>
 __global__ __launch_bounds__(kThreads) void copy_pages_kernel(PoolTable t, MoveArgs a,
                                                               const int32_t* __restrict__ src,
                                                               const int32_t* __restrict__ dst,
@@ -270,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void copy_pages_kernel(PoolTable t, MoveA
     const int64_t i = w / per_pair;
     const int64_t s = src[i], d = dst[i];
     if (s < 0 || d < 0 || s >= a.n_pages || d >= a.n_pages) continue;
-    move_piece(t, a, s, d, (int)(w % per_pair));
+    move_piece<kUnroll>(t, a, s, d, (int)(w % per_pair));
   }
 }
 
@@ -382,6 +387,7 @@ struct FollowArgs {
   int64_t follow_blocks;  // the grid's first blocks write counts and tables, the others move
 };
 
+template <int kUnroll>
 __global__ __launch_bounds__(kThreads) void compact_move_kernel(PoolTable t, MoveArgs a, PlanArgs pl,
                                                                 FollowArgs f) {
   const int64_t L = pl.head[0], base = pl.head[1];
@@ -405,7 +411,7 @@ __global__ __launch_bounds__(kThreads) void compact_move_kernel(PoolTable t, Mov
   const int64_t total = (L - base) * per_pair;
   for (int64_t w = blockIdx.x - f.follow_blocks; w < total; w += gridDim.x - f.follow_blocks) {
     const int64_t i = w / per_pair;
-    move_piece(t, a, pl.mover[base + i], pl.hole[i], (int)(w % per_pair));
+    move_piece<kUnroll>(t, a, pl.mover[base + i], pl.hole[i], (int)(w % per_pair));
   }
 }
 
@@ -427,7 +433,7 @@ ckv_status check_pools(const ckv_page_pool* pools, int32_t n_pools, MoveArgs& a)
   a.page_stride = page_stride_bytes(&pools[0]);
   a.page_bytes = page_bytes_of(&pools[0]);
   a.Hkv = pools[0].n_kv_heads;
-  a.pieces = (int)ceil_div(a.page_bytes, kPiece);
+  a.pieces = (int)ceil_div(a.page_bytes, piece_bytes(unroll_of(a.page_bytes)));
   return CKV_OK;
 }
 
@@ -441,9 +447,9 @@ void fill_table(PoolTable& t, const ckv_page_pool* pools, int n) {
   }
 }
 
-// Workgroups that a mover takes at most: enough for every CU's 8, whose loads then
-// cover the memory's latency.
-constexpr int64_t kMoveBlocks = 2048;
+// Workgroups that a mover takes at most: four rounds of every CU's 8, so that the last
+// ones spread (one round: 181 us where this took 176, half a round: 191).
+constexpr int64_t kMoveBlocks = 8192;
 
 struct PlanLayout {
   size_t counts, rank, hole, mover, mover_refs, head, bytes;
@@ -537,7 +543,9 @@ ckv_status ckv_page_copy(const ckv_page_pool* pools, int32_t n_pools, const int3
     PoolTable t;
     fill_table(t, pools + p0, std::min(kMaxPools, n_pools - p0));
     const int64_t work = count * a.pieces * 2 * t.n;
-    hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)std::min(work, kMoveBlocks)), dim3(kThreads),
+    const int u = unroll_of(a.page_bytes);
+    const auto kernel = u == 4 ? copy_pages_kernel<4> : u == 2 ? copy_pages_kernel<2> : copy_pages_kernel<1>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(work, kMoveBlocks)), dim3(kThreads),
                        0, (hipStream_t)stream, t, a, src, dst, count);
     CKV_HIP(hipGetLastError());
   }
@@ -590,7 +598,9 @@ ckv_status ckv_page_compact(const ckv_page_pool* pools, int32_t n_pools, const i
     const int64_t work = n_pages / 2 * a.pieces * 2 * t.n;
     const unsigned grid = (unsigned)(f.follow_blocks + std::min(work, kMoveBlocks));
     if (grid == 0) continue;
-    hipLaunchKernelGGL(compact_move_kernel, dim3(grid), dim3(kThreads), 0, st, t, a, pl, f);
+    const int u = unroll_of(a.page_bytes);
+    const auto kernel = u == 4 ? compact_move_kernel<4> : u == 2 ? compact_move_kernel<2> : compact_move_kernel<1>;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, st, t, a, pl, f);
     CKV_HIP(hipGetLastError());
   }
   return CKV_OK;

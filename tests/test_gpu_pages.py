@@ -39,6 +39,13 @@ ATTN = [
     ("f32", HF, 8, [(50, 333), (20, 20)], 0, 0),
     ("f32", (4, 2, 64), 32, [(96, 1000), (0, 5), (33, 64)], 128, 4),
     ("f32", HF, 96, [(1, 6000)], 0, 0),
+    ("bf16", (48, 1, 128), 32, [(1, 700), (1, 1), (2, 90)], 0, 0),      # one KV head for 48, 16 and 20
+    ("e4m3", (16, 1, 128), 16, [(1, 700), (2, 90)], 100, 4),
+    ("bf16", (20, 1, 64), 8, [(1, 333), (1, 64)], 0, 0),
+    ("f32", (20, 1, 64), 8, [(1, 333), (3, 64)], 0, 0),
+    ("e4m3", (5, 5, 64), 16, [(130, 200), (1, 7)], 40, 0),              # KV heads that 8 does not divide
+    ("bf16", (12, 6, 128), 32, [(150, 3000)], 0, 0),
+    ("e4m3", (7, 7, 128), 8, [(140, 2000)], 700, 9),
 ]
 
 
