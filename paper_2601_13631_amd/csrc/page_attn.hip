@@ -132,6 +132,15 @@ __device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
   return __builtin_bit_cast(uint32_t, b);
 }
 
+// l plus both numbers of a packed pair.  A row's sum takes its numerators as they are
+// rounded for the product with V, so that a key that outweighs the others keeps its exact
+// weight (500 tokens on 4,000: 2.34e-3 -> 2.22e-3 off 64 bits, 1.66e-3 of it the output's
+// own rounding; the product with ones also takes one instruction in place of two).
+__device__ __forceinline__ float add_pair(uint32_t pair, float l) {
+  const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), ones, l, false);
+}
+
 // 8 codes (two dwords) as bf16, each times the scale.
 __device__ __forceinline__ bf16x8 bf16_of_codes(uint32_t w0, uint32_t w1, float scale) {
   u32x4 r;
@@ -411,7 +420,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           s[i][y] = __builtin_amdgcn_exp2f(s[i][y] - ref);
-          l += s[i][y];
+          if constexpr (kF32) l += s[i][y];
         }
       if constexpr (kF32) {
 #pragma unroll
@@ -424,7 +433,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
       } else {
         u32x4 pb;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pb[i] = bf16_pair(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
+        for (int i = 0; i < 4; ++i) {
+          pb[i] = bf16_pair(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
+          l = add_pair(pb[i], l);
+        }
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           u32x4 vt;  // element e of the 8 keys
@@ -543,14 +555,37 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
   }
 }
 
+// numerator_step (attn_tile.h), but the row's sum takes the numerators as rounded.
+template <int E, int i>
+__device__ __forceinline__ void rounded_step(f32x16& s, float c1, float m, float (&l)[2], u32x4 (&pb)[2]) {
+  constexpr int kGroups = 16 / E;
+  if constexpr (i < 0 || i > kGroups + 1) return;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (i < kGroups) s[E * i + e] = fmaf(s[E * i + e], c1, -m);
+    if (i >= 1 && i <= kGroups) s[E * (i - 1) + e] = __builtin_amdgcn_exp2f(s[E * (i - 1) + e]);
+    const int v = E * (i - 2) + e;
+    if (i < 2 || i > kGroups + 1) continue;
+    if (v & 1) {
+      uint32_t w = bf16_pair(s[v - 1], s[v]);
+      asm volatile("" : "+v"(w));
+      float& sum = l[v >> 1 & 1];
+      sum = add_pair(w, sum);
+      asm volatile("" : "+v"(sum));
+      pb[v >> 3][(v & 7) >> 1] = w;
+    }
+  }
+}
+
 // Many rows: a workgroup owns 128 query rows (4 waves x 32) of one KV head and one split
 // of their 64-key stages; K and V go through LDS as bf16, two stages of buffers:
 //   S^T = K Q^T   MFMA 32x32x16 in two halves of 32 keys: a lane owns one row, 16 keys
 //   O^T += V^T P^T  V^T by transposing LDS reads, P^T from the softmax registers
 // bf16 rows go from memory straight to LDS, a page per load (8 keys of a stage lie in
 // one page).  8-bit rows come through registers, a stage further ahead, and are written
-// as bf16.  A row's reference is the ceiling of its maximum at some time before: where it is
-// followed the scaling is a power of two, so that numerators already rounded lose nothing.
+// as bf16.  A row's reference is the maximum of the first keys that it sees; where it is
+// followed later it moves by whole log2 units, so that numerators already rounded are scaled
+// by a power of two and lose nothing.
 template <int D, int T>
 __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   using namespace tile;
@@ -733,7 +768,8 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
     float mx = max16(s) * a.c1;
     if (!__any(mx > ref + kSlack)) return;
     mx = fmaxf(mx, partner_f(mx));
-    const float to = fmaxf(ceilf(mx), ref), by = ref - to, f = __builtin_amdgcn_exp2f(by);
+    const float to = ref == kNone ? fmaxf(mx, kNone) : ref + fmaxf(ceilf(mx - ref), 0.f);
+    const float by = ref - to, f = __builtin_amdgcn_exp2f(by);
     ref = to;
     l[0] *= f;
     l[1] *= f;
@@ -833,7 +869,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           constexpr int kk = i / (D / 32), db = i % (D / 32);
           va[kk][db] = read_v<D>(lv, vo, 0, kk, db);
           s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[i], qf[i], s1, 0, 0, 0);
-          numerator_step<kE, i>(s0, a.c1, ref, l, p0b);
+          rounded_step<kE, i>(s0, a.c1, ref, l, p0b);
           __builtin_amdgcn_sched_barrier(0);
         });
         if (edge) mask(st, 1, there, up, low, s1);
@@ -842,10 +878,10 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
           constexpr int kk = i / (D / 32), db = i % (D / 32);
           vb[kk][db] = read_v<D>(lv, vo, 1, kk, db);
-          if constexpr (i < 2) numerator_step<kE, kG + i>(s0, a.c1, ref, l, p0b);
+          if constexpr (i < 2) rounded_step<kE, kG + i>(s0, a.c1, ref, l, p0b);
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[kk][db], __builtin_bit_cast(bf16x8, p0b[kk]),
                                                           o[db], 0, 0, 0);
-          numerator_step<kE, i>(s1, a.c1, ref, l, p1b);
+          rounded_step<kE, i>(s1, a.c1, ref, l, p1b);
           __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (kE4) {  // the next stage's rows are written; loads stay in flight
@@ -860,7 +896,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
           constexpr int kk = i / (D / 32), db = i % (D / 32);
           ka[i] = read_k<D>(nk, ko, 0, i);  // (after the last stage: read and not used)
-          if constexpr (i < 2) numerator_step<kE, kG + i>(s1, a.c1, ref, l, p1b);
+          if constexpr (i < 2) rounded_step<kE, kG + i>(s1, a.c1, ref, l, p1b);
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[kk][db], __builtin_bit_cast(bf16x8, p1b[kk]),
                                                           o[db], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);

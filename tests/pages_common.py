@@ -221,12 +221,12 @@ def attend(pool, batch, q, window=0, sinks=0, sm=0.0, rows_after=0, out=None, st
 
 def check_attention(c: Cache, got: torch.Tensor, window=0, sinks=0, sm=None):
     """Element by element.  With u the unit roundoff of bf16 (2^-8) and a the row's attention
-    over |V|, bf16 and 8-bit pages give at most u |o| (the output's rounding) + u a (the
-    numerators', whose sum is not rounded) + 2^-11 a for fp32's share (logits, exponentials,
-    sums; below 2^-12 up to 60,000 keys of the sizes used here).  Wide products of many rows keep
-    their partials in half precision: u a / 8 more.  fp32 pages: logits over d + 3 roundings
-    of 2^-24 of the sum of |q k| that an exponential carries on, and sums over the keys, n
-    roundings at worst, on numerators and outputs both."""
+    over |V|, bf16 and 8-bit pages give at most u |o| (the output's rounding) + u (a + |o|) (the
+    numerators', p (1 + e) with |e| <= u in the product with V and in their sum alike: sum p e
+    (v - o) / sum p, to first order) + 2^-11 a for that product's second order and fp32's share
+    (logits, exponentials, sums; below 2^-12 up to 60,000 keys of the sizes used here).
+    fp32 pages: logits over d + 3 roundings of 2^-24 of the sum of |q k| that an exponential
+    carries on, and sums over the keys, n roundings at worst, on numerators and outputs both."""
     ref, a, logit = c.attention(window, sinks, sm)
     err = np.abs(got.cpu().double().numpy()[:c.tokens] - ref)
     if c.cache == "f32":
@@ -234,7 +234,7 @@ def check_attention(c: Cache, got: torch.Tensor, window=0, sinks=0, sm=None):
         bound = a * (2 * (c.d + 3) * 2.0 ** -24 * logit + 2 * n * 2.0 ** -24 + 2.0 ** -20) + 1e-30
     else:
         u = 2.0 ** -8
-        bound = u * np.abs(ref) + (u + u / 8 + 2.0 ** -11) * a + 1e-30
+        bound = 2 * u * np.abs(ref) + (u + 2.0 ** -11) * a + 1e-30
     ratio = float((err / bound).max()) if err.size else 0.0
     assert ratio <= 1.0, f"off by {float(err.max()):.3e}, {ratio:.3g} times the bound"
     return ratio
