@@ -14,7 +14,6 @@ namespace {
 
 constexpr int kTile = 32;  // keys per step of a wave
 constexpr int kRows = 16;  // query rows (query x head of one KV head) per workgroup
-constexpr int kWaves = 4;
 constexpr float kNone = -3.4028234663852886e38f;  // reference of a row that has seen no key
 // A row's reference follows its maximum once that is 8 log2 units above it: sums and
 // outputs stay below 2^8 times what the maximum itself would give, and a rescaling
@@ -156,7 +155,7 @@ __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }
 
 // Few rows: a workgroup owns 16 query rows of one KV head and one split of their
-// steps, each wave every fourth step of it:
+// steps, its 4 or 8 waves step by step in turn:
 //   S^T = K Q^T    MFMA 16x16 (bf16: x32, fp32: x4), two groups of 16 keys; lane l
 //                  then holds row l % 16 and keys 4 (l / 16) + 0..3 of each group
 //   O^T += V^T P^T the contraction's 8 (bf16) keys per lane are those it holds, so
@@ -169,8 +168,8 @@ __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f);
 // whole to LDS, a step ahead, into a buffer of the wave's own.  The waves' outputs are
 // joined through LDS, the splits' by page_combine_kernel.
 // kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page).
-template <int D, int T, bool kSmall>
-__global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs a) {
+template <int D, int T, bool kSmall, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(PageAttnArgs a) {
   using E = Elem<T>;
   using QT = typename E::Q;
   constexpr bool kF32 = T == CKV_DTYPE_F32, kE4 = T == CKV_DTYPE_E4M3;
@@ -516,7 +515,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void page_rows_kernel(PageAttnArgs 
     // 16 threads per row, D / 16 elements each
     const int row = threadIdx.x >> 4, col = (threadIdx.x & 15) * kVec;
     const int rr = r_first + row;
-    if (rr <= r_last) {
+    if (row < kRows && rr <= r_last) {
       float M = kNone, L = 0.f, f[kWaves], acc[kVec];
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) M = fmaxf(M, joined.ml[w][row].x);
@@ -1136,8 +1135,13 @@ ckv_status launch_page_attn(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t 
   } else {
     const int64_t wgs = (int64_t)align_up((size_t)a.s.n_seqs * a.n_splits, 8) * a.Hkv;
     if (wgs >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
-    const auto kernel = a.c == 8 ? page_rows_kernel<D, T, true> : page_rows_kernel<D, T, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)p.row_blocks), dim3(64 * kWaves), 0, st, a);
+    // A launch of at most a workgroup per CU has 8 waves in each, whose fewer steps follow
+    // one another (16 sequences of 4 tokens: 13.1 -> 11.7 us, fp32 prompts 8.7 -> 8.0); where
+    // there are more, 4 (48 sequences: 80 us, with 8: 94).
+    const bool eight = wgs * p.row_blocks <= 256;
+    const auto kernel = a.c == 8 ? (eight ? page_rows_kernel<D, T, true, 8> : page_rows_kernel<D, T, true, 4>)
+                                 : (eight ? page_rows_kernel<D, T, false, 8> : page_rows_kernel<D, T, false, 4>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)p.row_blocks), dim3(eight ? 512 : 256), 0, st, a);
   }
   CKV_HIP(hipGetLastError());
   if (a.n_splits > 1) {
