@@ -702,7 +702,7 @@ ckv_status ckv_page_copy(const ckv_page_pool* pools, int32_t n_pools, const int3
  *                     [0, n_pages) stays as it is; may be the same array
  *   n_live            device, int32[1]: L (written)
  *   ws                device workspace of ckv_page_compact_workspace_bytes(n_pages)
- * n_entries = 0 (table NULL) and n_pools = 0 are allowed. */
+ * n_pages <= 2^26.  n_entries = 0 (table NULL) and n_pools = 0 are allowed. */
 size_t ckv_page_compact_workspace_bytes(int64_t n_pages);
 ckv_status ckv_page_compact(const ckv_page_pool* pools, int32_t n_pools, const int32_t* refs,
                             int32_t* refs_out, int64_t n_pages, const int32_t* table,

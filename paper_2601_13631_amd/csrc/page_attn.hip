@@ -638,16 +638,20 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   }
   if (stream >= streams || blk >= a.n_blocks) return;
   const int g = (int)(stream % a.Hkv), split = (int)(stream / a.Hkv);
-  int64_t rb = a.n_blocks - 1 - blk;
-  SeqSpan sp{};
-  const int b = find_part(
-      a.s, [&](const SeqSpan& q) { return (q.count * a.G + kBlockRows - 1) / kBlockRows; }, rb, sp);
+  // n tokens of a sequence are ceil(n G / 128) blocks: numbered from floor(t G / 128) + 1 per
+  // sequence before, t its first token
+  const auto block_start = [&](int q) { return token_of(a.s, q) * a.G / kBlockRows + q; };
+  const int64_t block = a.n_blocks - 1 - blk;
+  const int b = find_seq(a.s, block, block_start);
   if (b < 0) return;
+  const SeqSpan sp = seq_span(a.s, b);
+  const int rb = (int)(block - block_start(b));
+  if ((int64_t)rb * kBlockRows >= (int64_t)sp.count * a.G) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t* tab = a.s.table + (int64_t)b * a.s.table_stride;
   const int kv_end = (int)min<int64_t>(max(sp.len, 0), (int64_t)a.s.max_pages * a.c);
-  const int rows = sp.count * a.G, r_first = (int)rb * kBlockRows, r_last = min(rows, r_first + kBlockRows) - 1;
+  const int rows = sp.count * a.G, r_first = rb * kBlockRows, r_last = min(rows, r_first + kBlockRows) - 1;
   const int p_base = sp.len - sp.count;
   const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
   const int all_steps = (groups_of(a, p_base, p_base + sp.count - 1, kv_end).n + 7) / 8;

@@ -76,7 +76,16 @@ struct AppendArgs {
   int64_t page_stride;  // bytes
   int64_t n_pages;
   int c, Hkv, row_bytes;  // of a pool row (all heads)
+  int by_token;           // numbering of the pages written to, see append_start
 };
+
+// Pages that the call writes to, as find_seq numbers them: n tokens of a sequence lie in at
+// most min(n, n / c + 2) pages, so either from its first token's number on, or from that
+// number / c + 2 per sequence before; the host takes the one with the lower end.
+__device__ __forceinline__ int64_t append_start(const AppendArgs& a, int b) {
+  const int64_t t = token_of(a.s, b);
+  return a.by_token ? t : t / a.c + 2 * (int64_t)b;
+}
 
 // The sequence whose rows hold token t: the last b with tok_off[b] <= t (those
 // before it that are empty share its offset); -1 if it is in none.
@@ -131,24 +140,16 @@ __device__ __forceinline__ uint32_t codes2(float x, float y) {
 // scale, rounds the page's older rows again if that rose, and writes the new rows.
 // Lanes hold 8 elements each, D / 8 lanes per row.
 //
-// The pages of the batch are numbered sequence by sequence, page slots in order.
 template <int D>
 __global__ __launch_bounds__(64) void append_e4m3_kernel(AppendArgs a) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes;
   const int lane = threadIdx.x, g = blockIdx.y;
-  int64_t want = blockIdx.x;
-  SeqSpan sp{};
-  const int b = find_part(
-      a.s,
-      [&](const SeqSpan& q) {  // pages that its tokens lie in
-        const int64_t start = max<int64_t>((int64_t)q.len - q.count, 0), end = q.len;
-        return end > start ? (int)((end - 1) / a.c - start / a.c) + 1 : 0;
-      },
-      want, sp);
-  if (b < 0) return;  // more waves than pages
+  const int b = find_seq(a.s, blockIdx.x, [&](int q) { return append_start(a, q); });
+  if (b < 0) return;
+  const SeqSpan sp = seq_span(a.s, b);
   const int64_t start = (int64_t)sp.len - sp.count;  // position of the call's first token
-  const int64_t slot = max<int64_t>(start, 0) / a.c + want;
-  if (slot >= a.s.max_pages) return;
+  const int64_t slot = max<int64_t>(start, 0) / a.c + ((int64_t)blockIdx.x - append_start(a, b));
+  if (sp.count == 0 || slot * a.c >= sp.len || slot >= a.s.max_pages) return;
   const int page = a.s.table[(int64_t)b * a.s.table_stride + slot];
   if (page < 0 || page >= a.n_pages) return;
 
@@ -516,8 +517,9 @@ ckv_status ckv_page_append(const ckv_page_pool* pool, const ckv_page_batch* batc
   a.row_bytes = pool->n_kv_heads * pool->head_dim * page_elem_bytes(pool->dtype);
   const hipStream_t st = (hipStream_t)stream;
   if (pool->dtype == CKV_DTYPE_E4M3) {
-    // n tokens of one sequence touch at most min(n, (n - 1) / c + 2) pages
-    const int64_t waves = std::min(batch->n_tokens, batch->n_tokens / a.c + 2 * (int64_t)batch->n_seqs);
+    const int64_t by_page = batch->n_tokens / a.c + 2 * (int64_t)batch->n_seqs;
+    a.by_token = batch->n_tokens <= by_page ? 1 : 0;
+    const int64_t waves = std::min(batch->n_tokens, by_page);
     if (waves >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "too many rows in one call");
     const dim3 grid((unsigned)waves, (unsigned)a.Hkv, 2);
     if (pool->head_dim == 128)
@@ -568,6 +570,8 @@ ckv_status ckv_page_compact(const ckv_page_pool* pools, int32_t n_pools, const i
   CKV_CHECK(check_pools(pools, n_pools, a));
   CKV_REQUIRE(n_pages >= 1 && n_pages <= INT32_MAX, "n_pages must be in [1, 2^31-1] (got %lld)",
               (long long)n_pages);
+  // (its plan goes over the blocks' counts from every block)
+  if (n_pages > (int64_t(1) << 26)) CKV_FAIL(CKV_EUNSUPPORTED, "more than 2^26 pages to compact");
   CKV_REQUIRE(n_pools == 0 || n_pages == a.n_pages, "the pools hold %lld pages, not %lld",
               (long long)a.n_pages, (long long)n_pages);
   CKV_REQUIRE(n_entries >= 0, "n_entries must be >= 0 (got %lld)", (long long)n_entries);

@@ -44,43 +44,34 @@ struct SeqSpan {
   int32_t count, len;
 };
 __device__ __forceinline__ SeqSpan seq_span(const PageSeqs& s, int b) {
-  const int64_t n = min<int64_t>(s.n_tokens, INT32_MAX);
-  const int64_t lo = min<int64_t>(max(s.tok_off[b], 0), n), hi = min<int64_t>(max(s.tok_off[b + 1], 0), n);
+  const int64_t lo = min<int64_t>(max(s.tok_off[b], 0), s.n_tokens);
+  const int64_t hi = min<int64_t>(max(s.tok_off[b + 1], 0), s.n_tokens);
   return SeqSpan{lo, (int32_t)max<int64_t>(hi - lo, 0), s.lens[b]};
 }
 
-// Work that the sequences have in parts, parts(span) of them each, numbered sequence by
-// sequence: the sequence b of part `want`, its span, and the part's number inside it (in
-// want).  b = -1 past the last part.  A whole wave calls it: 64 sequences at a time, by a
-// running sum over the lanes.
+// The last sequence b with start(b) <= k, -1 if there is none; start must not fall.  A whole
+// wave calls it: 64 sequences are looked at at a time (one round of loads for 64 of them, two
+// for 4,096).
+// Work that the sequences have in parts is numbered so: sequence b's parts from start(b) on,
+// where start(b + 1) - start(b) is at least their number and follows from the offsets alone;
+// a number past a sequence's last part has no work.
 template <class F>
-__device__ __forceinline__ int find_part(const PageSeqs& s, F&& parts, int64_t& want, SeqSpan& span) {
+__device__ __forceinline__ int find_seq(const PageSeqs& s, int64_t k, F&& start) {
   const int lane = threadIdx.x & 63;
-  for (int b0 = 0; b0 < s.n_seqs; b0 += 64) {
-    SeqSpan mine{0, 0, 0};
-    int n = 0;
-    if (b0 + lane < s.n_seqs) {
-      mine = seq_span(s, b0 + lane);
-      if (mine.count > 0) n = parts(mine);
-    }
-    int sum = n;  // up to this lane
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const int y = __shfl_up(sum, x);
-      if (lane >= x) sum += y;
-    }
-    const uint64_t past = __ballot((int64_t)sum > want);
-    if (past) {
-      const int at = __builtin_ctzll(past);
-      want -= __builtin_amdgcn_readlane(sum - n, at);
-      span.first = (int64_t)__builtin_amdgcn_readlane((int)mine.first, at);  // (below 2^31)
-      span.count = __builtin_amdgcn_readlane(mine.count, at);
-      span.len = __builtin_amdgcn_readlane(mine.len, at);
-      return b0 + at;
-    }
-    want -= __builtin_amdgcn_readlane(sum, 63);
-  }
-  return -1;
+  int lo = 0, n = s.n_seqs;
+  do {
+    const int step = (n + 63) / 64;
+    const uint64_t at_most = __ballot(lane * step < n && start(lo + min(lane * step, n - 1)) <= k);
+    if (!at_most) return -1;
+    const int at = (63 - __builtin_clzll(at_most)) * step;
+    lo += at;
+    n = min(step, n - at);
+  } while (n > 1);
+  return lo;
+}
+// tok_off[b] inside the token tensors.
+__device__ __forceinline__ int64_t token_of(const PageSeqs& s, int b) {
+  return min<int64_t>(max(s.tok_off[b], 0), s.n_tokens);
 }
 
 // The scale of an E4M3 page from its byte: 2^(e - 127), finite whatever the byte (a page

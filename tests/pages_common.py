@@ -79,16 +79,19 @@ class Cache:
             x = x * np.ldexp(1.0, self.scale[n].numpy().astype(int) - 127)[:, None, :, None]
         return x
 
-    def rows(self, n, b):
-        """Sequence b's rows of K or V in order, and whether each is there."""
-        x, page = self.values(n), self.page
+    def there(self, b):
+        """Whether each position of sequence b's table has a page."""
         t = self.table[b]
-        ok = (t >= 0) & (t < self.n_pages)
-        return x[np.where(ok, t, 0)].reshape(-1, self.hkv, self.d), np.repeat(ok, page)
+        return np.repeat((t >= 0) & (t < self.n_pages), self.page)
+
+    def rows(self, x, b):
+        """Sequence b's rows of x [n_pages, page, hkv, d] in order (of page 0 where there is none)."""
+        t = self.table[b]
+        return x[np.where((t >= 0) & (t < self.n_pages), t, 0)].reshape(-1, self.hkv, self.d)
 
     def sees(self, b, window, sinks):
         """[new, width * page]: which position each query sees."""
-        _, there = self.rows("k", b)
+        there = self.there(b)
         n, m = self.seqs[b]
         p = np.arange(m - n, m)[:, None]
         j = np.arange(there.size)[None]
@@ -104,11 +107,12 @@ class Cache:
         out = np.zeros((self.tokens, self.hq, self.d))
         size, logit = np.zeros_like(out), 0.0
         q = self.q.double().numpy()
+        every = [np.nan_to_num(self.values(n)) for n in "kv"]
         for b in range(len(self.seqs)):
             see = self.sees(b, window, sinks)
             if see.size == 0:
                 continue
-            k, v = (np.nan_to_num(self.rows(n, b)[0]) for n in "kv")
+            k, v = (self.rows(x, b) for x in every)
             for h in range(self.hq):
                 kk, vv = k[:, h // G], v[:, h // G]
                 qq = q[self.off[b]:self.off[b + 1], h]

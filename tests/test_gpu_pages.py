@@ -146,6 +146,44 @@ def test_attention_random(seed):
     assert torch.equal(out, attend(pool, batch, c.q.to(DEV), window, sinks, rows_after=after))  # bit for bit
 
 
+@pytest.mark.parametrize("cache,heads,n,most", [("e4m3", (1, 1, 64), 5000, 3), ("bf16", (40, 1, 64), 130, 2),
+                                                ("e4m3", (40, 2, 128), 65, 9), ("bf16", (1, 1, 128), 64, 1),
+                                                ("e4m3", (36, 1, 64), 700, 1)])
+def test_many_sequences(cache, heads, n, most):
+    """More sequences than a wave has lanes, some with no token; what each is found by."""
+    import paper_2601_13631_amd as ckv
+    rng = np.random.default_rng(n)
+    seqs = [(int(rng.integers(0, most + 1)), int(rng.integers(0, 20))) for _ in range(n)]
+    seqs = [(a, a + b) for a, b in seqs]
+    c = Cache(cache, heads, 8, seqs, seed=n)
+    pool, batch = c.device()
+    ckv.page_append(pool, batch, c.new_rows["k"].to(DEV), c.new_rows["v"].to(DEV))
+    c.append()
+    check_pages(c, pool.k, pool.v, pool.k_scale, pool.v_scale)
+    check_attention(c, attend(pool, batch, c.q.to(DEV)))
+
+
+def test_offsets_that_do_not_start_at_0():
+    """Rows before the first sequence and behind the last belong to none."""
+    import paper_2601_13631_amd as ckv
+    for cache, heads in (("bf16", H7), ("e4m3", H7), ("f32", HF)):
+        for new in (1, 45):
+            c = Cache(cache, heads, 16, [(new, 200), (0, 20), (new, 90)], seed=3)
+            pool, _ = c.device()
+            lead, tail = 37, 5
+            off = torch.from_numpy(c.off + lead).to(DEV)
+            batch = ckv.PageBatch(torch.from_numpy(c.table).to(DEV), torch.from_numpy(c.lens).to(DEV), off,
+                                  lead + c.tokens + tail, max_tokens=new)
+            pad = lambda t: torch.cat([torch.full_like(t[:1], 9.0).repeat(lead, 1, 1), t,  # noqa: E731
+                                       torch.full_like(t[:1], 9.0).repeat(tail, 1, 1)]).to(DEV)
+            ckv.page_append(pool, batch, pad(c.new_rows["k"]), pad(c.new_rows["v"]))
+            c.append()
+            check_pages(c, pool.k, pool.v, pool.k_scale, pool.v_scale)
+            out = attend(pool, batch, pad(c.q))
+            assert (out[:lead] == 7).all() and (out[lead + c.tokens:] == 7).all()
+            check_attention(c, out[lead:])
+
+
 def test_lengths_past_the_table():
     """A sequence longer than its table: its queries see what the table holds."""
     import paper_2601_13631_amd as ckv

@@ -117,6 +117,7 @@ def test_bad_moves():
     for over in (dict(n=99), dict(n=0), dict(refs=None), dict(out=None), dict(table=None), dict(table_out=None),
                  dict(entries=-1), dict(live=None), dict(ws=None), dict(ws=P + 4), dict(ws_bytes=need - 1)):
         assert compact(**over) == ckv.EINVAL and ckv.last_error()
+    assert ckv._lib.ckv_page_compact(None, 0, P, P, (1 << 26) + 1, None, None, 0, P, P, 1 << 40, None) == ckv.EUNSUPPORTED
 
 
 def test_handles_refuse_host_tensors():
