@@ -473,15 +473,16 @@ class Store:
 
 def _need(t, what: str, dtype, shape=None):
     """``t`` if it is a contiguous tensor of the current HIP device, of this type and shape."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if (t.dtype is dtype and t.get_device() == torch.cuda.current_device() and (shape is None or t.shape == shape)
+            and t.is_contiguous()):
+        return t
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{what} must be on the current device (it is on {t.device})")
     if t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype} (it is {t.dtype})")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)} (it has {tuple(t.shape)})")
-    if not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    return t
+    raise ValueError(f"{what} must be contiguous")
 
 
 def _int32(x, what: str) -> int:
