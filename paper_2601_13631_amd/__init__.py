@@ -485,6 +485,22 @@ def _need(t, what: str, dtype, shape=None):
     raise ValueError(f"{what} must be contiguous")
 
 
+def _together(t, *handles) -> None:
+    """Raises unless the handles' tensors are on the device of ``t`` (the current one)."""
+    for h in handles:
+        if h._device != t.get_device():
+            raise ValueError(f"the {type(h).__name__} is on device {h._device}, the call's tensors on {t.get_device()}")
+
+
+def _workspace(ws, t):
+    """Address and bytes of a workspace, on the device of ``t``."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != t.get_device() or not ws.is_contiguous():
+        raise ValueError(f"the workspace must be contiguous and on the call's device (it is on {ws.device})")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _int32(x, what: str) -> int:
     """``x`` as a C int that is not negative."""
     if not 0 <= x < 1 << 31:
@@ -523,6 +539,7 @@ class PagePool:
                 _need(t, "a scale tensor", torch.uint8, (n_pages, hkv))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = n_pages, page_size, hkv, d
+        self._device = k.get_device()
         self.token_dtype = torch.float32 if k.dtype == torch.float32 else torch.bfloat16
         self._c = _PagePool(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages,
                             k.stride(0) if n_pages > 1 else 0, page_size, hkv, d, _PAGE_DTYPES[k.dtype])
@@ -535,6 +552,9 @@ class PageLayers:
     def __init__(self, pools):
         self.pools = tuple(pools)
         self.n_pages = self.pools[0].n_pages if self.pools else 0
+        self._device = self.pools[0]._device if self.pools else None
+        if any(p._device != self._device for p in self.pools):
+            raise ValueError("the pools must be on one device")
         self._c = (_PagePool * len(self.pools))(*(p._c for p in self.pools))
 
 
@@ -562,6 +582,7 @@ class PageBatch:
         _int32(n_tokens, "n_tokens")
         self.table, self.lens, self.tok_off = table, lens, tok_off
         self.n_seqs, self.n_tokens = n_seqs, int(n_tokens)
+        self._device = table.get_device()
         self._c = _PageBatch(_ptr(table), _ptr(lens), _ptr(tok_off), stride, n_tokens, n_seqs, width,
                              _int32(max_tokens, "max_tokens"), _int32(max_len, "max_len"))
 
@@ -572,6 +593,7 @@ def page_append(pool: PagePool, batch: PageBatch, k_new, v_new, stream=None) -> 
     shape = (batch.n_tokens, pool.n_kv_heads, pool.head_dim)
     _need(k_new, "k_new", pool.token_dtype, shape)
     _need(v_new, "v_new", pool.token_dtype, shape)
+    _together(k_new, pool, batch)
     _check(_lib.ckv_page_append(pool._c, batch._c, k_new.data_ptr(), v_new.data_ptr(), _stream(stream)),
            "ckv_page_append")
 
@@ -594,9 +616,10 @@ def page_attn(pool: PagePool, batch: PageBatch, q, out, ws=None, window: int = 0
         raise ValueError("q must be [n_tokens, n_q_heads, head_dim]")
     _need(q, "q", pool.token_dtype)
     _need(out, "out", pool.token_dtype, q.shape)
-    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _together(q, pool, batch)
+    ws_ptr, nbytes = _workspace(ws, q)
     _check(_lib.ckv_page_attn(pool._c, batch._c, q.data_ptr(), q.shape[1], sm_scale,
-                              _int32(window, "window"), _int32(n_sinks, "n_sinks"), out.data_ptr(), _ptr(ws),
+                              _int32(window, "window"), _int32(n_sinks, "n_sinks"), out.data_ptr(), ws_ptr,
                               nbytes, _stream(stream)), "ckv_page_attn")
 
 
@@ -605,6 +628,8 @@ def page_copy(layers: PageLayers, src, dst, stream=None) -> None:
     every layer."""
     _need(src, "src", torch.int32)
     _need(dst, "dst", torch.int32, src.shape)
+    if layers.pools:
+        _together(src, layers)
     _check(_lib.ckv_page_copy(layers._c, len(layers.pools), src.data_ptr(), dst.data_ptr(), src.numel(),
                               _stream(stream)), "ckv_page_copy")
 
@@ -624,7 +649,10 @@ def page_compact(layers: PageLayers, refs, refs_out, table, table_out, n_live, w
     if table is not None:
         _need(table, "table", torch.int32)
         _need(table_out, "table_out", torch.int32, table.shape)
+    if layers.pools:
+        _together(refs, layers)
+    ws_ptr, nbytes = _workspace(ws, refs)
     _check(_lib.ckv_page_compact(layers._c, len(layers.pools), refs.data_ptr(), refs_out.data_ptr(),
                                  refs.numel(), _ptr(table), _ptr(table_out) if table is not None else None,
-                                 table.numel() if table is not None else 0, n_live.data_ptr(), _ptr(ws),
-                                 ws.numel() * ws.element_size(), _stream(stream)), "ckv_page_compact")
+                                 table.numel() if table is not None else 0, n_live.data_ptr(), ws_ptr,
+                                 nbytes, _stream(stream)), "ckv_page_compact")

@@ -585,3 +585,42 @@ def test_wrappers_refuse():
         ckv.page_copy(ckv.PageLayers([pool]), i, i[:2])
     with pytest.raises(ValueError):
         ckv.page_copy(ckv.PageLayers([pool]), i.long(), i)
+
+
+def test_wrappers_refuse_other_devices():
+    """Handles made on another device than the call's (a device number that none has stands for it),
+    and workspaces elsewhere or not contiguous."""
+    import paper_2601_13631_amd as ckv
+    c = Cache("bf16", H7, 16, [(3, 9000)], seed=0)
+    q, i = c.q.to(DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    rows = [c.new_rows[n].to(DEV) for n in "kv"]
+    for which in range(2):
+        made = c.device()
+        layers = ckv.PageLayers([made[0]])
+        n = ckv.page_attn_workspace_bytes(*made, 28)
+        assert n > 0
+        ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+        made[which]._device = layers._device = 77
+        with pytest.raises(ValueError, match="on device 77"):
+            ckv.page_attn(*made, q, torch.empty_like(q), ws)
+        with pytest.raises(ValueError, match="on device 77"):
+            ckv.page_append(*made, *rows)
+        with pytest.raises(ValueError, match="on device 77"):
+            ckv.page_copy(layers, i, i)
+        refs = torch.ones(c.n_pages, dtype=torch.int32, device=DEV)
+        with pytest.raises(ValueError, match="on device 77"):
+            ckv.page_compact(layers, refs, refs, None, None, i[:1], ws)
+        with pytest.raises(ValueError, match="one device"):
+            ckv.PageLayers([c.device()[0], _moved(c)])
+    made = c.device()
+    for bad in (ws.cpu(), ws[:1].expand(n), torch.empty(2 * n, dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            ckv.page_attn(*made, q, torch.empty_like(q), bad)
+        with pytest.raises(ValueError, match="workspace"):
+            ckv.page_compact(ckv.PageLayers([]), i, i, None, None, i[:1], bad)
+
+
+def _moved(c):
+    pool = c.device()[0]
+    pool._device = 77
+    return pool
