@@ -677,22 +677,43 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
     for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const bf16x8*>(q + 16 * i);
   }
 
-  // Table entries of a stage: lane l has that of keys 8 (l % 8) .. + 7.
+  // The pages of 8 stages at a time: lane l has group l of them, its table entry in the 8
+  // stages before, then where it begins in the pool (a missing page: page 0) and its scale
+  // bytes.  A load takes its group's by readlane.
+  const int row_bytes = a.Hkv * D * Elem<T>::kBytes;
+  struct Eight {
+    int next;        // entry of group l of the 8 stages after
+    int64_t of;
+    uint64_t there;  // bit l: group l's page is there
+    uint32_t ks, vs;
+  };
+  auto group_pos = [&](int st) __attribute__((always_inline)) { return groups.pos(min(8 * st + lane, 8 * end - 1)); };
   auto entries = [&](int st) __attribute__((always_inline)) {
-    const int pos = groups.pos(8 * min(st, end - 1) + (lane & 7));
+    const int pos = group_pos(st);
     return entry_of(a, tab, a.log2c >= 0 ? pos >> a.log2c : (int)((uint32_t)pos / (uint32_t)a.c));
   };
-  const int row_bytes = a.Hkv * D * Elem<T>::kBytes;
-  // Where a stage's groups begin in the pool: lane l has group l % 8 (a missing page: page 0).
-  // Found by the lanes at once; a load takes its group's by readlane.
-  auto places = [&](int st, int ent) __attribute__((always_inline)) {
-    const int pos = groups.pos(8 * st + (lane & 7));
-    const int r = a.log2c >= 0 ? pos & (a.c - 1) : (int)((uint32_t)pos % (uint32_t)a.c);
-    return (int64_t)(names_page(a, ent) ? ent : 0) * a.page_stride + (int64_t)r * row_bytes;
+  auto enter = [&](int st, Eight& x) __attribute__((always_inline)) {  // the 8 stages from st on
+    const int pos = group_pos(st), r = a.log2c >= 0 ? pos & (a.c - 1) : (int)((uint32_t)pos % (uint32_t)a.c);
+    const bool ok = names_page(a, x.next);
+    const int page = ok ? x.next : 0;
+    x.of = (int64_t)page * a.page_stride + (int64_t)r * row_bytes;
+    x.there = __ballot(ok);
+    if constexpr (kE4) {
+      x.ks = a.k_scale[(int64_t)page * a.Hkv + g];
+      x.vs = a.v_scale[(int64_t)page * a.Hkv + g];
+    }
+    x.next = entries(st + 8);
   };
-  auto place = [&](int64_t of, int group) __attribute__((always_inline)) {
-    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(of >> 32), group) << 32 |
-                     (uint32_t)__builtin_amdgcn_readlane((int)of, group));
+  // Before a stage's loads, stages in order; gives the bits of its 8 pages.
+  auto at_stage = [&](int st, Eight& x) __attribute__((always_inline)) {
+    const int i = (st - begin) & 7;
+    if (i == 0) enter(st, x);
+    return (uint32_t)(x.there >> (8 * i)) & 0xffu;
+  };
+  auto place = [&](const Eight& x, int st, int group) __attribute__((always_inline)) {
+    const int l = 8 * ((st - begin) & 7) + group;
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x.of >> 32), l) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int)x.of, l));
   };
 
   // bf16: this lane's byte of the rows that a load moves (the LDS permutation undone)
@@ -700,11 +721,11 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   const uint32_t rcol = (uint32_t)(((wave * St::kRowsPerLoad & 7) + lane / St::kSegs) * row_bytes);
   const uint32_t kcol = rcol + (uint32_t)(2 * (g * D + ((lane % St::kSegs ^ k_swz<D>(key0)) << 3)));
   const uint32_t vcol = rcol + (uint32_t)(2 * (g * D + ((lane % St::kSegs ^ v_swz<D>(key0)) << 3)));
-  auto load_direct = [&](int64_t of, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
+  auto load_direct = [&](const Eight& x, int st, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < St::kPer; ++i) {
       const int key = i * St::kKeyStep + wave * St::kRowsPerLoad;
-      const int64_t off = place(of, key >> 3);
+      const int64_t off = place(x, st, key >> 3);
       buffer_to_lds(raw_rsrc(a.k + off, 0xffffffffu), kcol, 0, dk + key * D);
       buffer_to_lds(raw_rsrc(a.v + off, 0xffffffffu), vcol, 0, dv + key * D);
     }
@@ -713,35 +734,33 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   constexpr int kELanes = D / 16, kERows = 64 / kELanes, kLoads = kKeys / (4 * kERows);
   struct Codes {
     u32x4 k[kLoads], v[kLoads];
-    uint32_t ks, vs;  // scale bytes of the stage, as its entries
   };
   const uint32_t ecol = (uint32_t)((lane / kELanes & 7) * row_bytes + g * D + lane % kELanes * 16);
-  auto load_codes = [&](int64_t of, int ent, Codes& x) __attribute__((always_inline)) {
-    ent = names_page(a, ent) ? ent : 0;
-    x.ks = a.k_scale[(int64_t)ent * a.Hkv + g];
-    x.vs = a.v_scale[(int64_t)ent * a.Hkv + g];
+  auto load_codes = [&](const Eight& e, int st, Codes& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int group = (4 * i + wave) * kERows >> 3;
       if constexpr (kERows == 8) {
-        const int64_t off = place(of, group);
+        const int64_t off = place(e, st, group);
         x.k[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(raw_rsrc(a.k + off, 0xffffffffu), ecol, 0, 0));
         x.v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(raw_rsrc(a.v + off, 0xffffffffu), ecol, 0, 0));
       } else {  // (at D = 64 a load has rows of two groups)
-        const int64_t lo = place(of, group), hi = place(of, group + 1), off = (lane >> 5 ? hi : lo) + ecol;
+        const int64_t lo = place(e, st, group), hi = place(e, st, group + 1), off = (lane >> 5 ? hi : lo) + ecol;
         x.k[i] = *reinterpret_cast<const u32x4*>(a.k + off);
         x.v[i] = *reinterpret_cast<const u32x4*>(a.v + off);
       }
     }
   };
   // Piece n < 4 kLoads of a stage's codes as bf16 in LDS: half n % 2 of load n / 4, K then V.
-  auto write_codes = [&](auto n, const Codes& x, uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
+  auto write_codes = [&](auto n, const Eight& e, int st, const Codes& x, uint16_t* dk, uint16_t* dv)
+      __attribute__((always_inline)) {
     constexpr int i = n / 4, kv = n / 2 % 2, h = n % 2;
     const int first = (4 * i + wave) * kERows, key = first + lane / kELanes;
-    const uint32_t bytes = kv ? x.vs : x.ks;
-    uint32_t byte = (uint32_t)__builtin_amdgcn_readlane(bytes, first >> 3);
+    const int l = 8 * ((st - begin) & 7) + (first >> 3);
+    const uint32_t bytes = kv ? e.vs : e.ks;
+    uint32_t byte = (uint32_t)__builtin_amdgcn_readlane(bytes, l);
     if constexpr (kERows == 16) {
-      const uint32_t up = (uint32_t)__builtin_amdgcn_readlane(bytes, (first >> 3) + 1);
+      const uint32_t up = (uint32_t)__builtin_amdgcn_readlane(bytes, l + 1);
       byte = lane >> 5 ? up : byte;
     }
     const int seg = (2 * (lane % kELanes) + h) ^ (kv ? v_swz<D>(key) : k_swz<D>(key));
@@ -767,6 +786,13 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   // (`there`: bit i, the page of the stage's group i), as far as the stage has any.
   // Registers 8 i .. + 7 hold the keys of group 4 sub + 2 i + half.
   const int upper = min(p, kv_end - 1);
+  // Stages all of whose keys every row sees (as far as their pages are there): from `low_end`
+  // on, where the sinks' groups are past and the window holds, `n_clear` of them, the groups
+  // below the first row's position.
+  const int m = max(min(p0 + 1, kv_end), 0) >> 3;
+  const int below = m <= groups.n_sink ? m : groups.n_sink + max(m - groups.first, 0);
+  const int low_end = a.window > 0 ? (max(groups.n_sink, groups.n_sink + ((p1 - a.window) >> 3) - groups.first + 1) + 7) >> 3 : 0;
+  const uint32_t n_clear = (uint32_t)max((below >> 3) - low_end, 0);
   auto mask = [&](int st, int sub, uint32_t there, bool up, bool low, f32x16& s) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -830,16 +856,20 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
     l[0] = l[1] = 0.f;
     ref = kNone;
     if (begin < end) {
-      // entries of the current stage and of the ones after it
-      int ent = entries(begin), ent1 = entries(begin + 1), ent2 = 0;
+      Eight pages;
+      pages.next = entries(begin);
+      // the bits of the current stage's pages and of the next one's
+      uint32_t there = at_stage(begin, pages), there1 = 0xffu;
       Codes codes;
       if constexpr (kE4) {
-        ent2 = entries(begin + 2);
-        load_codes(places(begin, ent), ent, codes);
-        static_for<4 * kLoads>([&](auto n) { write_codes(n, codes, k0, v0); });
-        load_codes(places(min(begin + 1, end - 1), ent1), ent1, codes);
+        load_codes(pages, begin, codes);
+        static_for<4 * kLoads>([&](auto n) { write_codes(n, pages, begin, codes, k0, v0); });
+        if (begin + 1 < end) {
+          there1 = at_stage(begin + 1, pages);
+          load_codes(pages, begin + 1, codes);
+        }
       } else {
-        load_direct(places(begin, ent), k0, v0);
+        load_direct(pages, begin, k0, v0);
       }
       stage_barrier();
       bf16x8 ka[kG];  // K fragments of the current stage's first 32 keys
@@ -850,19 +880,22 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           __attribute__((always_inline)) {
         uint32_t ko = kfo, vo = voff;
         asm volatile("" : "+v"(ko), "+v"(vo));
+        // what some row of the block must not see
+        const bool clear = (uint32_t)(st - low_end) < n_clear && there == 0xffu;
         const int pos0 = groups.pos(8 * st), last = groups.pos(8 * st + 7) + 8;
         const bool sinks = 8 * st < groups.n_sink;  // the first groups are of the sinks
-        // what some row of the block must not see, and which pages are there
-        const uint32_t there = (uint32_t)__ballot(names_page(a, ent)) & 0xffu;
-        const bool up = last > min(p0 + 1, kv_end);
-        const bool low = a.window > 0 && (sinks || pos0 <= p1 - a.window) && last > a.sinks;
+        const bool up = !clear && last > min(p0 + 1, kv_end);
+        const bool low = !clear && a.window > 0 && (sinks || pos0 <= p1 - a.window) && last > a.sinks;
         const bool edge = up || low || there != 0xffu;
         const bool check = edge || st == begin || look;
-        const int after = entries(st + (kE4 ? 3 : 2));
+        uint32_t after = 0xffu;
         if constexpr (!kE4)
-          if (st + 1 < end) load_direct(places(st + 1, ent1), nk, nv);
-        if (there != 0xffu || last > min(p1 + 1, kv_end) ||
-            (a.window > 0 && (sinks || pos0 <= p0 - a.window) && last > a.sinks)) {
+          if (st + 1 < end) {
+            after = at_stage(st + 1, pages);
+            load_direct(pages, st + 1, nk, nv);
+          }
+        if (!clear && (there != 0xffu || last > min(p1 + 1, kv_end) ||
+                       (a.window > 0 && (sinks || pos0 <= p0 - a.window) && last > a.sinks))) {
           // a weight of 0 does not undo a NaN: V rows that no query of the block sees are cleared
           const int key = (int)threadIdx.x >> 2, pos = groups.pos(8 * st + (key >> 3)) + (key & 7);  // four threads a row
           if (!((there >> (key >> 3) & 1) && pos < kv_end && pos <= p1 &&
@@ -885,11 +918,15 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           kb[i] = read_k<D>(lk, ko, 1, i);
           s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[i], qf[i], s0, 0, 0, 0);
           // (kG pieces: the stage after the last one is written as well, and not used)
-          if constexpr (kE4) write_codes(i, codes, nk, nv);
+          if constexpr (kE4) write_codes(i, pages, st + 1, codes, nk, nv);
           __builtin_amdgcn_sched_barrier(0);
         });
         __builtin_amdgcn_s_setprio(1);
-        if constexpr (kE4) load_codes(places(min(st + 2, end - 1), ent2), ent2, codes);
+        if constexpr (kE4)
+          if (st + 2 < end) {
+            after = at_stage(st + 2, pages);
+            load_codes(pages, st + 2, codes);
+          }
         if (edge) mask(st, 0, there, up, low, s0);
         if (check) follow(s0, nullptr, nullptr);
         __builtin_amdgcn_sched_barrier(0);
@@ -929,13 +966,8 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
                                                           o[db], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
         });
-        ent = ent1;
-        if constexpr (kE4) {
-          ent1 = ent2;
-          ent2 = after;
-        } else {
-          ent1 = after;
-        }
+        there = kE4 ? there1 : after;
+        there1 = after;
       };
       for (int st = begin; st < end; st += 2) {
         stage(st, k0, v0, k1, v1);
