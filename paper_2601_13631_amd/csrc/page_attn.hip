@@ -603,11 +603,14 @@ __device__ __forceinline__ void rounded_step(f32x16& s, float c1, float m, float
 // as bf16.  A row's reference is the maximum of the first keys that it sees; where it is
 // followed later it moves by whole log2 units, so that numerators already rounded are scaled
 // by a power of two and lose nothing.
-// Bound by what one wave issues beside its products: 32 MFMAs of 32 cycles a stage, about 170
-// VALU instructions (the exponentials the dearest; 32 conversions more in 8 bits) and 40
-// scalar ones.  Hence no maximum in the loop (a chain from the products to the exponentials),
-// pages found by the lanes for all groups of a stage at once (by scalar code per load: 274
-// us where this took 255), and conversions beside the first run of products.
+// Bound by what the two waves of a SIMD issue beside their products: 32 MFMAs of 33 cycles a
+// stage, three VALU instructions per logit and lane (one an exponential, 8 cycles) and the
+// stage's own work, and the two pipes overlap in part only (two waves with 1 MFMA and 8 FMAs
+// each, in a loop of these: 87 cycles where the MFMAs take 67 and the FMAs 47).  A wave
+// alone issues an instruction in 5 cycles.  Hence no maximum in the loop (a chain from the
+// products to the exponentials), pages found by the lanes for the 64 groups of 8 stages at
+// once (for a stage: 258 us where this took 243), masks and their conditions in the stages
+// that need some only (243 -> 235), and conversions beside the first run of products.
 template <int D, int T>
 __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   using namespace tile;
@@ -781,18 +784,20 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   f32x16 o[D / 32];
   float l[2], ref;
 
+  // Stages all of whose keys every row sees, as far as their pages are there, take no masks:
+  // `n_clear` of them from `clear_from` on, past the sinks' groups, in the window of the last
+  // row and below the position of the first one, but for the split's first stage (in whose
+  // keys the reference is looked for).
+  const int whole_groups = max(min(p0 + 1, kv_end), 0) >> 3;
+  const int below = whole_groups <= groups.n_sink ? whole_groups : groups.n_sink + max(whole_groups - groups.first, 0);
+  const int in_window = a.window > 0 ? max(groups.n_sink, groups.n_sink + ((p1 - a.window) >> 3) - groups.first + 1) : 0;
+  const int clear_from = max((in_window + 7) >> 3, begin + 1), n_clear = max((below >> 3) - clear_from, 0);
+
   // -inf where this lane's row must not see a key of half `sub` of stage st: keys past its
   // own position or the sequence's end, keys before its window, keys of a missing page
   // (`there`: bit i, the page of the stage's group i), as far as the stage has any.
   // Registers 8 i .. + 7 hold the keys of group 4 sub + 2 i + half.
   const int upper = min(p, kv_end - 1);
-  // Stages all of whose keys every row sees (as far as their pages are there): from `low_end`
-  // on, where the sinks' groups are past and the window holds, `n_clear` of them, the groups
-  // below the first row's position.
-  const int m = max(min(p0 + 1, kv_end), 0) >> 3;
-  const int below = m <= groups.n_sink ? m : groups.n_sink + max(m - groups.first, 0);
-  const int low_end = a.window > 0 ? (max(groups.n_sink, groups.n_sink + ((p1 - a.window) >> 3) - groups.first + 1) + 7) >> 3 : 0;
-  const uint32_t n_clear = (uint32_t)max((below >> 3) - low_end, 0);
   auto mask = [&](int st, int sub, uint32_t there, bool up, bool low, f32x16& s) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -880,22 +885,26 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           __attribute__((always_inline)) {
         uint32_t ko = kfo, vo = voff;
         asm volatile("" : "+v"(ko), "+v"(vo));
-        // what some row of the block must not see
-        const bool clear = (uint32_t)(st - low_end) < n_clear && there == 0xffu;
-        const int pos0 = groups.pos(8 * st), last = groups.pos(8 * st + 7) + 8;
-        const bool sinks = 8 * st < groups.n_sink;  // the first groups are of the sinks
-        const bool up = !clear && last > min(p0 + 1, kv_end);
-        const bool low = !clear && a.window > 0 && (sinks || pos0 <= p1 - a.window) && last > a.sinks;
-        const bool edge = up || low || there != 0xffu;
-        const bool check = edge || st == begin || look;
+        // what some row of the block must not see: keys past its position, keys before its
+        // window; and V rows that no row sees
+        const bool clear = (uint32_t)(st - clear_from) < (uint32_t)n_clear && there == 0xffu;
+        bool up = false, low = false, hide = false;
+        if (!clear) {
+          const int pos0 = groups.pos(8 * st), last = groups.pos(8 * st + 7) + 8;
+          const bool sinks = 8 * st < groups.n_sink;  // the first groups are of the sinks
+          up = last > min(p0 + 1, kv_end);
+          low = a.window > 0 && (sinks || pos0 <= p1 - a.window) && last > a.sinks;
+          hide = there != 0xffu || last > min(p1 + 1, kv_end) ||
+                 (a.window > 0 && (sinks || pos0 <= p0 - a.window) && last > a.sinks);
+        }
+        const bool check = !clear || look;
         uint32_t after = 0xffu;
         if constexpr (!kE4)
           if (st + 1 < end) {
             after = at_stage(st + 1, pages);
             load_direct(pages, st + 1, nk, nv);
           }
-        if (!clear && (there != 0xffu || last > min(p1 + 1, kv_end) ||
-                       (a.window > 0 && (sinks || pos0 <= p0 - a.window) && last > a.sinks))) {
+        if (hide) {
           // a weight of 0 does not undo a NaN: V rows that no query of the block sees are cleared
           const int key = (int)threadIdx.x >> 2, pos = groups.pos(8 * st + (key >> 3)) + (key & 7);  // four threads a row
           if (!((there >> (key >> 3) & 1) && pos < kv_end && pos <= p1 &&
@@ -927,8 +936,10 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
             after = at_stage(st + 2, pages);
             load_codes(pages, st + 2, codes);
           }
-        if (edge) mask(st, 0, there, up, low, s0);
-        if (check) follow(s0, nullptr, nullptr);
+        if (check) {
+          mask(st, 0, there, up, low, s0);
+          follow(s0, nullptr, nullptr);
+        }
         __builtin_amdgcn_sched_barrier(0);
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
           constexpr int kk = i / (D / 32), db = i % (D / 32);
@@ -937,8 +948,10 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           rounded_step<kE, i>(s0, a.c1, ref, l, p0b);
           __builtin_amdgcn_sched_barrier(0);
         });
-        if (edge) mask(st, 1, there, up, low, s1);
-        if (check) follow(s1, &s0, p0b);
+        if (check) {
+          mask(st, 1, there, up, low, s1);
+          follow(s1, &s0, p0b);
+        }
         __builtin_amdgcn_sched_barrier(0);
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
           constexpr int kk = i / (D / 32), db = i % (D / 32);
@@ -986,7 +999,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
     const uint32_t total = __float_as_uint((any[0] + any[1]) + (any[2] + any[3]));
     const bool bad = (total & 0x7f800000u) == 0x7f800000u ||
                      (__float_as_uint(l[0]) & 0x7fffffffu) > __float_as_uint(0x1p120f);
-    if (!__syncthreads_or(bad)) break;
+    if (!__builtin_amdgcn_readfirstlane(__syncthreads_or(bad))) break;
   }
 
   // o[db][v] holds d = 32*db + 8*(v/4) + 4*half + v%4 of this lane's row
