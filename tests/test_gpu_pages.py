@@ -80,6 +80,21 @@ def test_attention_layouts(cache, heads, new):
             want = out[:c.tokens]
 
 
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("bf16", H05), ("e4m3", H7), ("e4m3", H05)])
+@pytest.mark.parametrize("page", [8, 16, 96])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1800, 40)])
+@pytest.mark.parametrize("max_len", [0, 40])
+def test_missing_pages_far_in(cache, heads, page, window, sinks, max_len):
+    """Pages missing here and there along thousands of keys, in one split (max_len 40) and in many."""
+    rng = np.random.default_rng(page)
+    seqs = [(90, 3333), (40, 1500)]
+    missing = [(b, int(s)) for b, (_, n) in enumerate(seqs) for s in rng.choice(-(-n // page), 9, replace=False)]
+    c = Cache(cache, heads, page, seqs, seed=page, missing=missing)
+    c.poison(window, sinks)
+    pool, batch = c.device(max_len=max_len)
+    check_attention(c, attend(pool, batch, c.q.to(DEV), window, sinks), window, sinks)
+
+
 @pytest.mark.parametrize("cache,heads", [("bf16", H7), ("e4m3", H7), ("f32", HF)])
 @pytest.mark.parametrize("new", [1, 100])
 def test_rows_without_keys_are_zero(cache, heads, new):
