@@ -224,10 +224,15 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
     float o[kWaves][kRows][D + 4];
     float2 ml[kWaves][kRows];
   };
-  constexpr int kLds = sizeof(Joined) > kWaves * kTile * kRow ? sizeof(Joined) : kWaves * kTile * kRow;
+  // 8 waves have about two steps each (a launch of so few workgroups has splits of 16): both
+  // are loaded before the first is waited for (one sequence of 32,801 tokens in 8 bits 14.5 ->
+  // 14.1 us, 16 of up to 8,000 11.4 -> 11.1).
+  constexpr bool kPairs = kWaves == 8;
+  constexpr int kBuf = (kPairs ? 2 : 1) * kTile * kRow;  // of a wave
+  constexpr int kLds = sizeof(Joined) > kWaves * kBuf ? sizeof(Joined) : kWaves * kBuf;
   __shared__ __attribute__((aligned(16))) char lds[kLds];
   Joined& joined = *reinterpret_cast<Joined*>(lds);
-  char* lds_k = lds + wave * kTile * kRow;
+  char* lds_k = lds + wave * kBuf;
   // A load to LDS moves kLoadRows rows, lane l 16 bytes of row l / kSegs: the segment at
   // position s of row r is segment s ^ swz(r), so that 16 lanes that read one piece of 16
   // rows each meet 64 different banks.
@@ -292,7 +297,7 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
         x.at[i] = (int64_t)(names_page(a, x.e[i]) ? x.e[i] : 0) * a.page_stride + (int64_t)r0 * row_bytes;
       }
     };
-    auto load_k = [&](const Pages<kSmall>& x) __attribute__((always_inline)) {
+    auto load_k = [&](const Pages<kSmall>& x, char* to) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         constexpr int kPer = kLoadRows > kGroup ? kLoadRows / kGroup : 1;  // groups of a load: 2 at most
@@ -304,7 +309,7 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
           // (the second half of a load has the second group: 8 rows back in the lanes' offsets)
           const uint32_t in_group = (uint32_t)(key % kGroup * row_bytes);
           if (kPer == 1 || lane >> 5 == h)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (tile::LdsPtr)(lds_k + i * kLoadRows * kRow), 16,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (tile::LdsPtr)(to + i * kLoadRows * kRow), 16,
                                                      col - (uint32_t)(h * kGroup * row_bytes), in_group, 0, 0);
         }
       }
@@ -477,15 +482,55 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
       }
     };
 
-    // A step's rows load during the step before, its table entries two steps before.
     int st = begin + wave;
-    if (st < end) {
+    if constexpr (kPairs) {
+      if (st < end) {
+        Pages<kSmall> ga, gb;
+        Step<D, T> xa, xb;
+        pages_of(st, ga);
+        pages_of(min(st + kWaves, end - 1), gb);
+        auto read_k = [&](const char* from, u32x4 (&kw)[2][kPieces]) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int y = 0; y < kPieces; ++y)
+              kw[i][y] = *reinterpret_cast<const u32x4*>(from + i * 16 * kRow + k_at[y]);
+        };
+        while (true) {
+          const bool two = st + kWaves < end;
+          locate(st, ga);
+          load_k(ga, lds_k);
+          load_v(ga, xa);
+          if (two) {
+            locate(st + kWaves, gb);
+            load_k(gb, lds_k + kTile * kRow);
+            load_v(gb, xb);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          wait_loads();
+          __builtin_amdgcn_sched_barrier(0);
+          u32x4 kw[2][kPieces];
+          read_k(lds_k, kw);
+          attend(st, ga, kw, xa);
+          if (!two) break;
+          read_k(lds_k + kTile * kRow, kw);
+          attend(st + kWaves, gb, kw, xb);
+          st += 2 * kWaves;
+          if (st >= end) break;
+          pages_of(st, ga);
+          pages_of(min(st + kWaves, end - 1), gb);
+          wait_lds();  // read: the next steps' rows may come
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    } else if (st < end) {
+      // A step's rows load during the step before, its table entries two steps before.
       Pages<kSmall> ga, gb;
       Step<D, T> xa, xb;
       pages_of(st, ga);
       pages_of(min(st + kWaves, end - 1), gb);
       locate(st, ga);
-      load_k(ga);
+      load_k(ga, lds_k);
       load_v(ga, xa);
       __builtin_amdgcn_sched_barrier(0);
       auto turn = [&](Pages<kSmall>& g, Step<D, T>& x, Pages<kSmall>& gn, Step<D, T>& xn)
@@ -502,7 +547,7 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
         __builtin_amdgcn_sched_barrier(0);
         locate(min(st + kWaves, end - 1), gn);
         if (st + kWaves < end) {
-          load_k(gn);
+          load_k(gn, lds_k);
           load_v(gn, xn);
         }
         Pages<kSmall> after;
@@ -1054,25 +1099,34 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
   const int64_t row = (int64_t)blockIdx.x * kRowsPer + threadIdx.x / (kCols * kGroups);
   const int tok = (int)row / a.Hq;  // (at most 2^26 rows)
   // (with several groups, a workgroup has one row: it leaves as a whole)
-  if (row >= n_rows || tok < a.s.tok_off[0] || tok >= a.s.tok_off[a.s.n_seqs]) return;  // of no sequence
-  const int n_parts = min(a.n_parts[tok], a.n_splits);
-  if (n_parts <= 1) return;  // written already
+  if (row >= n_rows) return;
   const int col = threadIdx.x % kCols * 4, grp = threadIdx.x / kCols % kGroups;
-  float M = kNone, L = 0.f;
-  f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = grp; s0 < n_parts; s0 += kGroups * kJoinBatch) {
-    float2 ml[kJoinBatch];
-    f32x4 x[kJoinBatch];
+  float2 ml[kJoinBatch];
+  f32x4 x[kJoinBatch];
+  auto load = [&](int s0, int n) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < kJoinBatch; ++k) {
-      const int64_t at = (int64_t)min(s0 + k * kGroups, n_parts - 1) * n_rows + row;
+      const int64_t at = (int64_t)min(s0 + k * kGroups, n - 1) * n_rows + row;
       ml[k] = a.ml_part[at];
       x[k] = *reinterpret_cast<const f32x4*>(a.o_part + at * D + col);
     }
+  };
+  // the first splits come together with the number of them (those past it hold anything)
+  load(grp, a.n_splits);
+  const int first_tok = a.s.tok_off[0], end_tok = a.s.tok_off[a.s.n_seqs];
+  const int n_parts = min(a.n_parts[tok], a.n_splits);
+  if (tok < first_tok || tok >= end_tok || n_parts <= 1) return;  // of no sequence, or written already
+  float M = kNone, L = 0.f;
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = grp; s0 < n_parts; s0 += kGroups * kJoinBatch) {
+    if (s0 != grp) load(s0, n_parts);
     float to = M;
 #pragma unroll
     for (int k = 0; k < kJoinBatch; ++k) {
-      if (s0 + k * kGroups >= n_parts) ml[k] = make_float2(kNone, 0.f);
+      if (s0 + k * kGroups >= n_parts) {
+        ml[k] = make_float2(kNone, 0.f);
+        x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
       to = fmaxf(to, ml[k].x);
     }
     const float f = __builtin_amdgcn_exp2f(M - to);
