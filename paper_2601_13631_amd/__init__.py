@@ -473,8 +473,9 @@ class Store:
 
 def _need(t, what: str, dtype, shape=None):
     """``t`` if it is a contiguous tensor of the current HIP device, of this type and shape."""
-    if (t.dtype is dtype and t.get_device() == torch.cuda.current_device() and (shape is None or t.shape == shape)
-            and t.is_contiguous()):
+    # (of a device tensor: torch.cuda.current_device() without its look whether HIP has begun)
+    if (t.dtype is dtype and t.is_cuda and t.get_device() == torch._C._cuda_getDevice()
+            and (shape is None or t.shape == shape) and t.is_contiguous()):
         return t
     if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{what} must be on the current device (it is on {t.device})")
@@ -485,11 +486,18 @@ def _need(t, what: str, dtype, shape=None):
     raise ValueError(f"{what} must be contiguous")
 
 
-def _together(t, *handles) -> None:
-    """Raises unless the handles' tensors are on the device of ``t`` (the current one)."""
+def _together(t, *handles) -> int:
+    """The device of ``t``, the current one, where the handles' tensors have to be as well."""
+    device = t.get_device()
     for h in handles:
-        if h._device != t.get_device():
-            raise ValueError(f"the {type(h).__name__} is on device {h._device}, the call's tensors on {t.get_device()}")
+        if h._device != device:
+            raise ValueError(f"the {type(h).__name__} is on device {h._device}, the call's tensors on {device}")
+    return device
+
+
+def _stream_on(device: int, stream) -> int | None:
+    """``_stream`` where the current device is known."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
 
 
 def _workspace(ws, t):
@@ -593,8 +601,9 @@ def page_append(pool: PagePool, batch: PageBatch, k_new, v_new, stream=None) -> 
     shape = (batch.n_tokens, pool.n_kv_heads, pool.head_dim)
     _need(k_new, "k_new", pool.token_dtype, shape)
     _need(v_new, "v_new", pool.token_dtype, shape)
-    _together(k_new, pool, batch)
-    _check(_lib.ckv_page_append(pool._c, batch._c, k_new.data_ptr(), v_new.data_ptr(), _stream(stream)),
+    device = _together(k_new, pool, batch)
+    _check(_lib.ckv_page_append(pool._c, batch._c, k_new.data_ptr(), v_new.data_ptr(),
+                                _stream_on(device, stream)),
            "ckv_page_append")
 
 
@@ -612,15 +621,16 @@ def page_attn(pool: PagePool, batch: PageBatch, q, out, ws=None, window: int = 0
     pool, else bfloat16.  ``ws``: a uint8 tensor of
     :func:`page_attn_workspace_bytes` bytes (None where that is 0).
     """
-    if q.dim() != 3 or q.shape[0] != batch.n_tokens or q.shape[2] != pool.head_dim:
+    shape = q.shape
+    if len(shape) != 3 or shape[0] != batch.n_tokens or shape[2] != pool.head_dim:
         raise ValueError("q must be [n_tokens, n_q_heads, head_dim]")
     _need(q, "q", pool.token_dtype)
-    _need(out, "out", pool.token_dtype, q.shape)
-    _together(q, pool, batch)
+    _need(out, "out", pool.token_dtype, shape)
+    device = _together(q, pool, batch)
     ws_ptr, nbytes = _workspace(ws, q)
-    _check(_lib.ckv_page_attn(pool._c, batch._c, q.data_ptr(), q.shape[1], sm_scale,
+    _check(_lib.ckv_page_attn(pool._c, batch._c, q.data_ptr(), shape[1], sm_scale,
                               _int32(window, "window"), _int32(n_sinks, "n_sinks"), out.data_ptr(), ws_ptr,
-                              nbytes, _stream(stream)), "ckv_page_attn")
+                              nbytes, _stream_on(device, stream)), "ckv_page_attn")
 
 
 def page_copy(layers: PageLayers, src, dst, stream=None) -> None:
@@ -628,10 +638,9 @@ def page_copy(layers: PageLayers, src, dst, stream=None) -> None:
     every layer."""
     _need(src, "src", torch.int32)
     _need(dst, "dst", torch.int32, src.shape)
-    if layers.pools:
-        _together(src, layers)
+    device = _together(src, layers) if layers.pools else src.get_device()
     _check(_lib.ckv_page_copy(layers._c, len(layers.pools), src.data_ptr(), dst.data_ptr(), src.numel(),
-                              _stream(stream)), "ckv_page_copy")
+                              _stream_on(device, stream)), "ckv_page_copy")
 
 
 def page_compact_workspace_bytes(n_pages: int) -> int:
@@ -649,10 +658,9 @@ def page_compact(layers: PageLayers, refs, refs_out, table, table_out, n_live, w
     if table is not None:
         _need(table, "table", torch.int32)
         _need(table_out, "table_out", torch.int32, table.shape)
-    if layers.pools:
-        _together(refs, layers)
+    device = _together(refs, layers) if layers.pools else refs.get_device()
     ws_ptr, nbytes = _workspace(ws, refs)
     _check(_lib.ckv_page_compact(layers._c, len(layers.pools), refs.data_ptr(), refs_out.data_ptr(),
                                  refs.numel(), _ptr(table), _ptr(table_out) if table is not None else None,
                                  table.numel() if table is not None else 0, n_live.data_ptr(), ws_ptr,
-                                 nbytes, _stream(stream)), "ckv_page_compact")
+                                 nbytes, _stream_on(device, stream)), "ckv_page_compact")
