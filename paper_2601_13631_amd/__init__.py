@@ -530,27 +530,29 @@ class PagePool:
     """
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+        shape, dtype, stride = k.shape, k.dtype, k.stride()
+        if len(shape) != 4 or v.shape != shape or v.dtype is not dtype:
             raise ValueError("k and v must be of one type and shape [n_pages, page_size, n_kv_heads, head_dim]")
-        if k.dtype not in _PAGE_DTYPES:
-            raise ValueError(f"pages are float32, bfloat16 or float8_e4m3fn (not {k.dtype})")
-        n_pages, page_size, hkv, d = k.shape
+        number = _PAGE_DTYPES.get(dtype)
+        if number is None:
+            raise ValueError(f"pages are float32, bfloat16 or float8_e4m3fn (not {dtype})")
+        n_pages, page_size, hkv, d = shape
         for t in (k, v):
-            if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
                 raise ValueError(f"pages must be on the current device (they are on {t.device})")
-            if t.stride()[1:] != (hkv * d, d, 1) or (n_pages > 1 and t.stride(0) != k.stride(0)):
-                raise ValueError("a page's rows must be contiguous, and K and V pages equally far apart")
-        if (k.dtype == torch.float8_e4m3fn) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+        if stride[1:] != (hkv * d, d, 1) or (v.stride() != stride if n_pages > 1 else v.stride()[1:] != stride[1:]):
+            raise ValueError("a page's rows must be contiguous, and K and V pages equally far apart")
+        if (number == DTYPE_E4M3) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
             raise ValueError("k_scale and v_scale belong to float8_e4m3fn pages, and to those only")
-        for t in (k_scale, v_scale):
-            if t is not None:
-                _need(t, "a scale tensor", torch.uint8, (n_pages, hkv))
+        if k_scale is not None:
+            _need(k_scale, "k_scale", torch.uint8, (n_pages, hkv))
+            _need(v_scale, "v_scale", torch.uint8, (n_pages, hkv))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = n_pages, page_size, hkv, d
         self._device = k.get_device()
-        self.token_dtype = torch.float32 if k.dtype == torch.float32 else torch.bfloat16
-        self._c = _PagePool(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages,
-                            k.stride(0) if n_pages > 1 else 0, page_size, hkv, d, _PAGE_DTYPES[k.dtype])
+        self.token_dtype = torch.float32 if number == DTYPE_F32 else torch.bfloat16
+        self._c = _PagePool(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), n_pages,
+                            stride[0] if n_pages > 1 else 0, page_size, hkv, d, number)
 
 
 class PageLayers:
