@@ -19,8 +19,8 @@
 // Measured, join included: 64 sequences of 1,024 to 16,384 tokens in 8 bits, 40 heads on 8,
 // 162 us, 4.9 TB/s (a copy of 4 GiB reaches 4.8 read + write, a kernel that only reads 5.7 to
 // 6.1); 48 of up to 30,011 with a window of 4,096 in bf16 80 us, 4.6 TB/s; 512 tokens on 32,768
-// others, 28 heads on 4: bf16 248 us, 978 TFLOP/s, 8 bits 258 us, 940 (a matrix product of 8,192
-// reaches 1,230); five prompts of up to 2,048 tokens with a window of 1,000 135 us, 740.
+// others, 28 heads on 4: bf16 240 us, 1,010 TFLOP/s, 8 bits 242 us, 1,000 (a matrix product of
+// 8,192 reaches 1,230); five prompts of up to 2,048 tokens with a window of 1,000 130 us, 766.
 
 #include "attn_tile.h"
 #include "pages_internal.h"
@@ -184,7 +184,8 @@ __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f);
 // whole to LDS, a step ahead, into a buffer of the wave's own (64 sequences in 8 bits: 173 us
 // with K read to registers, 165 so).  The waves' outputs are joined through LDS.
 // Bound by memory, and by latency where there is little of it: a decoding step of one
-// sequence of 1,000 tokens takes 7.4 us, four dependent round trips and two steps per wave.
+// sequence of 1,000 tokens takes 6.6 us: four dependent round trips, two steps per wave of 0.9,
+// the waves' join 0.4.
 // kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page).
 template <int D, int T, bool kSmall, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(PageAttnArgs a) {
