@@ -542,6 +542,8 @@ class PagePool:
                 raise ValueError(f"pages must be on the current device (they are on {t.device})")
         if stride[1:] != (hkv * d, d, 1) or (v.stride() != stride if n_pages > 1 else v.stride()[1:] != stride[1:]):
             raise ValueError("a page's rows must be contiguous, and K and V pages equally far apart")
+        if n_pages > 1 and stride[0] < page_size * hkv * d:  # (0, of an expanded tensor, would mean dense)
+            raise ValueError(f"pages must not overlap (they are {stride[0]} elements apart)")
         if (number == DTYPE_E4M3) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
             raise ValueError("k_scale and v_scale belong to float8_e4m3fn pages, and to those only")
         if k_scale is not None:
