@@ -530,7 +530,7 @@ class PagePool:
     """
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        shape, dtype, stride = k.shape, k.dtype, k.stride()
+        shape, dtype, stride, v_stride = k.shape, k.dtype, k.stride(), v.stride()
         if len(shape) != 4 or v.shape != shape or v.dtype is not dtype:
             raise ValueError("k and v must be of one type and shape [n_pages, page_size, n_kv_heads, head_dim]")
         number = _PAGE_DTYPES.get(dtype)
@@ -540,7 +540,9 @@ class PagePool:
         for t in (k, v):
             if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
                 raise ValueError(f"pages must be on the current device (they are on {t.device})")
-        if stride[1:] != (hkv * d, d, 1) or (v.stride() != stride if n_pages > 1 else v.stride()[1:] != stride[1:]):
+        if hkv == 1:  # (where there is one head, its stride is not used)
+            stride, v_stride = ((*s[:2], d, s[3]) for s in (stride, v_stride))
+        if stride[1:] != (hkv * d, d, 1) or (v_stride != stride if n_pages > 1 else v_stride[1:] != stride[1:]):
             raise ValueError("a page's rows must be contiguous, and K and V pages equally far apart")
         if n_pages > 1 and stride[0] < page_size * hkv * d:  # (0, of an expanded tensor, would mean dense)
             raise ValueError(f"pages must not overlap (they are {stride[0]} elements apart)")

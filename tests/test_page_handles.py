@@ -66,3 +66,17 @@ def test_one_page_has_no_stride():
         k = pages((apart, 512, 128, 1), (1,) + SHAPE[1:])
         pool = ckv.PagePool(k, pages((8192, 512, 128, 1), (1,) + SHAPE[1:]))
         assert last_byte(pool) <= k.untyped_storage().nbytes()
+
+
+def test_one_head():
+    """Pages of one KV head that come from [n_pages, 1, page_size, head_dim]: contiguous, whatever the
+    stride of the one head says; heads cut out of more are not."""
+    x = torch.zeros(9, 1, 16, 64, dtype=torch.bfloat16)
+    turned, plain = x.transpose(1, 2).as_subclass(OnDevice), x.view(9, 16, 1, 64).as_subclass(OnDevice)
+    assert turned.stride() == (1024, 64, 1024, 1) and turned[0].is_contiguous()
+    for k, v in ((turned, turned), (turned, plain), (plain, turned)):
+        assert last_byte(ckv.PagePool(k, v)) <= x.untyped_storage().nbytes()
+    cut = torch.zeros(9, 16, 2, 64, dtype=torch.bfloat16)[:, :, :1].as_subclass(OnDevice)
+    for k, v in ((cut, cut), (plain, cut), (cut, plain)):
+        with pytest.raises(ValueError):
+            ckv.PagePool(k, v)
