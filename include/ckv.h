@@ -603,8 +603,10 @@ ckv_status ckv_cache_resident(const ckv_cache* cache, int32_t tier, int64_t* key
  * holds 8-bit codes (OCP e4m3: 1 sign, 4 exponent and 3 mantissa bits, no
  * infinity, largest 448) and a scale byte e per page and KV head for K, one for
  * V: a row's element is code * 2^(e - 127), e in [10, 247], which bf16 holds
- * exactly.  A power of two loses nothing: the codes keep four significant bits
- * whatever the scale.  page_size: 8, 16 or a multiple of 32.
+ * exactly, but for codes of 256 and more at e = 247: 2^128 and up, past bf16, they
+ * are read as 240 * 2^120 (what a finite number is appended as stays finite, and
+ * within 2^-4 of it).  A power of two loses nothing: the codes keep four
+ * significant bits whatever the scale.  page_size: 8, 16 or a multiple of 32.
  * ------------------------------------------------------------------------- */
 #define CKV_DTYPE_E4M3 2 /* page pools only */
 
@@ -651,8 +653,8 @@ typedef struct ckv_page_batch {
  * e >= 10, with |x| <= 448 * scale for the page's new rows; where the page
  * already held rows of this sequence, it is no less than before, and if it rises
  * the old codes are rounded again to it.  Codes are rounded to nearest even.
- * An infinity becomes the largest code of its sign, a NaN stays one; neither
- * counts for the scale.  A page must be written by one sequence of the call
+ * An infinity becomes the largest code of its sign (a finite element, then), a
+ * NaN stays one; neither counts for the scale.  A page must be written by one sequence of the call
  * only (give a forked sequence a copy of the page it goes on writing:
  * ckv_page_copy). */
 ckv_status ckv_page_append(const ckv_page_pool* pool, const ckv_page_batch* batch,

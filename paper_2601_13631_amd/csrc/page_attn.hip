@@ -5,7 +5,7 @@
 //   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  s_j = sm_scale q.k_j,
 // for any reference m.  A key is seen if j <= p, its page is there, and (window > 0)
 // j > p - window or j < n_sinks.  An 8-bit row is code * 2^(byte - 127), which bf16 holds
-// exactly: what follows the conversion is the bf16 computation.
+// exactly but for the largest (finite_codes): what follows the conversion is the bf16 computation.
 //
 // A sequence of few rows (query x head of one KV head) is bound by reading its K and V once:
 // page_rows_kernel, 16 rows per workgroup, many splits of the keys.  One of many rows by its
@@ -169,6 +169,16 @@ __device__ __forceinline__ bf16x8 bf16_of_codes(uint32_t w0, uint32_t w1, float 
 // s_waitcnt: vmcnt(0); lgkmcnt(0).
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }
+
+// 4 codes of a page whose scale byte is kTopByte or more.  There 256 times the scale is 2^128,
+// which bf16 does not hold: codes of 256 and more are taken for 240, the largest below (a
+// finite number appended is then read within the half step that its rounding is off by).
+// Bytes 0x78 to 0x7e become 0x77; 0x7f, a NaN, stays.
+constexpr uint32_t kTopByte = 247;
+__device__ __forceinline__ uint32_t finite_codes(uint32_t w) {
+  const uint32_t big = w >> 3 & w >> 4 & w >> 5 & w >> 6 & 0x01010101u, top = big & ~(w & w >> 1 & w >> 2);
+  return (w & ~(top * 0x7fu)) | top * 0x77u;
+}
 
 // Few rows: a workgroup owns 16 query rows of one KV head and one split of their
 // steps, its 4 or 8 waves step by step in turn:
@@ -358,7 +368,7 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
         }
       }
     };
-    auto attend = [&](int st, const Pages<kSmall>& e, const u32x4 (&kw)[2][kPieces], Step<D, T>& x)
+    auto attend = [&](int st, const Pages<kSmall>& e, u32x4 (&kw)[2][kPieces], Step<D, T>& x)
         __attribute__((always_inline)) {
       const int pos0 = steps.tile(st) * kTile;
       float ks[2], vs[2];
@@ -367,6 +377,21 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
         for (int i = 0; i < 2; ++i) {
           ks[i] = scale_of(x.ks[i]);
           vs[i] = scale_of(x.vs[i]);
+        }
+        if (__builtin_expect(__any(max(max(x.ks[0], x.ks[1]), max(x.vs[0], x.vs[1])) >= kTopByte), 0)) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (x.ks[i] >= kTopByte)
+#pragma unroll
+              for (int y = 0; y < kPieces; ++y)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) kw[i][y][w] = finite_codes(kw[i][y][w]);
+            if (x.vs[i] >= kTopByte)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int w = 0; w < kVWords; ++w) x.v[i][k][w] = finite_codes(x.v[i][k][w]);
+          }
         }
       }
       f32x4 s[2];
@@ -817,6 +842,23 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
     *reinterpret_cast<bf16x8*>((kv ? dv : dk) + key * D + (seg << 3)) =
         bf16_of_codes(w[2 * h], w[2 * h + 1], scale_of(byte));
   };
+  // finite_codes for what this lane has written of a stage, where one of the pages of its 8 has such
+  // a byte: codes past what bf16 holds are infinities by now, and become 240 * 2^120.  (On the codes
+  // in registers, for which there is no room, the long prefill takes 2% more, so 1%.)
+  auto any_top = [&](const Eight& x) __attribute__((always_inline)) { return __any(max(x.ks, x.vs) >= kTopByte) != 0; };
+  auto keep_finite = [&](uint16_t* dk, uint16_t* dv) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int n = 0; n < 4 * kLoads; ++n) {
+      const int key = (4 * (n / 4) + wave) * kERows + lane / kELanes;
+      const int seg = (2 * (lane % kELanes) + n % 2) ^ (n & 2 ? v_swz<D>(key) : k_swz<D>(key));
+      u32x4& w = *reinterpret_cast<u32x4*>((n & 2 ? dv : dk) + key * D + (seg << 3));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x = w[j], y = (x & 0x7fffu) == 0x7f80u ? x - 0x10u : x;
+        w[j] = (y & 0x7fff0000u) == 0x7f800000u ? y - 0x100000u : y;
+      }
+    }
+  };
 
   // byte offsets of the operand reads (the same for every stage)
   const int kr = kappa(lane & 31);
@@ -915,6 +957,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
       if constexpr (kE4) {
         load_codes(pages, begin, codes);
         static_for<4 * kLoads>([&](auto n) { write_codes(n, pages, begin, codes, k0, v0); });
+        if (any_top(pages)) keep_finite(k0, v0);
         if (begin + 1 < end) {
           there1 = at_stage(begin + 1, pages);
           load_codes(pages, begin + 1, codes);
@@ -943,7 +986,8 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
           hide = there != 0xffu || last > min(p1 + 1, kv_end) ||
                  (a.window > 0 && (sinks || pos0 <= p0 - a.window) && last > a.sinks);
         }
-        const bool check = !clear || look;
+        const bool top = kE4 && any_top(pages);  // (of the next stage's eight)
+        const bool check = !clear || look || top;
         uint32_t after = 0xffu;
         if constexpr (!kE4)
           if (st + 1 < end) {
@@ -983,6 +1027,8 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
             load_codes(pages, st + 2, codes);
           }
         if (check) {
+          if constexpr (kE4)
+            if (top) keep_finite(nk, nv);
           mask(st, 0, there, up, low, s0);
           follow(s0, nullptr, nullptr);
         }
