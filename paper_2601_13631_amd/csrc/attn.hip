@@ -61,6 +61,32 @@ namespace {
 
 using namespace tile;
 
+// The numerators exp2(c1 s - m) of 32 keys in 16 / E + 2 steps, which are
+// issued between MFMAs: step i scales the E logits of group i, takes the
+// exponentials of group i - 1, and adds those of group i - 2 to the row's sums
+// and packs them to bf16 pairs (P^T).  The empty asm keeps a step in its place.
+template <int E, int i>
+__device__ __forceinline__ void numerator_step(f32x16& s, float c1, float m, float (&l)[2],
+                                               u32x4 (&pb)[2]) {
+  constexpr int kGroups = 16 / E;
+  if constexpr (i < 0 || i > kGroups + 1) return;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (i < kGroups) s[E * i + e] = fmaf(s[E * i + e], c1, -m);
+    if (i >= 1 && i <= kGroups) s[E * (i - 1) + e] = __builtin_amdgcn_exp2f(s[E * (i - 1) + e]);
+    const int v = E * (i - 2) + e;
+    if (i < 2 || i > kGroups + 1) continue;
+    l[v & 1] += s[v];
+    asm volatile("" : "+v"(l[v & 1]));
+    if (v & 1) {
+      const bf16x2 b = {(__bf16)s[v - 1], (__bf16)s[v]};
+      uint32_t w = __builtin_bit_cast(uint32_t, b);
+      asm volatile("" : "+v"(w));
+      pb[v >> 3][(v & 7) >> 1] = w;
+    }
+  }
+}
+
 std::atomic<int> g_force_wide{0};  // ckv_debug_attn_wide_addressing
 
 // A slice is done again when its sum of numerators passes kGuard (1 / sum stays a normal

@@ -643,7 +643,10 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
   }
 }
 
-// numerator_step (attn_tile.h), but the row's sum takes the numerators as rounded.
+// The numerators exp2(c1 s - m) of 32 keys in 16 / E + 2 steps, which are issued between
+// MFMAs: step i scales the E logits of group i, takes the exponentials of group i - 1, and
+// packs those of group i - 2 to bf16 pairs (P^T), which as rounded are added to the row's sums.
+// The empty asm keeps a step in its place.
 template <int E, int i>
 __device__ __forceinline__ void rounded_step(f32x16& s, float c1, float m, float (&l)[2], u32x4 (&pb)[2]) {
   constexpr int kGroups = 16 / E;
