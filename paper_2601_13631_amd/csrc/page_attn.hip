@@ -10,17 +10,18 @@
 // A sequence of few rows (query x head of one KV head) is bound by reading its K and V once:
 // page_rows_kernel, 16 rows per workgroup, many splits of the keys.  One of many rows by its
 // products: page_tile_kernel, 128 rows against tiles in LDS.  A call takes the second from
-// 33 rows per KV head on (one sequence of 33,000 tokens in 8 bits, 28 heads on 4, at 3, 7 and
-// 18 tokens of 7 rows: rows 19.9, 27.0 and 45.8 us, tiles 26.1, 25.9 and 29.9; 16 sequences of
-// up to 8,000 in bf16: 38, 55 and 97, 39, 43 and 50).  fp32 takes the first always: its MFMA
-// needs no turning over, and its shapes are small.  Splits (by each sequence's own length)
-// leave partials in fp32 that page_combine_kernel joins in split order.
+// 33 rows per KV head on (one sequence of 33,000 tokens in 8 bits, 28 heads on 4, at 3, 4, 5, 7
+// and 18 tokens of 7 rows: rows 16.7, 17.0, 23.8, 26.3 and 46.3 us, tiles 22.5, 22.7, 23.1, 23.7
+// and 27.7; 16 sequences of up to 8,000 in bf16 with up to as many: 43.1, 43.6, 46.2, 57.3 and
+// 83.5, 46.4, 44.5, 45.1, 48.5 and 52.9).  fp32 has the first only: 128 tokens on 4,096 14.1 us,
+// 1,000 on 4,000 59 (3.6 GFLOP; a product of 8,192 reaches 154 TFLOP/s).  Splits (by each
+// sequence's own length) leave partials in fp32 that page_combine_kernel joins in split order.
 //
 // Measured, join included: 64 sequences of 1,024 to 16,384 tokens in 8 bits, 40 heads on 8,
-// 162 us, 4.9 TB/s (a copy of 4 GiB reaches 4.8 read + write, a kernel that only reads 5.7 to
-// 6.1); 48 of up to 30,011 with a window of 4,096 in bf16 80 us, 4.6 TB/s; 512 tokens on 32,768
-// others, 28 heads on 4: bf16 240 us, 1,010 TFLOP/s, 8 bits 242 us, 1,000 (a matrix product of
-// 8,192 reaches 1,230); five prompts of up to 2,048 tokens with a window of 1,000 130 us, 766.
+// 163 us, 4.8 TB/s (a kernel that only reads such pages reaches 5.6 to 6.0); 48 of up to 30,011
+// with a window of 4,096 in bf16 80 us, 4.6 TB/s; 512 tokens on 32,768 others, 28 heads on 4:
+// 239 to 254 us by the card, 955 to 1,010 TFLOP/s, in bf16 and 8 bits alike (a matrix product of
+// 8,192 reaches 1,210 to 1,230); five prompts of up to 2,048 tokens with a window of 1,000 130 us, 766.
 
 #include "attn_tile.h"
 #include "pages_internal.h"
@@ -1235,7 +1236,8 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
                                          : b->n_tokens;
   int64_t len = (int64_t)b->max_pages * pool->page_size;
   if (b->max_len > 0) len = std::min<int64_t>(len, b->max_len);
-  p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32;  // (both sides: top of the file)
+  // (both sides: top of the file; one kernel for the call, by its longest sequence)
+  p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32;
   if (p.wide) {
     p.blocks = b->n_tokens * G / tile::kBlockRows + b->n_seqs;
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + ceil_div(tile::kBlockRows, G) + sinks + 16);
@@ -1247,6 +1249,7 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
     // one split, 1,148 in 4, 1,125 in 6; after a window of 1,000: 67 us in one, 86 in 2.)
     constexpr double kFixed = 15000, kStage = 3440, kFixedAlone = 12500, kStageAlone = 2100;
     constexpr double kJoin = 5500, kJoinBytes = 2500;
+    // (sequences' last blocks are taken as full: many short ones are more workgroups than this)
     const int64_t wgs = (b->n_tokens * G / tile::kBlockRows + 1) * pool->n_kv_heads;
     const double join = (double)b->n_tokens * Hq * pool->head_dim * 2 * sizeof(float) / kJoinBytes;
     double best = 0;

@@ -2,9 +2,10 @@
 //
 // All three move bytes, each 16-byte piece read once and written once: memory bounds the
 // large calls, launch and latency the small ones.  Measured: the rows of four prompts (15,300
-// tokens of 4 heads of 128, bf16 to 8 bits, 47 MB) 12.5 us, of one step of 64 sequences 5.1; eight
-// pages copied in 28 layers (15 MB) 6 us; 850 of 4,000 pages of 8 KB moved in 28 layers (780 MB
-// read + written) 173 us, 4.5 TB/s (a copy of 4 GiB: 4.8).
+// tokens of 4 heads of 128, bf16 to 8 bits, 47 MB) 12.5 us, of one step of 64 sequences 5.2; the
+// same prompts into a bf16 pool (63 MB) 14.7, the step 5.2; eight pages copied in 28 layers
+// (15 MB) 6 us; 850 of 4,000 pages of 8 KB moved in 28 layers (780 MB read + written) 173 us,
+// 4.5 TB/s (a copy of 4 GiB: 4.8).
 
 #include "pages_internal.h"
 
