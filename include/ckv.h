@@ -716,6 +716,154 @@ ckv_status ckv_page_compact(const ckv_page_pool* pools, int32_t n_pools, const i
                             int32_t* table_out, int64_t n_entries, int32_t* n_live, void* ws,
                             size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Sequences that share a prefix -- a decoding step over a paged cache whose
+ * sequences begin with the same pages (the beams of a request, questions on one
+ * document): ckv_beam_select chooses the continuations, ckv_page_fork lets the
+ * sequences follow their parents, ckv_page_extend finds the step's pages and slots,
+ * ckv_page_copy copies the pages that it names, ckv_page_append writes the rows,
+ * ckv_page_share finds what each group shares (once for all layers) and
+ * ckv_page_attn_shared attends.  Everything is read on the device only: a captured
+ * graph of these calls serves other lengths, tables and parents.
+ * ------------------------------------------------------------------------- */
+
+/* The groups of a batch: group g is the sequences grp_off[g] .. grp_off[g+1]-1.
+ * grp_off must not fall; what it names outside [0, n_seqs] is not there.  Sequences
+ * in no group share nothing. */
+typedef struct ckv_page_groups {
+  const int32_t* grp_off; /* device, [n_groups + 1]                                       */
+  int32_t* shared;        /* device, ckv_page_share_ints(...) numbers that ckv_page_share
+                             leaves for ckv_page_attn_shared                              */
+  int32_t n_groups;       /* 0 .. 2^20; 0: no sequence shares anything                    */
+  int32_t max_tokens;     /* about the most tokens of one group's sequences together, and */
+  int32_t max_shared;     /*   about the most tokens that one shares: they choose kernels
+                               and splits, results hold for any; 0: not known, taken for
+                               n_tokens and max_len                                       */
+} ckv_page_groups;
+
+/* Finds what the sequences of each group share, from the batch's table, lengths and
+ * offsets: with P the pages on which the tables of all its sequences that have tokens
+ * in the call agree from the first on, and m the keys that every one of the group's
+ * queries sees (the least lens[b] - n_b + 1), E = 32 * floor(min(P * page_size, m) / 32)
+ * tokens.  shared receives E and the first sequence with tokens of each group, then
+ * every sequence's E (0 outside the groups).  page_size as in a pool. */
+int64_t ckv_page_share_ints(int32_t n_groups, int32_t n_seqs);
+ckv_status ckv_page_share(int32_t page_size, const ckv_page_batch* batch,
+                          const ckv_page_groups* groups, void* stream);
+
+/* ckv_page_attn without a window, where groups of sequences share their first pages:
+ * a group's shared keys are read once for all of its rows.  `groups` as ckv_page_share
+ * left it for this batch's table, lengths and offsets (the keys that it counts are read
+ * from the first of a group's tables).  Everything else as ckv_page_attn: what rows and
+ * pages that no query sees hold, the rows behind the last sequence, the limits.
+ * Where the shared pages are few, every sequence reads them for itself. */
+size_t ckv_page_attn_shared_workspace_bytes(const ckv_page_pool* pool, const ckv_page_batch* batch,
+                                            const ckv_page_groups* groups, int32_t n_q_heads);
+ckv_status ckv_page_attn_shared(const ckv_page_pool* pool, const ckv_page_batch* batch,
+                                const ckv_page_groups* groups, const void* q, int32_t n_q_heads,
+                                float sm_scale, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Tables, lengths and use counts of sequences, before a call and after it.  Sequence b
+ * holds the pages table[b][0 .. ceil(lens[b] / page_size)), refs[p] counts who holds page
+ * p (sequences, and a prefix store, say); a page of count 0 or less is free.  Entries
+ * outside [0, n_pages) name no page.  A negative length counts as 0; one past the table as
+ * the whole table. */
+typedef struct ckv_page_tables {
+  const int32_t* table;     /* device, [n_seqs][table_stride]                             */
+  int32_t* table_out;       /* device, [n_out][table_out_stride]                          */
+  const int32_t* lens;      /* device, [n_seqs]                                           */
+  int32_t* lens_out;        /* device, [n_out]                                            */
+  const int32_t* refs;      /* device, [n_pages]                                          */
+  int32_t* refs_out;        /* device, [n_pages]; may be refs                             */
+  int64_t table_stride;     /* entries between consecutive sequences; 0: max_pages        */
+  int64_t table_out_stride;
+  int64_t n_pages;          /* 1 .. 2^26                                                  */
+  int32_t n_seqs;           /* 0 .. 2^20                                                  */
+  int32_t n_out;
+  int32_t max_pages;        /* entries used per sequence, at least 1; at most 2^30 tokens  */
+  int32_t page_size;        /* as in a pool                                               */
+} ckv_page_tables;
+
+/* Rows of a state that every sequence has (its tokens so far, say): row i of dst becomes
+ * row parents[i] of src.  Rows are row_bytes bytes, their strides apart (0: row_bytes). */
+typedef struct ckv_seq_rows {
+  const void* src;    /* device, [n_seqs] rows */
+  void* dst;          /* device, [n_out] rows; another buffer than src */
+  int64_t row_bytes;  /* 1 .. 2^40 */
+  int64_t src_stride; /* bytes */
+  int64_t dst_stride;
+} ckv_seq_rows;
+#define CKV_MAX_SEQ_ROWS 8
+
+/* After the call, sequence i < n_out is a copy of sequence parents[i] as it was: its
+ * table entries (-1 behind them), its length, its rows of the n_states states.  With a
+ * parent outside [0, n_seqs) it is empty: no entries, length 0, the states' rows as they
+ * were.  refs_out[p] = refs[p] + (children of b - 1) summed over the sequences b that
+ * hold page p: who has no children gives its pages back.  Tables and lengths go to other
+ * buffers than they come from. */
+ckv_status ckv_page_fork(const ckv_page_tables* tables, const int32_t* parents,
+                         const ckv_seq_rows* states, int32_t n_states, void* stream);
+
+/* What the token rows of a step are, written by ckv_page_extend (device). */
+typedef struct ckv_page_step {
+  int32_t* tok_off;   /* [n_seqs + 1]: a ckv_page_batch's                                 */
+  int64_t* slots;     /* [n_tokens]: page * page_size + row of each token; -1: without a  */
+  int32_t* positions; /*   page, or behind the last token                                 */
+  int32_t* seqs;      /* [n_tokens]: positions and sequences; -1 behind the last token.   */
+                      /*   slots, positions and seqs may be NULL                          */
+  int32_t* copy_src;  /* [n_seqs]: pages to copy before the tokens are written            */
+  int32_t* copy_dst;  /*   (ckv_page_copy), -1: none                                      */
+  int32_t* counts;    /* [4]: tokens, pages taken, pages left free, sequences refused     */
+  int64_t n_tokens;   /* rows there are, up to 2^31 - 1                                   */
+} ckv_page_step;
+
+/* Gives sequence b pages for n_new[b] more tokens (device, [n_seqs]; below 0: 0).
+ *   pages   It needs those behind its last one, and where that one has room and
+ *           refs > 1 before the call (others hold it) another in its place:
+ *           copy_src[b], copy_dst[b] name the two.  Needs are met in the order of the
+ *           sequences, their places ascending, by the free pages (refs <= 0) ascending.
+ *   counts  A page that is taken gets 1, one that was replaced one less for each who
+ *           replaced it (0 if they all did: it is free from the next call on, so copy
+ *           first).
+ *   refusal A sequence is refused, and stays as it is, if its length would pass its
+ *           table; or if those that need pages up to and with it, refused ones too, need
+ *           more than are free; or their n_new more than n_tokens rows (of the former
+ *           kind of refusal neither counts).  Its n_new becomes 0.
+ *   lens_out gets the lengths with the new tokens, tok_off and the token arrays the
+ *           rows: sequence after sequence, positions ascending.
+ * n_out must be n_seqs; table_out, lens_out and refs_out may be table, lens and refs.
+ * ws: ckv_page_extend_workspace_bytes(n_pages, n_seqs) bytes. */
+size_t ckv_page_extend_workspace_bytes(int64_t n_pages, int32_t n_seqs);
+ckv_status ckv_page_extend(const ckv_page_tables* tables, const int32_t* n_new,
+                           const ckv_page_step* step, void* ws, size_t ws_bytes, void* stream);
+
+/* The continuations of beams.  Request r has n_beams beams with scores c_b (sums of log
+ * probabilities, -inf: an empty place) and, for a vocabulary of V, logits x_b.  A live
+ * beam offers its V tokens at c_b + x_bv - log sum_u exp(x_bu); one that is done offers
+ * only `eos`, at c_b; an empty one nothing.  The `keep` best of a request, best first, are
+ * written as (parent, token, score, done); equal scores go to the lower beam, then the
+ * larger logit, then the lower token.  Scores are held in 64 bits (the exponentials under
+ * the logarithm in 32, their sums in 64) and rounded once.  -inf and NaN logits offer
+ * nothing and add nothing; an infinity counts as the largest finite number.
+ *   parent  r * n_beams + b; token; score; done: 1 for eos and for who was done.  Where
+ *           fewer are offered: -1, -1, -inf, 0
+ *   ws      ckv_beam_select_workspace_bytes(...) bytes for the same beams */
+typedef struct ckv_beams {
+  const void* logits;    /* device, rows r * n_beams + b of vocab elements, aligned to one */
+  const float* scores;   /* device, [n_reqs][n_beams]                                     */
+  const uint8_t* done;   /* device, [n_reqs][n_beams], or NULL: none                      */
+  int64_t row_stride;    /* elements between consecutive rows; 0: vocab                   */
+  int32_t n_reqs;        /* 0 .. 2^20                                                     */
+  int32_t n_beams;       /* 1 .. 64                                                       */
+  int32_t vocab;         /* at least 1                                                    */
+  int32_t keep;          /* 1 .. 64                                                       */
+  int32_t eos;           /* the token that ends a beam; -1: none (then without done)      */
+  int32_t dtype;         /* CKV_DTYPE_F32 or CKV_DTYPE_BF16                               */
+} ckv_beams;
+size_t ckv_beam_select_workspace_bytes(const ckv_beams* beams);
+ckv_status ckv_beam_select(const ckv_beams* beams, int32_t* parent, int32_t* token, float* score,
+                           uint8_t* done, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

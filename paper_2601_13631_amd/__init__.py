@@ -94,10 +94,44 @@ class _PageBatch(ctypes.Structure):
         (f, ctypes.c_int32) for f in ("n_seqs", "max_pages", "max_tokens", "max_len")]
 
 
+class _PageGroups(ctypes.Structure):
+    """``ckv_page_groups``."""
+    _fields_ = [(f, ctypes.c_void_p) for f in ("grp_off", "shared")] + [
+        (f, ctypes.c_int32) for f in ("n_groups", "max_tokens", "max_shared")]
+
+
+class _PageTables(ctypes.Structure):
+    """``ckv_page_tables``."""
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "table", "table_out", "lens", "lens_out", "refs", "refs_out")] + [
+        (f, ctypes.c_int64) for f in ("table_stride", "table_out_stride", "n_pages")] + [
+        (f, ctypes.c_int32) for f in ("n_seqs", "n_out", "max_pages", "page_size")]
+
+
+class _SeqRows(ctypes.Structure):
+    """``ckv_seq_rows``."""
+    _fields_ = [(f, ctypes.c_void_p) for f in ("src", "dst")] + [
+        (f, ctypes.c_int64) for f in ("row_bytes", "src_stride", "dst_stride")]
+
+
+class _PageStep(ctypes.Structure):
+    """``ckv_page_step``."""
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "tok_off", "slots", "positions", "seqs", "copy_src", "copy_dst", "counts")] + [("n_tokens", ctypes.c_int64)]
+
+
+class _Beams(ctypes.Structure):
+    """``ckv_beams``."""
+    _fields_ = [(f, ctypes.c_void_p) for f in ("logits", "scores", "done")] + [("row_stride", ctypes.c_int64)] + [
+        (f, ctypes.c_int32) for f in ("n_reqs", "n_beams", "vocab", "keep", "eos", "dtype")]
+
+
 _P = ctypes.c_void_p
 _DP = ctypes.POINTER(Dims)
 _PP = ctypes.POINTER(_PagePool)
 _BP = ctypes.POINTER(_PageBatch)
+_GP = ctypes.POINTER(_PageGroups)
+_TP = ctypes.POINTER(_PageTables)
 _I32, _I64, _SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 _SIG = {
     "ckv_last_error": ([], ctypes.c_char_p),
@@ -151,6 +185,15 @@ _SIG = {
     "ckv_page_copy": ([_PP, _I32, _P, _P, _I64, _P], _I32),
     "ckv_page_compact_workspace_bytes": ([_I64], _SZ),
     "ckv_page_compact": ([_PP, _I32, _P, _P, _I64, _P, _P, _I64, _P, _P, _SZ, _P], _I32),
+    "ckv_page_share_ints": ([_I32, _I32], _I64),
+    "ckv_page_share": ([_I32, _BP, _GP, _P], _I32),
+    "ckv_page_attn_shared_workspace_bytes": ([_PP, _BP, _GP, _I32], _SZ),
+    "ckv_page_attn_shared": ([_PP, _BP, _GP, _P, _I32, ctypes.c_float, _P, _P, _SZ, _P], _I32),
+    "ckv_page_fork": ([_TP, _P, ctypes.POINTER(_SeqRows), _I32, _P], _I32),
+    "ckv_page_extend_workspace_bytes": ([_I64, _I32], _SZ),
+    "ckv_page_extend": ([_TP, _P, ctypes.POINTER(_PageStep), _P, _SZ, _P], _I32),
+    "ckv_beam_select_workspace_bytes": ([ctypes.POINTER(_Beams)], _SZ),
+    "ckv_beam_select": ([ctypes.POINTER(_Beams), _P, _P, _P, _P, _P, _SZ, _P], _I32),
 }
 for _name, (_args, _res) in _SIG.items():
     _f = getattr(_lib, _name)
@@ -672,3 +715,248 @@ def page_compact(layers: PageLayers, refs, refs_out, table, table_out, n_live, w
                                  refs.numel(), _ptr(table), _ptr(table_out) if table is not None else None,
                                  table.numel() if table is not None else 0, n_live.data_ptr(), ws_ptr,
                                  nbytes, _stream_on(device, stream)), "ckv_page_compact")
+
+
+class PageGroups:
+    """``ckv_page_groups``: the groups of a batch whose sequences share their first pages.
+
+    ``grp_off`` (int32 [n_groups + 1], device): group g is the sequences ``grp_off[g]`` to
+    ``grp_off[g + 1] - 1``.  ``shared``: an int32 tensor of :func:`page_share_ints` numbers,
+    which :func:`page_share` writes.  ``max_tokens`` and ``max_shared``: about the most tokens
+    of one group's sequences together, and the most that one shares (0: not known).  Keeps
+    the tensors alive; one handle serves every step on the same tensors.
+    """
+
+    def __init__(self, grp_off, shared, max_tokens: int = 0, max_shared: int = 0):
+        if grp_off.dim() != 1 or grp_off.shape[0] < 1:
+            raise ValueError("grp_off must be [n_groups + 1]")
+        _need(grp_off, "grp_off", torch.int32)
+        _need(shared, "shared", torch.int32)
+        self.grp_off, self.shared = grp_off, shared
+        self.n_groups = grp_off.shape[0] - 1
+        self._device = grp_off.get_device()
+        self._c = _PageGroups(_ptr(grp_off), _ptr(shared), self.n_groups, _int32(max_tokens, "max_tokens"),
+                              _int32(max_shared, "max_shared"))
+
+    def _fits(self, batch: PageBatch) -> None:
+        if self.shared.numel() < 2 * self.n_groups + batch.n_seqs:
+            raise ValueError(f"shared must have {2 * self.n_groups + batch.n_seqs} numbers (it has "
+                             f"{self.shared.numel()})")
+
+
+def page_share_ints(n_groups: int, n_seqs: int) -> int:
+    return int(_lib.ckv_page_share_ints(_int32(n_groups, "n_groups"), _int32(n_seqs, "n_seqs")))
+
+
+def page_share(page_size: int, batch: PageBatch, groups: PageGroups, stream=None) -> None:
+    """``ckv_page_share``: what each group's sequences share, for :func:`page_attn_shared` in
+    every layer; again whenever the table, the lengths or the offsets have changed."""
+    groups._fits(batch)
+    device = _together(groups.grp_off, groups, batch)
+    _check(_lib.ckv_page_share(_int32(page_size, "page_size"), batch._c, groups._c, _stream_on(device, stream)),
+           "ckv_page_share")
+
+
+def page_attn_shared_workspace_bytes(pool: PagePool, batch: PageBatch, groups: PageGroups, n_q_heads: int) -> int:
+    return int(_lib.ckv_page_attn_shared_workspace_bytes(pool._c, batch._c, groups._c,
+                                                         _int32(n_q_heads, "n_q_heads")))
+
+
+def page_attn_shared(pool: PagePool, batch: PageBatch, groups: PageGroups, q, out, ws=None, sm_scale: float = 0.0,
+                     stream=None) -> None:
+    """``ckv_page_attn_shared``: :func:`page_attn` without a window, the pages that a group's
+    sequences share read once for all of them (``groups`` as :func:`page_share` left it).
+
+    ``ws``: a uint8 tensor of :func:`page_attn_shared_workspace_bytes` bytes (None where that is 0).
+    """
+    shape = q.shape
+    if len(shape) != 3 or shape[0] != batch.n_tokens or shape[2] != pool.head_dim:
+        raise ValueError("q must be [n_tokens, n_q_heads, head_dim]")
+    _need(q, "q", pool.token_dtype)
+    _need(out, "out", pool.token_dtype, shape)
+    groups._fits(batch)
+    device = _together(q, pool, batch, groups)
+    ws_ptr, nbytes = _workspace(ws, q)
+    _check(_lib.ckv_page_attn_shared(pool._c, batch._c, groups._c, q.data_ptr(), shape[1], sm_scale,
+                                     out.data_ptr(), ws_ptr, nbytes, _stream_on(device, stream)),
+           "ckv_page_attn_shared")
+
+
+def _rows(t, what: str) -> int:
+    """Elements between the rows of an int32 table of the current device."""
+    if t.dim() != 2 or t.dtype != torch.int32 or not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} must be an int32 tensor [n_seqs, max_pages] of the current device")
+    n, width = t.shape
+    if n > 0 and width > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    stride = t.stride(0) if n > 1 else width
+    if stride < width:
+        raise ValueError(f"the rows of {what} must not overlap")
+    return stride
+
+
+def _tables(page_size, table, table_out, lens, lens_out, refs, refs_out) -> _PageTables:
+    stride, out_stride = _rows(table, "table"), _rows(table_out, "table_out")
+    if table_out.shape[1] != table.shape[1]:
+        raise ValueError("table and table_out must be equally wide")
+    _need(lens, "lens", torch.int32, table.shape[:1])
+    _need(lens_out, "lens_out", torch.int32, table_out.shape[:1])
+    _need(refs, "refs", torch.int32)
+    _need(refs_out, "refs_out", torch.int32, refs.shape)
+    return _PageTables(_ptr(table), _ptr(table_out), _ptr(lens), _ptr(lens_out), _ptr(refs), _ptr(refs_out),
+                       stride, out_stride, refs.numel(), table.shape[0], table_out.shape[0], table.shape[1],
+                       _int32(page_size, "page_size"))
+
+
+class PageFork:
+    """What :func:`page_fork` reads and writes, as one handle.
+
+    ``table`` [n_seqs, max_pages], ``lens`` [n_seqs] and ``refs`` [n_pages] (int32, device) are the
+    sequences as they are, ``table_out`` [n_out, max_pages], ``lens_out`` [n_out] and ``refs_out`` (which
+    may be ``refs``) those after the call.  ``states``: pairs of tensors [n_seqs, ...] and
+    [n_out, ...] of one type whose rows follow the sequences, up to eight; a row is
+    contiguous, rows may lie apart.  Keeps the tensors alive; make it once per pair of buffers.
+    """
+
+    def __init__(self, page_size: int, table, table_out, lens, lens_out, refs, refs_out, states=()):
+        self._c = _tables(page_size, table, table_out, lens, lens_out, refs, refs_out)
+        self.n_seqs, self.n_out = table.shape[0], table_out.shape[0]
+        self._device = refs.get_device()
+        self._tensors = (table, table_out, lens, lens_out, refs, refs_out, *(t for pair in states for t in pair))
+        rows = []
+        for src, dst in states:
+            if src.dtype != dst.dtype or src.shape[1:] != dst.shape[1:]:
+                raise ValueError("a state's tensors must be of one type and row shape")
+            if src.dim() < 1 or src.shape[0] != self.n_seqs or dst.shape[0] != self.n_out:
+                raise ValueError(f"a state needs {self.n_seqs} rows, and {self.n_out} to write")
+            strides = []
+            for t in (src, dst):
+                if not t.is_cuda or t.get_device() != self._device:
+                    raise ValueError(f"states must be on the current device (one is on {t.device})")
+                if t.shape[0] > 0 and not t[0].is_contiguous():
+                    raise ValueError("a state's rows must be contiguous")
+                strides.append(t.stride(0) * t.element_size() if t.shape[0] > 1 else 0)
+            nbytes = src[0].numel() * src.element_size() if self.n_seqs > 0 else 0
+            if nbytes == 0:
+                continue
+            if any(t.shape[0] > 1 and s < nbytes for t, s in zip((src, dst), strides)):
+                raise ValueError("a state's rows must not overlap")
+            rows.append(_SeqRows(src.data_ptr(), dst.data_ptr(), nbytes, *strides))
+        self._states = (_SeqRows * len(rows))(*rows)
+        self._n_states = len(rows)
+
+
+def page_fork(fork: PageFork, parents, stream=None) -> None:
+    """``ckv_page_fork``: sequence i becomes a copy of sequence ``parents[i]`` (int32 [n_out], device; one
+    outside the sequences: empty): its pages, its length, its rows of the states."""
+    _need(parents, "parents", torch.int32)
+    if parents.numel() != fork.n_out:
+        raise ValueError(f"parents must have {fork.n_out} numbers (it has {parents.numel()})")
+    device = _together(parents, fork)
+    _check(_lib.ckv_page_fork(fork._c, _ptr(parents), fork._states, fork._n_states, _stream_on(device, stream)),
+           "ckv_page_fork")
+
+
+class PageStep:
+    """What :func:`page_extend` reads and writes, as one handle.
+
+    ``table``, ``lens`` and ``refs`` (int32, device) as in :class:`PageFork`; ``table_out``, ``lens_out`` and
+    ``refs_out`` may be the same tensors.  ``n_new`` [n_seqs]: the tokens that each sequence
+    gets.  Written: ``tok_off`` [n_seqs + 1], ``copy_src`` and ``copy_dst`` [n_seqs], ``counts`` [4], and, each
+    of as many rows as the call's token tensors, ``slots`` (int64), ``positions`` and ``seqs`` (int32; any
+    of these may be None).  ``n_tokens``: those rows, where all three are None.
+    Keeps the tensors alive; one handle serves every step on the same tensors.
+    """
+
+    def __init__(self, page_size: int, table, table_out, lens, lens_out, refs, refs_out, n_new, tok_off, copy_src,
+                 copy_dst, counts, slots=None, positions=None, seqs=None, n_tokens: int = 0):
+        self._c = _tables(page_size, table, table_out, lens, lens_out, refs, refs_out)
+        n = table.shape[0]
+        if table_out.shape[0] != n:
+            raise ValueError("table and table_out must have as many rows")
+        _need(n_new, "n_new", torch.int32, (n,))
+        _need(tok_off, "tok_off", torch.int32, (n + 1,))
+        _need(copy_src, "copy_src", torch.int32, (n,))
+        _need(copy_dst, "copy_dst", torch.int32, (n,))
+        _need(counts, "counts", torch.int32, (4,))
+        given = [(t, w, d) for t, w, d in ((slots, "slots", torch.int64), (positions, "positions", torch.int32),
+                                           (seqs, "seqs", torch.int32)) if t is not None]
+        if given:
+            n_tokens = given[0][0].numel()
+        for t, what, dtype in given:
+            _need(t, what, dtype, (n_tokens,))
+        self._device = refs.get_device()
+        self.n_seqs, self.n_pages = n, refs.numel()
+        self.n_new = n_new
+        self._tensors = (table, table_out, lens, lens_out, refs, refs_out, tok_off, copy_src, copy_dst, counts, slots,
+                         positions, seqs)
+        self._step = _PageStep(_ptr(tok_off), _ptr(slots), _ptr(positions), _ptr(seqs), _ptr(copy_src),
+                               _ptr(copy_dst), _ptr(counts), _int32(n_tokens, "n_tokens"))
+
+
+def page_extend_workspace_bytes(n_pages: int, n_seqs: int) -> int:
+    return int(_lib.ckv_page_extend_workspace_bytes(n_pages, _int32(n_seqs, "n_seqs")))
+
+
+def page_extend(step: PageStep, ws, stream=None) -> None:
+    """``ckv_page_extend``: pages for every sequence's ``n_new`` tokens, and what the step's token rows
+    are; then :func:`page_copy` of ``copy_src`` to ``copy_dst``, and :func:`page_append`.  ``ws``: a uint8
+    tensor of :func:`page_extend_workspace_bytes` bytes."""
+    device = _together(step.n_new, step)
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"the step is on device {device}, not the current one")
+    ws_ptr, nbytes = _workspace(ws, step.n_new)
+    _check(_lib.ckv_page_extend(step._c, _ptr(step.n_new), step._step, ws_ptr, nbytes, _stream_on(device, stream)),
+           "ckv_page_extend")
+
+
+_LOGIT_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+def _beams(logits, keep: int, scores=None, done=None, eos: int = -1) -> _Beams:
+    if logits.dim() != 3 or logits.dtype not in _LOGIT_DTYPES:
+        raise ValueError("logits must be a float32 or bfloat16 tensor [n_reqs, n_beams, vocab]")
+    n_reqs, n_beams, vocab = logits.shape
+    if logits.numel() > 0 and vocab > 1 and logits.stride(2) != 1:
+        raise ValueError("a beam's logits must be contiguous")
+    # (a dimension of one has no stride that counts)
+    stride = logits.stride(1) if n_beams > 1 else logits.stride(0) if n_reqs > 1 else vocab
+    if n_reqs > 1 and n_beams > 1 and logits.stride(0) != n_beams * stride:
+        raise ValueError("the beams' logits must be equally far apart")
+    if n_reqs * n_beams > 1 and stride < vocab:
+        raise ValueError("the beams' logits must not overlap")
+    return _Beams(_ptr(logits), _ptr(scores), _ptr(done), stride, n_reqs, n_beams, vocab, _int32(keep, "keep"), eos,
+                  _LOGIT_DTYPES[logits.dtype])
+
+
+def beam_select_workspace_bytes(logits, keep: int) -> int:
+    return int(_lib.ckv_beam_select_workspace_bytes(_beams(logits, keep)))
+
+
+def beam_select(logits, scores, parent, token, scores_out, ws, done=None, done_out=None, eos: int = -1,
+                stream=None) -> None:
+    """``ckv_beam_select``: the best continuations of each request's beams.
+
+    ``logits`` [n_reqs, n_beams, vocab] (float32 or bfloat16, rows equally far apart), ``scores`` float32
+    [n_reqs, n_beams] (-inf: an empty place), ``done`` uint8 of that shape or None; ``parent`` and ``token``
+    (int32), ``scores_out`` (float32) and ``done_out`` (uint8 or None): [n_reqs, keep], written, best
+    first.  ``parent`` counts sequences, request * n_beams + beam, as :func:`page_fork` takes them; -1
+    where fewer are offered.  ``ws``: a uint8 tensor of :func:`beam_select_workspace_bytes` bytes.
+    """
+    if parent.dim() != 2:
+        raise ValueError("parent must be [n_reqs, keep]")
+    shape = (logits.shape[0], parent.shape[1])
+    if not logits.is_cuda or logits.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"logits must be on the current device (they are on {logits.device})")
+    _need(scores, "scores", torch.float32, logits.shape[:2])
+    _need(parent, "parent", torch.int32, shape)
+    _need(token, "token", torch.int32, shape)
+    _need(scores_out, "scores_out", torch.float32, shape)
+    if done is not None:
+        _need(done, "done", torch.uint8, logits.shape[:2])
+    if done_out is not None:
+        _need(done_out, "done_out", torch.uint8, shape)
+    beams = _beams(logits, shape[1], scores, done, eos)
+    ws_ptr, nbytes = _workspace(ws, scores)
+    _check(_lib.ckv_beam_select(beams, _ptr(parent), _ptr(token), _ptr(scores_out), _ptr(done_out), ws_ptr, nbytes,
+                                _stream_on(logits.get_device(), stream)), "ckv_beam_select")

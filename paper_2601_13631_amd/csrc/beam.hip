@@ -1,0 +1,487 @@
+// beam.hip -- the continuations of beams for gfx950.
+//
+// A live beam's token v has score c + x_v - log sum_u exp(x_u); the `keep` best of a request's
+// beams go on.  Within a beam the scores fall with the logits, so the keep largest logits of
+// each beam are enough, and the logits are read once:
+//   beam_scan_kernel   a workgroup per slice of a beam's vocabulary: the sum of the exponentials
+//                      against the slice's maximum, and its keep largest logits
+//   beam_join_kernel   a workgroup per request: the slices of each beam, then the beams
+// The scan is bound by reading the logits.
+
+#include "ckv_internal.h"
+
+namespace ckv {
+namespace {
+
+constexpr int kMost = 64;  // beams of a request, and continuations that are kept: lanes of a wave
+constexpr float kLowest = -3.4028234663852886e38f;
+
+// A logit and its token as one number: larger for a larger logit, then for a lower token.
+// 0: none; numbers up to kNoKey are of logits that are -infinity.
+constexpr uint64_t kNoKey = uint64_t(0x007fffff) << 32 | 0xffffffffu;
+__device__ __forceinline__ uint64_t key_of(float x, int token) {
+  const uint32_t b = __float_as_uint(x + 0.f);  // (-0 is 0)
+  return join64(b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u), ~(uint32_t)token);
+}
+__device__ __forceinline__ float value_of(uint64_t key) {
+  const uint32_t b = (uint32_t)(key >> 32);
+  return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+}
+__device__ __forceinline__ int token_of_key(uint64_t key) { return (int)~(uint32_t)key; }
+
+// The key of lane ^ X.
+template <int X>
+__device__ __forceinline__ uint64_t other(uint64_t k) {
+  if constexpr (X == 1) return dpp64<kDppQuadXor1>(k);
+  if constexpr (X == 2) return dpp64<kDppQuadXor2>(k);
+  if constexpr (X == 4) return dpp64<0x1B>(dpp64<kDppRowHalfMirror>(k));  // (lane ^ 7) ^ 3
+  if constexpr (X == 8) return dpp64<0x128>(k);                           // rotated by 8 in 16
+  uint64_t a, b;
+  swap_pair64<X>(k, a, b);
+  return a ^ b ^ k;  // (a, b: own and partner's)
+}
+// One step of a bitonic network: of each pair lane, lane ^ X the lower lane of a descending
+// run keeps the larger.  Runs of R lanes alternate; the last ones go down, with kUp up.
+template <int X, int R, bool kUp>
+__device__ __forceinline__ uint64_t exchange(uint64_t k) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t o = other<X>(k);
+  const bool larger = (((lane & X) == 0) == ((lane & R) == 0)) != kUp;
+  return (k > o) == larger ? k : o;
+}
+template <int X, int R, bool kUp>
+__device__ __forceinline__ uint64_t merge_runs(uint64_t k) {
+  k = exchange<X, R, kUp>(k);
+  if constexpr (X > 1) k = merge_runs<X / 2, R, kUp>(k);
+  return k;
+}
+// A wave's 64 keys in descending (kUp: ascending) order.
+template <bool kUp>
+__device__ __forceinline__ uint64_t sorted(uint64_t k) {
+  k = merge_runs<1, 2, kUp>(k);
+  k = merge_runs<2, 4, kUp>(k);
+  k = merge_runs<4, 8, kUp>(k);
+  k = merge_runs<8, 16, kUp>(k);
+  k = merge_runs<16, 32, kUp>(k);
+  return merge_runs<32, 64, kUp>(k);
+}
+// The 64 largest of two runs, the first in descending, the second in ascending order.
+__device__ __forceinline__ uint64_t largest(uint64_t k, uint64_t ascending) {
+  return merge_runs<32, 64, false>(k > ascending ? k : ascending);
+}
+__device__ __forceinline__ uint64_t lane_of(uint64_t k, int lane) {  // (lane: one for the wave)
+  return join64((uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane),
+                (uint32_t)__builtin_amdgcn_readlane((int)k, lane));
+}
+
+// What the wave's lanes wrote to LDS is there for its other lanes.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+struct BeamArgs {
+  const char* logits;
+  const float* scores;
+  const uint8_t* done;
+  int64_t row_stride;  // elements
+  int32_t n_reqs, n_beams, vocab, keep, eos;
+  int32_t slices, slice;  // of a beam, and batches (of 64 lanes' pieces) of one
+  float* ref;             // [rows][slices]
+  double* sum;            // [rows][slices]
+  uint64_t* keys;         // [rows][slices][keep], descending, 0 behind the last
+  int32_t* parent;
+  int32_t* token;
+  float* score;
+  uint8_t* done_out;
+};
+
+constexpr int kWaves = 4;
+constexpr int kPieces = 4;  // 16-byte pieces of a lane per batch
+constexpr int64_t kScanBlocks = 1024;  // workgroups of a scan, about: 4 per CU
+constexpr int64_t kMaxScanGrid = int64_t(1) << 24;
+
+// 16 bytes from any element on.
+__device__ __forceinline__ u32x4 piece_at(const char* p) {
+  u32x4 x;
+  __builtin_memcpy(&x, p, sizeof x);
+  return x;
+}
+
+// An element of a piece (four words).
+template <bool kBf16>
+__device__ __forceinline__ float element(const uint32_t* w, int e) {
+  if constexpr (kBf16) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+  return __uint_as_float(w[e]);
+}
+
+// A wave goes over its batches, the next one's loads under way.  Of a batch, lanes take their
+// largest element; lanes that may hold one of the keep best put their elements into LDS,
+// where the wave looks at 64 of them at a time and collects those that do.  64 collected are
+// sorted and merged into the list that the lanes hold.  Typically few lanes have any.
+template <bool kBf16>
+__global__ __launch_bounds__(64 * kWaves) void beam_scan_kernel(BeamArgs a) {
+  constexpr int kPer = kBf16 ? 8 : 4, kBytes = kBf16 ? 2 : 4;  // elements of a piece, bytes of one
+  constexpr int kLane = kPieces * kPer;                        // elements of a lane per batch
+  constexpr int kWords = 4 * kPieces;
+  __shared__ uint32_t words[kWaves][64][kWords];  // elements of the lanes looked at
+  __shared__ int32_t lanes[kWaves][64];
+  __shared__ uint64_t found[kWaves][2 * 64];
+  __shared__ double sums[kWaves];
+  __shared__ float refs[kWaves];
+  const int64_t row = blockIdx.x / a.slices;
+  const int slice = blockIdx.x % a.slices;
+  const float c = a.scores[row];
+  if (!(c > -INFINITY) || (a.done && a.done[row])) return;  // offers no token: the join knows
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Pieces count from the row's begin, wherever that lies: rows of equal logits are then added up
+  // alike, and their scores tie as they should.
+  const char* const base = a.logits + row * a.row_stride * kBytes;
+  const int64_t end = a.vocab;
+  constexpr int64_t kBatch = 64 * kLane;
+  const int64_t batches = (end + kBatch - 1) / kBatch;
+  const int64_t b0 = (int64_t)slice * a.slice, b1 = min(b0 + a.slice, batches);
+  const int keep = a.keep;
+
+  using Batch = u32x4[kPieces];
+  auto load = [&](int64_t batch, Batch& x) __attribute__((always_inline)) {
+    const int64_t e0 = batch * kBatch;
+    if (e0 + kBatch <= end) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) x[i] = piece_at(base + (e0 + (int64_t)(i * 64 + lane) * kPer) * kBytes);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int64_t p0 = e0 + (i * 64 + lane) * kPer;
+      if (p0 + kPer <= end) {
+        x[i] = piece_at(base + p0 * kBytes);
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if constexpr (kBf16) {
+            uint32_t v[2] = {0xff80u, 0xff80u};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int64_t p = p0 + 2 * w + h;
+              if (p < end) v[h] = *reinterpret_cast<const uint16_t*>(base + p * 2);
+            }
+            x[i][w] = v[0] | v[1] << 16;
+          } else {
+            const int64_t p = p0 + w;
+            x[i][w] = p < end ? *reinterpret_cast<const uint32_t*>(base + p * 4) : 0xff800000u;
+          }
+        }
+      }
+    }
+  };
+
+  float ref;
+  double sum;
+  uint64_t list;  // this lane's of the 64 best so far
+  // `careful`: NaN is taken for -infinity and an infinity for the largest number.  They show
+  // in the sum, after which the slice is done again.
+  for (bool careful = false;; careful = true) {
+    ref = kLowest;
+    sum = 0;
+    list = 0;
+    uint64_t least = kNoKey + 1;  // what the best have at least
+    int n_found = 0;
+    auto flush = [&](int n) __attribute__((always_inline)) {  // the n <= 64 first ones found
+      wave_sync();
+      list = largest(list, sorted<true>(lane < n ? found[wave][lane] : 0));
+      wave_sync();
+      const uint64_t last = lane_of(list, keep - 1);
+      least = last > least ? last : least;
+    };
+    Batch x, next;
+    int64_t batch = b0 + wave;
+    if (batch < b1) load(batch, x);
+    for (; batch < b1; batch += kWaves) {
+      if (batch + kWaves < b1) load(batch + kWaves, next);
+      if (careful) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t v = x[i][w];
+            if constexpr (kBf16) {
+              uint32_t h[2] = {v & 0xffffu, v >> 16};
+#pragma unroll
+              for (int j = 0; j < 2; ++j) h[j] = (h[j] & 0x7fffu) > 0x7f80u ? 0xff80u : h[j] == 0x7f80u ? 0x7f7fu : h[j];
+              v = h[0] | h[1] << 16;
+            } else {
+              v = (v & 0x7fffffffu) > 0x7f800000u ? 0xff800000u : v == 0x7f800000u ? 0x7f7fffffu : v;
+            }
+            x[i][w] = v;
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const uint32_t w[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) mx = fmaxf(mx, element<kBf16>(w, e));
+      }
+      if (__any(mx > ref)) {
+        float to = mx;
+#pragma unroll
+        for (int i = 1; i < 64; i <<= 1) to = fmaxf(to, __shfl_xor(to, i));
+        sum *= (double)__builtin_amdgcn_exp2f((ref - to) * 1.4426950408889634f);
+        ref = to;
+      }
+      // the difference first: it is exact for logits near the maximum, whose terms count
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const uint32_t w[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+          part[e & 3] += __builtin_amdgcn_exp2f((element<kBf16>(w, e) - ref) * 1.4426950408889634f);
+      }
+      sum += (double)((part[0] + part[1]) + (part[2] + part[3]));
+
+      // (the threshold as a logit: a little wide where tokens decide)
+      const float at_least = value_of(least);
+      uint64_t hit = __ballot(mx >= at_least);
+      if (hit) {
+        if (__builtin_popcountll(hit) >= keep) {
+          // keep lanes have an element each that is no less than the keep-th lane's largest
+          const float kth = value_of(lane_of(sorted<false>(key_of(mx, lane)), keep - 1));
+          hit = __ballot(mx >= kth && mx >= at_least);
+          const uint64_t bound = key_of(kth, 0x7fffffff);
+          least = bound > least ? bound : least;
+        }
+        if (hit >> lane & 1) {
+          const int at = __builtin_popcountll(hit & ((1ull << lane) - 1));
+          lanes[wave][at] = lane;
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) *reinterpret_cast<u32x4*>(&words[wave][at][4 * i]) = x[i];
+        }
+        wave_sync();
+        const int total = __builtin_popcountll(hit) * kLane;
+        for (int at = lane; at - lane < total; at += 64) {
+          const int l = min(at / kLane, 63), e = at % kLane, i = e / kPer;
+          const float v = element<kBf16>(&words[wave][l][4 * i], e % kPer);
+          const int64_t token = batch * kBatch + (int64_t)(i * 64 + lanes[wave][l]) * kPer + e % kPer;
+          const uint64_t k = key_of(v, (int)token);
+          const uint64_t yes = __ballot(at < total && k >= least && v > -INFINITY);
+          if (!yes) continue;
+          if (yes >> lane & 1) found[wave][n_found + __builtin_popcountll(yes & ((1ull << lane) - 1))] = k;
+          n_found += __builtin_popcountll(yes);
+          if (n_found >= 64) {
+            flush(64);
+            n_found -= 64;
+            const uint64_t rest = found[wave][64 + lane];
+            wave_sync();
+            found[wave][lane] = rest;
+          }
+        }
+        wave_sync();
+      }
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) x[i] = next[i];
+    }
+    if (n_found > 0) flush(n_found);
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
+    if (careful || !__any(!__builtin_isfinite(sum))) break;
+  }
+
+  // the waves' parts
+  __syncthreads();
+  uint64_t(&lists)[kWaves][64] = *reinterpret_cast<uint64_t(*)[kWaves][64]>(&words[0][0][0]);
+  lists[wave][lane] = list;
+  if (lane == 0) {
+    sums[wave] = sum;
+    refs[wave] = ref;
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  float top = refs[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, refs[w]);
+  sum = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w)
+    sum += sums[w] * (double)__builtin_amdgcn_exp2f((refs[w] - top) * 1.4426950408889634f);
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) list = largest(list, lists[w][63 - lane]);
+  const int64_t at = row * a.slices + slice;
+  if (lane == 0) {
+    a.ref[at] = top;
+    a.sum[at] = sum;
+  }
+  if (lane < keep) a.keys[at * keep + lane] = list;
+}
+
+// A wave per beam in turn joins its slices' sums and lists; then the beams' lists, which fall,
+// are merged by counting what goes before each entry: equal scores go to the lower beam.
+constexpr int kJoinWaves = 8;
+__global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a) {
+  extern __shared__ double scores[];  // [n_beams][keep], then tokens, then entries of each beam
+  int32_t* const tokens = reinterpret_cast<int32_t*>(scores + a.n_beams * a.keep);
+  int32_t* const entries = tokens + a.n_beams * a.keep;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row0 = (int64_t)blockIdx.x * a.n_beams;
+  const int keep = a.keep;
+  for (int b = wave; b < a.n_beams; b += kJoinWaves) {
+    const int64_t row = row0 + b, at = row * a.slices;
+    const float c = a.scores[row];
+    const bool live = c > -INFINITY, done = live && a.done && a.done[row];
+    int n = 0;
+    if (done) {
+      n = 1;
+      if (lane == 0) {
+        scores[b * keep] = (double)c;
+        tokens[b * keep] = a.eos;
+      }
+    } else if (live) {
+      const uint64_t* const keys = a.keys + at * keep;
+      const int up = 63 - lane;
+      uint64_t list = lane < keep ? keys[lane] : 0, next = a.slices > 1 && up < keep ? keys[keep + up] : 0;
+      const float ref = lane < a.slices ? a.ref[at + lane] : kLowest;
+      double sum = lane < a.slices ? a.sum[at + lane] : 0;
+      float top = ref;
+#pragma unroll
+      for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+      sum *= exp((double)ref - (double)top);
+#pragma unroll
+      for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
+      for (int s = 1; s < a.slices; ++s) {
+        const uint64_t x = next;
+        next = s + 1 < a.slices && up < keep ? keys[(int64_t)(s + 1) * keep + up] : 0;
+        list = largest(list, x);
+      }
+      // A whole number of 2^-40, finer than the exponentials are: what is added to it in 64 bits
+      // (logits and scores below 2^12 that are whole numbers of it as well) is added exactly, so
+      // that scores which are equal by arithmetic compare equal.
+      const double all = rint(((double)top + log(sum)) * 0x1p40) * 0x1p-40;
+      n = __builtin_popcountll(__ballot(lane < keep && list != 0));
+      if (lane < n) {
+        scores[b * keep + lane] = ((double)value_of(list) - all) + (double)c;
+        tokens[b * keep + lane] = token_of_key(list);
+      }
+    }
+    if (lane == 0) entries[b] = n;
+  }
+  __syncthreads();
+  int total = 0;
+  for (int b = 0; b < a.n_beams; ++b) total += entries[b];
+  const int64_t out0 = (int64_t)blockIdx.x * keep;
+  for (int i = threadIdx.x; i < a.n_beams * keep; i += 64 * kJoinWaves) {
+    const int b = i / keep;
+    if (i % keep >= entries[b]) continue;
+    const double s = scores[i];
+    int rank = i % keep;
+    for (int o = 0; o < a.n_beams && rank < keep; ++o) {
+      if (o == b) continue;
+      int lo = 0, hi = entries[o];  // the first entry of beam o that does not go before
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const double x = scores[o * keep + mid];
+        if (x > s || (x == s && o < b))
+          lo = mid + 1;
+        else
+          hi = mid;
+      }
+      rank += lo;
+    }
+    if (rank >= keep) continue;
+    const int64_t row = row0 + b;
+    a.parent[out0 + rank] = (int32_t)row;
+    a.token[out0 + rank] = tokens[i];
+    a.score[out0 + rank] = (float)s;
+    if (a.done_out) a.done_out[out0 + rank] = tokens[i] == a.eos || (a.done && a.done[row]) ? 1 : 0;
+  }
+  for (int i = total + (int)threadIdx.x; i < keep; i += 64 * kJoinWaves) {
+    a.parent[out0 + i] = -1;
+    a.token[out0 + i] = -1;
+    a.score[out0 + i] = -INFINITY;
+    if (a.done_out) a.done_out[out0 + i] = 0;
+  }
+}
+
+struct BeamPlan {
+  int32_t slices, slice;
+  size_t off_sum, off_keys, bytes;
+};
+
+BeamPlan make_beam_plan(const ckv_beams* b) {
+  BeamPlan p{};
+  const int64_t rows = (int64_t)b->n_reqs * b->n_beams;
+  const int64_t batch = 64 * kPieces * (b->dtype == CKV_DTYPE_BF16 ? 8 : 4);
+  const int64_t batches = ceil_div(b->vocab, batch);
+  const int64_t most = std::min<int64_t>(kMost, ceil_div(batches, kWaves));
+  const int64_t want = std::max<int64_t>(1, std::min(most, ceil_div(kScanBlocks, std::max<int64_t>(rows, 1))));
+  p.slice = (int32_t)ceil_div(batches, want);
+  p.slices = (int32_t)ceil_div(batches, p.slice);
+  p.off_sum = align_up((size_t)rows * p.slices * sizeof(float), 256);
+  p.off_keys = align_up(p.off_sum + (size_t)rows * p.slices * sizeof(double), 256);
+  p.bytes = align_up(p.off_keys + (size_t)rows * p.slices * b->keep * sizeof(uint64_t), 256);
+  return p;
+}
+
+ckv_status check_beams(const ckv_beams* b, bool with_pointers) {
+  if (!b) CKV_FAIL(CKV_EINVAL, "beams is NULL");
+  if (b->dtype != CKV_DTYPE_F32 && b->dtype != CKV_DTYPE_BF16) CKV_FAIL(CKV_EINVAL, "logits are fp32 or bf16");
+  if (b->n_reqs < 0 || b->n_reqs > (1 << 20))
+    CKV_FAIL(CKV_EINVAL, "n_reqs must be in [0, 2^20] (got %d)", b->n_reqs);
+  if (b->n_beams < 1 || b->keep < 1) CKV_FAIL(CKV_EINVAL, "n_beams and keep must be >= 1");
+  if (b->n_beams > kMost || b->keep > kMost)
+    CKV_FAIL(CKV_EUNSUPPORTED, "more than %d beams or continuations (%d, %d)", kMost, b->n_beams, b->keep);
+  if ((int64_t)b->n_reqs * b->n_beams > (1 << 20)) CKV_FAIL(CKV_EUNSUPPORTED, "more than 2^20 beams in one call");
+  if (b->vocab < 1) CKV_FAIL(CKV_EINVAL, "vocab must be >= 1 (got %d)", b->vocab);
+  if (b->vocab > (1 << 30)) CKV_FAIL(CKV_EUNSUPPORTED, "vocab past 2^30");
+  if (b->row_stride != 0 && (b->row_stride < b->vocab || b->row_stride > (int64_t(1) << 40)))
+    CKV_FAIL(CKV_EINVAL, "row_stride must be 0 or at least vocab");
+  if (b->eos < -1 || b->eos >= b->vocab) CKV_FAIL(CKV_EINVAL, "eos must be -1 or below vocab (got %d)", b->eos);
+  if (b->done && b->eos < 0) CKV_FAIL(CKV_EINVAL, "beams that are done need eos");
+  if (!with_pointers || b->n_reqs == 0) return CKV_OK;
+  if (!b->logits || !b->scores) CKV_FAIL(CKV_EINVAL, "NULL beams pointer");
+  if (reinterpret_cast<uintptr_t>(b->logits) % elem_bytes(b->dtype))
+    CKV_FAIL(CKV_EINVAL, "logits must be aligned to an element");
+  return CKV_OK;
+}
+
+}  // namespace
+}  // namespace ckv
+
+using namespace ckv;
+
+extern "C" {
+
+size_t ckv_beam_select_workspace_bytes(const ckv_beams* beams) {
+  return check_beams(beams, false) == CKV_OK ? make_beam_plan(beams).bytes : 0;
+}
+
+ckv_status ckv_beam_select(const ckv_beams* beams, int32_t* parent, int32_t* token, float* score, uint8_t* done,
+                           void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  if (ckv_status s = check_beams(beams, true); s != CKV_OK) return s;
+  if (beams->n_reqs == 0) return CKV_OK;
+  if (!parent || !token || !score || !ws) CKV_FAIL(CKV_EINVAL, "NULL pointer argument");
+  const BeamPlan p = make_beam_plan(beams);
+  if (ws_bytes < p.bytes) CKV_FAIL(CKV_EINVAL, "workspace too small: %zu < %zu", ws_bytes, p.bytes);
+  if (!aligned16(ws)) CKV_FAIL(CKV_EINVAL, "pointers must be 16-byte aligned");
+  char* const w = static_cast<char*>(ws);
+  const BeamArgs a{static_cast<const char*>(beams->logits), beams->scores, beams->done,
+                   beams->row_stride ? beams->row_stride : beams->vocab, beams->n_reqs, beams->n_beams,
+                   beams->vocab, beams->keep, beams->eos, p.slices, p.slice, reinterpret_cast<float*>(w),
+                   reinterpret_cast<double*>(w + p.off_sum), reinterpret_cast<uint64_t*>(w + p.off_keys),
+                   parent, token, score, done};
+  const int64_t grid = (int64_t)beams->n_reqs * beams->n_beams * p.slices;
+  if (grid >= kMaxScanGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
+  const hipStream_t st = (hipStream_t)stream;
+  if (beams->dtype == CKV_DTYPE_BF16)
+    hipLaunchKernelGGL(beam_scan_kernel<true>, dim3((unsigned)grid), dim3(64 * kWaves), 0, st, a);
+  else
+    hipLaunchKernelGGL(beam_scan_kernel<false>, dim3((unsigned)grid), dim3(64 * kWaves), 0, st, a);
+  CKV_HIP(hipGetLastError());
+  const size_t lds = (size_t)a.n_beams * (a.keep * (sizeof(double) + sizeof(int32_t)) + sizeof(int32_t));
+  hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)beams->n_reqs), dim3(64 * kJoinWaves), lds, st, a);
+  CKV_HIP(hipGetLastError());
+  return CKV_OK;
+}
+
+}  // extern "C"

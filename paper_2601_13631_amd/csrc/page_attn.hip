@@ -23,6 +23,8 @@
 // 239 to 254 us by the card, 955 to 1,010 TFLOP/s, in bf16 and 8 bits alike (a matrix product of
 // 8,192 reaches 1,210 to 1,230); five prompts of up to 2,048 tokens with a window of 1,000 130 us, 766.
 
+#include <type_traits>
+
 #include "attn_tile.h"
 #include "pages_internal.h"
 
@@ -56,7 +58,75 @@ struct PageAttnArgs {
   uint32_t n_blocks;    // blocks of 128 rows, at most (page_tile_kernel)
   int slice;            // steps that a sequence takes another split for
   float c1;
+  // groups that share a prefix (parts below)
+  const int32_t* grp_off;  // [n_groups + 1]
+  const int32_t* shared;   // [n_groups] tokens, [n_groups] leaders, [n_seqs] tokens
+  int n_groups;
+  const int32_t* shared_parts;  // the join: splits of the shared keys by token
+  int shared_splits;            //   and the places that they have
 };
+
+// What a launch attends over: whole sequences; or, where groups of them share a prefix, in one
+// launch the shared keys for all rows of a group, in another each sequence's own keys behind
+// them.  The parts meet in the join of the splits.
+enum Part { kWhole, kShared, kOwn };
+
+// The rows and keys of one unit of a launch's work: a sequence, or a group (kShared), whose
+// rows are those of its sequences.
+struct Unit {
+  SeqSpan sp;          // its token rows
+  const int32_t* tab;  // its table
+  int first, kv_end;   // its keys' positions; `first` is a whole number of kTile
+  int p_base;          // the first row's position
+};
+template <int P>
+__device__ __forceinline__ int n_units(const PageAttnArgs& a) {
+  return P == kShared ? a.n_groups : a.s.n_seqs;
+}
+// The first sequence of a group, inside the batch whatever grp_off holds.
+__device__ __forceinline__ int group_begin(const PageAttnArgs& a, int g) {
+  return min(max(a.grp_off[g], 0), a.s.n_seqs);
+}
+template <int P>
+__device__ __forceinline__ int64_t unit_token(const PageAttnArgs& a, int u) {
+  return token_of(a.s, P == kShared ? group_begin(a, u) : u);
+}
+// Shared tokens as ckv_page_share left them, inside the table whatever they are.
+__device__ __forceinline__ int shared_tokens(const PageAttnArgs& a, int at) {
+  return (int)min((int64_t)max(a.shared[at], 0), (int64_t)a.s.max_pages * a.c) & ~31;
+}
+template <int P>
+__device__ __forceinline__ Unit unit_of(const PageAttnArgs& a, int u) {
+  Unit x;
+  if constexpr (P == kShared) {
+    const int64_t lo = unit_token<P>(a, u), hi = unit_token<P>(a, u + 1);
+    x.kv_end = shared_tokens(a, u);
+    x.p_base = x.kv_end;  // past every key: nothing is hidden
+    x.sp = SeqSpan{lo, (int32_t)max<int64_t>(hi - lo, 0), x.kv_end};
+    x.tab = a.s.table + (int64_t)min(max(a.shared[a.n_groups + u], 0), a.s.n_seqs - 1) * a.s.table_stride;
+    x.first = 0;
+  } else {
+    x.sp = seq_span(a.s, u);
+    x.tab = a.s.table + (int64_t)u * a.s.table_stride;
+    x.kv_end = (int)min<int64_t>(max(x.sp.len, 0), (int64_t)a.s.max_pages * a.c);
+    x.first = P == kOwn ? shared_tokens(a, 2 * a.n_groups + u) : 0;
+    x.p_base = x.sp.len - x.sp.count;
+  }
+  return x;
+}
+// Splits of a unit of so many steps.  A whole sequence without a key has one, which writes its
+// rows' zeros; a part that another one completes has none.
+template <int P>
+__device__ __forceinline__ int parts_of(const PageAttnArgs& a, const Unit& x, int steps) {
+  const int least = P == kWhole || (P == kOwn && x.first == 0) ? 1 : 0;
+  return min(max((steps + a.slice - 1) / a.slice, least), a.n_splits);
+}
+// What the join reads of a token's sequence: its splits and, of kOwn, whether shared ones go before.
+constexpr int kAfterShared = 1 << 30;
+template <int P>
+__device__ __forceinline__ int parts_note(const Unit& x, int n_parts) {
+  return P == kOwn && x.first > 0 ? n_parts | kAfterShared : n_parts;
+}
 
 // The keys of a block of rows as steps of kTile: those that hold the sinks, then those
 // from the window's begin on.
@@ -65,12 +135,13 @@ struct Steps {
   __device__ __forceinline__ int tile(int i) const { return i < n_sink ? i : first + (i - n_sink); }
 };
 // For queries at positions p0 .. p1 of a sequence with keys below kv_end.
-__device__ __forceinline__ Steps steps_of(const PageAttnArgs& a, int p0, int p1, int kv_end) {
-  Steps s{0, 0, 0};
+template <int P>
+__device__ __forceinline__ Steps steps_of(const PageAttnArgs& a, int p0, int p1, int first, int kv_end) {
+  Steps s{0, P == kOwn ? first / kTile : 0, 0};
   const int hi = min(p1 + 1, kv_end);
   if (hi <= 0) return s;
   const int tiles = (hi + kTile - 1) / kTile;
-  if (a.window > 0) {
+  if (P == kWhole && a.window > 0) {
     const int lo = max(p0 - a.window + 1, 0);
     s.n_sink = (min(min(a.sinks, lo), hi) + kTile - 1) / kTile;
     s.first = max(lo / kTile, s.n_sink);
@@ -85,11 +156,12 @@ struct Groups {
   int n_sink, first, n;
   __device__ __forceinline__ int pos(int i) const { return 8 * (i < n_sink ? i : first + (i - n_sink)); }
 };
-__device__ __forceinline__ Groups groups_of(const PageAttnArgs& a, int p0, int p1, int kv_end) {
-  Groups s{0, 0, 0};
+template <int P>
+__device__ __forceinline__ Groups groups_of(const PageAttnArgs& a, int p0, int p1, int first, int kv_end) {
+  Groups s{0, P == kOwn ? first / 8 : 0, 0};
   const int hi = min(p1 + 1, kv_end);
   if (hi <= 0) return s;
-  if (a.window > 0) {
+  if (P == kWhole && a.window > 0) {
     const int lo = max(p0 - a.window + 1, 0);
     s.n_sink = (min(min(a.sinks, lo), hi) + 7) / 8;
     s.first = max(lo / 8, s.n_sink);
@@ -198,7 +270,7 @@ __device__ __forceinline__ uint32_t finite_codes(uint32_t w) {
 // sequence of 1,000 tokens takes 6.6 us: four dependent round trips, two steps per wave of 0.9,
 // the waves' join 0.4.
 // kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page).
-template <int D, int T, bool kSmall, int kWaves>
+template <int D, int T, bool kSmall, int kWaves, int P>
 __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(PageAttnArgs a) {
   using E = Elem<T>;
   using QT = typename E::Q;
@@ -211,25 +283,26 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
   // The KV heads of one slice of keys are neighbours on one XCD, where together they read
   // whole token rows.  The slices go round the XCDs, every sequence's first ones before the
   // second ones and so on, turned by one from split to split: long sequences spread.
-  const uint32_t pair = blockIdx.x / 8 / a.Hkv * 8 + (blockIdx.x & 7);
-  if (pair >= (uint32_t)a.s.n_seqs * a.n_splits) return;
-  const int g = (int)(blockIdx.x / 8 % a.Hkv), split = (int)(pair / a.s.n_seqs);
-  const int b = (int)((pair + split) % a.s.n_seqs);
+  const uint32_t pair = blockIdx.x / 8 / a.Hkv * 8 + (blockIdx.x & 7), units = n_units<P>(a);
+  if (pair >= units * a.n_splits) return;
+  const int g = (int)(blockIdx.x / 8 % a.Hkv), split = (int)(pair / units);
+  const int b = (int)((pair + split) % units);
   const int lane = threadIdx.x & 63, n16 = lane & 15, j4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const SeqSpan sp = seq_span(a.s, b);
+  const Unit unit = unit_of<P>(a, b);
+  const SeqSpan& sp = unit.sp;
   if (sp.count == 0) return;
-  const int32_t* tab = a.s.table + (int64_t)b * a.s.table_stride;
-  const int kv_end = (int)min<int64_t>(max(sp.len, 0), (int64_t)a.s.max_pages * a.c);
+  const int32_t* tab = unit.tab;
+  const int kv_end = unit.kv_end;
   const int row_bytes = a.Hkv * kRow, kvh = g, g_bytes = g * kRow;
   const int rows = sp.count * a.G;
-  const int p_base = sp.len - sp.count;
+  const int p_base = unit.p_base;
   // this sequence's own number of splits, by its length
-  const int all_steps = steps_of(a, p_base, p_base + sp.count - 1, kv_end).n;
-  const int n_parts = min(max((all_steps + a.slice - 1) / a.slice, 1), a.n_splits);
+  const int all_steps = steps_of<P>(a, p_base, p_base + sp.count - 1, unit.first, kv_end).n;
+  const int n_parts = parts_of<P>(a, unit, all_steps);
+  if ((P != kWhole || a.n_splits > 1) && split == 0 && g == 0 && blockIdx.y == 0)
+    for (int i = threadIdx.x; i < sp.count; i += 64 * kWaves) a.n_parts[sp.first + i] = parts_note<P>(unit, n_parts);
   if (split >= n_parts) return;
-  if (a.n_splits > 1 && split == 0 && g == 0 && blockIdx.y == 0)
-    for (int i = threadIdx.x; i < sp.count; i += 64 * kWaves) a.n_parts[sp.first + i] = n_parts;
 
   // the waves' K buffers, and after the last step their outputs
   struct Joined {
@@ -259,7 +332,7 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
   for (int rb = blockIdx.y; rb * kRows < rows; rb += gridDim.y) {
     const int r_first = rb * kRows, r_last = min(rows, r_first + kRows) - 1;
     const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
-    const Steps steps = steps_of(a, p0, p1, kv_end);
+    const Steps steps = steps_of<P>(a, p0, p1, unit.first, kv_end);
     const int per = steps.n / n_parts, over = steps.n % n_parts;  // the first `over` splits: one more
     const int begin = split * per + min(split, over), end = begin + per + (split < over ? 1 : 0);
 
@@ -621,7 +694,7 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
         for (int w = 0; w < kWaves; ++w) acc[x] += f[w] * joined.o[w][row][col + x];
       }
       const int64_t at = (sp.first + rr / a.G) * a.Hq + g * a.G + rr % a.G;
-      if (n_parts > 1) {
+      if (P == kShared || n_parts > 1 || (P == kOwn && unit.first > 0)) {
         const int64_t prow = (int64_t)split * a.s.n_tokens * a.Hq + at;
         float* dst = a.o_part + prow * D + col;
 #pragma unroll
@@ -686,7 +759,7 @@ __device__ __forceinline__ void rounded_step(f32x16& s, float c1, float m, float
 // products to the exponentials), pages found by the lanes for the 64 groups of 8 stages at
 // once (for a stage: 258 us where this took 243), masks and their conditions in the stages
 // that need some only (243 -> 235), and conversions beside the first run of products.
-template <int D, int T>
+template <int D, int T, int P>
 __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   using namespace tile;
   using St = Stage<D>;
@@ -718,26 +791,28 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   const int g = (int)(stream % a.Hkv), split = (int)(stream / a.Hkv);
   // n tokens of a sequence are ceil(n G / 128) blocks: numbered from floor(t G / 128) + 1 per
   // sequence before, t its first token
-  const auto block_start = [&](int q) { return token_of(a.s, q) * a.G / kBlockRows + q; };
+  const auto block_start = [&](int q) { return unit_token<P>(a, q) * a.G / kBlockRows + q; };
   const int64_t block = a.n_blocks - 1 - blk;
-  const int b = find_seq(a.s, block, block_start);
+  const int b = find_seq(n_units<P>(a), block, block_start);
   if (b < 0) return;
-  const SeqSpan sp = seq_span(a.s, b);
+  const Unit unit = unit_of<P>(a, b);
+  const SeqSpan& sp = unit.sp;
   const int rb = (int)(block - block_start(b));
   if ((int64_t)rb * kBlockRows >= (int64_t)sp.count * a.G) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t* tab = a.s.table + (int64_t)b * a.s.table_stride;
-  const int kv_end = (int)min<int64_t>(max(sp.len, 0), (int64_t)a.s.max_pages * a.c);
+  const int32_t* tab = unit.tab;
+  const int kv_end = unit.kv_end;
   const int rows = sp.count * a.G, r_first = rb * kBlockRows, r_last = min(rows, r_first + kBlockRows) - 1;
-  const int p_base = sp.len - sp.count;
+  const int p_base = unit.p_base;
   const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
-  const int all_steps = (groups_of(a, p_base, p_base + sp.count - 1, kv_end).n + 7) / 8;
-  const int n_parts = min(max((all_steps + a.slice - 1) / a.slice, 1), a.n_splits);
+  const int all_steps = (groups_of<P>(a, p_base, p_base + sp.count - 1, unit.first, kv_end).n + 7) / 8;
+  const int n_parts = parts_of<P>(a, unit, all_steps);
+  if ((P != kWhole || a.n_splits > 1) && split == 0 && g == 0)
+    for (int i = r_first / a.G + (int)threadIdx.x; i <= r_last / a.G; i += 256)
+      a.n_parts[sp.first + i] = parts_note<P>(unit, n_parts);
   if (split >= n_parts) return;
-  if (a.n_splits > 1 && split == 0 && g == 0)
-    for (int i = r_first / a.G + (int)threadIdx.x; i <= r_last / a.G; i += 256) a.n_parts[sp.first + i] = n_parts;
-  const Groups groups = groups_of(a, p0, p1, kv_end);  // a stage: 8 of them
+  const Groups groups = groups_of<P>(a, p0, p1, unit.first, kv_end);  // a stage: 8 of them
   const int stages = (groups.n + 7) / 8;
   const int per = stages / n_parts, over = stages % n_parts;  // the first `over` splits: one more
   const int begin = split * per + min(split, over), end = begin + per + (split < over ? 1 : 0);
@@ -1099,7 +1174,7 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   }
 
   // o[db][v] holds d = 32*db + 8*(v/4) + 4*half + v%4 of this lane's row
-  if (n_parts > 1) {
+  if (P == kShared || n_parts > 1 || (P == kOwn && unit.first > 0)) {
     if (!row_ok) return;
     // The sum in [1, 2), so that outputs are of V's size whatever the reference was.
     const int e = l[0] > 0.f ? (int)(__float_as_uint(l[0]) >> 23) - 127 : 0;
@@ -1142,8 +1217,9 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
 // a thread, and meet in LDS, all in a fixed order.  One group (and several rows per
 // workgroup) up to kJoinBatch splits, whose loads are all in flight together; else the
 // whole workgroup.
+// kParts: the first `shared_splits` places are of the shared keys, the others of the sequences' own.
 constexpr int kJoinBatch = 8;
-template <int D, class QT, int kGroups>
+template <int D, class QT, int kGroups, bool kParts>
 __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
   constexpr int kCols = D / 4, kRowsPer = 256 / kCols / kGroups;
   const int64_t n_rows = a.s.n_tokens * a.Hq;
@@ -1165,8 +1241,17 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
   // the first splits come together with the number of them (those past it hold anything)
   load(grp, a.n_splits);
   const int first_tok = a.s.tok_off[0], end_tok = a.s.tok_off[a.s.n_seqs];
-  const int n_parts = min(a.n_parts[tok], a.n_splits);
-  if (tok < first_tok || tok >= end_tok || n_parts <= 1) return;  // of no sequence, or written already
+  int n_parts, n_shared = 0, own_from = 0;  // places [0, n_shared) and [own_from, n_parts) are this row's
+  if constexpr (kParts) {
+    const int own = a.n_parts[tok], shared = a.shared_parts[tok];
+    own_from = a.shared_splits;
+    n_parts = own_from + min(own & (kAfterShared - 1), a.n_splits - own_from);
+    n_shared = own & kAfterShared ? min(shared, own_from) : 0;
+    if (tok < first_tok || tok >= end_tok || (!(own & kAfterShared) && n_parts - own_from <= 1)) return;
+  } else {
+    n_parts = min(a.n_parts[tok], a.n_splits);
+    if (tok < first_tok || tok >= end_tok || n_parts <= 1) return;  // of no sequence, or written already
+  }
   float M = kNone, L = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
   for (int s0 = grp; s0 < n_parts; s0 += kGroups * kJoinBatch) {
@@ -1174,7 +1259,8 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
     float to = M;
 #pragma unroll
     for (int k = 0; k < kJoinBatch; ++k) {
-      if (s0 + k * kGroups >= n_parts) {
+      const int at = s0 + k * kGroups;
+      if (at >= n_parts || (kParts && at >= n_shared && at < own_from)) {
         ml[k] = make_float2(kNone, 0.f);
         x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
@@ -1220,6 +1306,9 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
     *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(y);
 }
 
+// Bytes of shared pages read again and again that are worth the parts' launch and join.
+constexpr int64_t kWorthParts = int64_t(24) << 20;
+
 struct PageAttnPlan {
   bool wide;       // page_tile_kernel
   int n_splits, slice;
@@ -1228,18 +1317,26 @@ struct PageAttnPlan {
   size_t off_ml, off_n, bytes;
 };
 
-PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq, int window, int sinks) {
+// About the most rows' tokens of one of n_units units: some unit has at least the mean,
+// whatever the caller says (0: not known).
+int64_t most_tokens(int64_t said, int64_t n_tokens, int n_units) {
+  return said > 0 ? std::min(std::max<int64_t>(said, ceil_div(n_tokens, std::max(n_units, 1))), n_tokens) : n_tokens;
+}
+int64_t longest(const ckv_page_pool* pool, const ckv_page_batch* b) {
+  const int64_t len = (int64_t)b->max_pages * pool->page_size;
+  return b->max_len > 0 ? std::min<int64_t>(len, b->max_len) : len;
+}
+
+// The launch for n_units units of up to `most` of the n_tokens tokens, which see up to `len`
+// keys; tile_blocks: about how many blocks of 128 rows they are.
+PageAttnPlan plan_units(const ckv_page_pool* pool, int Hq, int n_units, int64_t n_tokens, int64_t most, int64_t len,
+                        int64_t tile_blocks, int window, int sinks) {
   PageAttnPlan p{};
   const int G = Hq / pool->n_kv_heads;
-  // (some sequence has at least the mean, whatever max_tokens says)
-  const int64_t most = b->max_tokens > 0 ? std::min(std::max<int64_t>(b->max_tokens, ceil_div(b->n_tokens, std::max(b->n_seqs, 1))), b->n_tokens)
-                                         : b->n_tokens;
-  int64_t len = (int64_t)b->max_pages * pool->page_size;
-  if (b->max_len > 0) len = std::min<int64_t>(len, b->max_len);
   // (both sides: top of the file; one kernel for the call, by its longest sequence)
   p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32;
   if (p.wide) {
-    p.blocks = b->n_tokens * G / tile::kBlockRows + b->n_seqs;
+    p.blocks = n_tokens * G / tile::kBlockRows + n_units;
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + ceil_div(tile::kBlockRows, G) + sinks + 16);
     const int64_t steps = ceil_div(len, tile::kTile);
     // The splits that cost least by a model of the launch, in cycles at 1.85 GHz: 512
@@ -1249,9 +1346,8 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
     // one split, 1,148 in 4, 1,125 in 6; after a window of 1,000: 67 us in one, 86 in 2.)
     constexpr double kFixed = 15000, kStage = 3440, kFixedAlone = 12500, kStageAlone = 2100;
     constexpr double kJoin = 5500, kJoinBytes = 2500;
-    // (sequences' last blocks are taken as full: many short ones are more workgroups than this)
-    const int64_t wgs = (b->n_tokens * G / tile::kBlockRows + 1) * pool->n_kv_heads;
-    const double join = (double)b->n_tokens * Hq * pool->head_dim * 2 * sizeof(float) / kJoinBytes;
+    const int64_t wgs = tile_blocks * pool->n_kv_heads;
+    const double join = (double)n_tokens * Hq * pool->head_dim * 2 * sizeof(float) / kJoinBytes;
     double best = 0;
     for (int64_t n0 = 1; n0 <= 64 && n0 * 4 <= std::max<int64_t>(steps, 4); ++n0) {
       const int64_t per = ceil_div(steps, n0), n = ceil_div(steps, per), rem = wgs * n % 512;
@@ -1269,20 +1365,65 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
     p.row_blocks = (int)std::min<int64_t>(65535, std::max<int64_t>(1, ceil_div(most * G, kRows)));
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + most + sinks + 2 * kTile);
     const int64_t steps = ceil_div(len, kTile);
-    const int64_t wgs = (int64_t)b->n_seqs * pool->n_kv_heads * p.row_blocks;
+    const int64_t wgs = (int64_t)n_units * pool->n_kv_heads * p.row_blocks;
     // Splits of 16 steps or more (a sequence of 1,026 steps: 14.0 us; of 12: 15.8, of 24: 14.5),
     // up to 4,096 workgroups, so that sequences of unequal lengths spread over the chip (64
     // of 1,024 to 16,384 tokens: 165 us; up to 2,048: 183, up to 8,192: 170).
     p.n_splits = (int)std::max<int64_t>(1, std::min(4096 / std::max<int64_t>(wgs, 1), steps / 16));
     p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
   }
+  if (n_tokens * Hq >= kMaxGrid) p.n_splits = 1;  // (the join has a workgroup per row)
+  return p;
+}
+
+PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq, int window, int sinks) {
+  // (sequences' last blocks are taken as full: many short ones are more workgroups than this)
+  const int64_t blocks = b->n_tokens * (Hq / pool->n_kv_heads) / tile::kBlockRows + 1;
+  PageAttnPlan p = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most_tokens(b->max_tokens, b->n_tokens, b->n_seqs),
+                              longest(pool, b), blocks, window, sinks);
   const size_t rows = (size_t)b->n_tokens * Hq;
-  if (rows >= (size_t)kMaxGrid) p.n_splits = 1;  // (the join has a workgroup per row)
   if (p.n_splits > 1) {
     p.off_ml = align_up((size_t)p.n_splits * rows * pool->head_dim * sizeof(float), 256);
     p.off_n = align_up(p.off_ml + (size_t)p.n_splits * rows * sizeof(float2), 256);
     p.bytes = align_up(p.off_n + (size_t)b->n_tokens * sizeof(int32_t), 256);
   }
+  return p;
+}
+
+// Attention of groups: a launch over the shared keys, one over the sequences' own, the join.
+struct SharedPlan {
+  bool apart;  // false: every sequence by itself is less work than the parts and their join
+  PageAttnPlan whole, shared, own;
+  size_t off_ml, off_shared, off_own, bytes;
+};
+
+SharedPlan make_shared_plan(const ckv_page_pool* pool, const ckv_page_batch* b, const ckv_page_groups* g, int Hq) {
+  SharedPlan p{};
+  const int G = Hq / pool->n_kv_heads;
+  const int64_t len = longest(pool, b);
+  const int64_t shared_len = g->max_shared > 0 ? std::min<int64_t>(len, g->max_shared) : len;
+  const int64_t most = most_tokens(b->max_tokens, b->n_tokens, b->n_seqs);
+  const int64_t saved = ((int64_t)b->n_seqs - g->n_groups) * shared_len * 2 * pool->n_kv_heads * pool->head_dim *
+                        page_elem_bytes(pool->dtype);
+  p.apart = g->n_groups > 0 && saved >= kWorthParts;
+  if (!p.apart) {
+    p.whole = make_plan(pool, b, Hq, 0, 0);
+    p.bytes = p.whole.bytes;
+    return p;
+  }
+  const auto blocks = [&](int units, int64_t most_of) {
+    return std::min(b->n_tokens * G / tile::kBlockRows + units, units * ceil_div(most_of * G, tile::kBlockRows));
+  };
+  const int64_t most_group = most_tokens(g->max_tokens, b->n_tokens, g->n_groups);
+  p.shared = plan_units(pool, Hq, g->n_groups, b->n_tokens, most_group, shared_len, blocks(g->n_groups, most_group), 0, 0);
+  // (own keys: what the longest sequence has behind the longest prefix, a page at least)
+  const int64_t own_len = std::max<int64_t>(len - shared_len, pool->page_size);
+  p.own = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most, own_len, blocks(b->n_seqs, most), 0, 0);
+  const size_t rows = (size_t)b->n_tokens * Hq, places = (size_t)p.shared.n_splits + p.own.n_splits;
+  p.off_ml = align_up(places * rows * pool->head_dim * sizeof(float), 256);
+  p.off_shared = align_up(p.off_ml + places * rows * sizeof(float2), 256);
+  p.off_own = align_up(p.off_shared + (size_t)b->n_tokens * sizeof(int32_t), 256);
+  p.bytes = align_up(p.off_own + (size_t)b->n_tokens * sizeof(int32_t), 256);
   return p;
 }
 
@@ -1300,8 +1441,9 @@ ckv_status check_attn(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq
   return CKV_OK;
 }
 
-template <int D, int T>
-ckv_status launch_page_attn(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) {
+template <int D, int T, int P>
+ckv_status launch_units(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) {
+  const int units = P == kShared ? a.n_groups : a.s.n_seqs;
   if (p.wide) {
     if constexpr (T != CKV_DTYPE_F32) {
       const int64_t streams = (int64_t)a.Hkv * a.n_splits;
@@ -1309,31 +1451,120 @@ ckv_status launch_page_attn(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t 
       const int64_t grid = 8 * (streams / 8 * p.blocks + ceil_div(rest * p.blocks, 8));
       if (grid >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
       a.n_blocks = (uint32_t)p.blocks;
-      hipLaunchKernelGGL((page_tile_kernel<D, T>), dim3((unsigned)grid), dim3(256), 0, st, a);
+      hipLaunchKernelGGL((page_tile_kernel<D, T, P>), dim3((unsigned)grid), dim3(256), 0, st, a);
     }
   } else {
-    const int64_t wgs = (int64_t)align_up((size_t)a.s.n_seqs * a.n_splits, 8) * a.Hkv;
+    const int64_t wgs = (int64_t)align_up((size_t)units * a.n_splits, 8) * a.Hkv;
     if (wgs >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
     // A launch of at most a workgroup per CU has 8 waves in each, whose fewer steps follow
     // one another (16 sequences of 4 tokens: 13.1 -> 11.7 us, fp32 prompts 8.7 -> 8.0); where
     // there are more, 4 (48 sequences: 80 us, with 8: 94).
     const bool eight = wgs * p.row_blocks <= 256;
-    const auto kernel = a.c == 8 ? (eight ? page_rows_kernel<D, T, true, 8> : page_rows_kernel<D, T, true, 4>)
-                                 : (eight ? page_rows_kernel<D, T, false, 8> : page_rows_kernel<D, T, false, 4>);
+    const auto kernel = a.c == 8 ? (eight ? page_rows_kernel<D, T, true, 8, P> : page_rows_kernel<D, T, true, 4, P>)
+                                 : (eight ? page_rows_kernel<D, T, false, 8, P> : page_rows_kernel<D, T, false, 4, P>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)p.row_blocks), dim3(eight ? 512 : 256), 0, st, a);
   }
   CKV_HIP(hipGetLastError());
-  if (a.n_splits > 1) {
-    using QT = typename Elem<T>::Q;
-    constexpr int kUnits = 256 / (D / 4);
-    const int64_t rows = a.s.n_tokens * a.Hq;
-    if (a.n_splits <= kJoinBatch)
-      hipLaunchKernelGGL((page_combine_kernel<D, QT, 1>), dim3((unsigned)ceil_div(rows, kUnits)), dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL((page_combine_kernel<D, QT, kUnits>), dim3((unsigned)rows), dim3(256), 0, st, a);
-    CKV_HIP(hipGetLastError());
-  }
   return CKV_OK;
+}
+
+// Joins the a.n_splits places of every row.
+template <int D, int T, bool kParts>
+ckv_status launch_join(const PageAttnArgs& a, hipStream_t st) {
+  using QT = typename Elem<T>::Q;
+  constexpr int kUnits = 256 / (D / 4);
+  const int64_t rows = a.s.n_tokens * a.Hq;
+  if (a.n_splits <= kJoinBatch)
+    hipLaunchKernelGGL((page_combine_kernel<D, QT, 1, kParts>), dim3((unsigned)ceil_div(rows, kUnits)), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((page_combine_kernel<D, QT, kUnits, kParts>), dim3((unsigned)rows), dim3(256), 0, st, a);
+  CKV_HIP(hipGetLastError());
+  return CKV_OK;
+}
+
+template <int D, int T>
+ckv_status launch_page_attn(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) {
+  if (ckv_status s = launch_units<D, T, kWhole>(a, p, st); s != CKV_OK) return s;
+  return a.n_splits > 1 ? launch_join<D, T, false>(a, st) : CKV_OK;
+}
+
+template <int D, int T>
+ckv_status launch_shared_attn(PageAttnArgs& a, const SharedPlan& p, char* ws, hipStream_t st) {
+  const size_t rows = (size_t)a.s.n_tokens * a.Hq;
+  float* const o_part = reinterpret_cast<float*>(ws);
+  float2* const ml_part = reinterpret_cast<float2*>(ws + p.off_ml);
+  int32_t* const shared_parts = reinterpret_cast<int32_t*>(ws + p.off_shared);
+  a.o_part = o_part;
+  a.ml_part = ml_part;
+  a.n_parts = shared_parts;
+  a.n_splits = p.shared.n_splits;
+  a.slice = p.shared.slice;
+  if (ckv_status s = launch_units<D, T, kShared>(a, p.shared, st); s != CKV_OK) return s;
+  a.o_part = o_part + (size_t)p.shared.n_splits * rows * D;
+  a.ml_part = ml_part + (size_t)p.shared.n_splits * rows;
+  a.n_parts = reinterpret_cast<int32_t*>(ws + p.off_own);
+  a.n_splits = p.own.n_splits;
+  a.slice = p.own.slice;
+  if (ckv_status s = launch_units<D, T, kOwn>(a, p.own, st); s != CKV_OK) return s;
+  a.o_part = o_part;
+  a.ml_part = ml_part;
+  a.shared_parts = shared_parts;
+  a.shared_splits = p.shared.n_splits;
+  a.n_splits = p.shared.n_splits + p.own.n_splits;
+  return launch_join<D, T, true>(a, st);
+}
+
+// f(D, T) of a pool, as integral constants.
+template <class F>
+ckv_status for_pool(const ckv_page_pool* pool, F&& f) {
+  using std::integral_constant;
+  if (pool->dtype == CKV_DTYPE_F32) return f(integral_constant<int, 64>{}, integral_constant<int, CKV_DTYPE_F32>{});
+  if (pool->dtype == CKV_DTYPE_BF16)
+    return pool->head_dim == 128 ? f(integral_constant<int, 128>{}, integral_constant<int, CKV_DTYPE_BF16>{})
+                                 : f(integral_constant<int, 64>{}, integral_constant<int, CKV_DTYPE_BF16>{});
+  return pool->head_dim == 128 ? f(integral_constant<int, 128>{}, integral_constant<int, CKV_DTYPE_E4M3>{})
+                               : f(integral_constant<int, 64>{}, integral_constant<int, CKV_DTYPE_E4M3>{});
+}
+
+// What both calls need of q, out and ws, and the kernels' arguments but for their plan's.
+ckv_status check_rows(const ckv_page_batch* batch, const void* q, int32_t n_q_heads, const void* out, const void* ws) {
+  if (!q || !out) CKV_FAIL(CKV_EINVAL, "NULL pointer argument");
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws))
+    CKV_FAIL(CKV_EINVAL, "pointers must be 16-byte aligned");
+  if (batch->n_tokens * n_q_heads > (int64_t(1) << 26))
+    CKV_FAIL(CKV_EUNSUPPORTED, "more than 2^26 query rows in one call");
+  return CKV_OK;
+}
+ckv_status check_scale(float sm_scale) {
+  if (!(sm_scale >= 0.f) || std::isinf(sm_scale)) CKV_FAIL(CKV_EINVAL, "sm_scale must be finite and >= 0");
+  return CKV_OK;
+}
+PageAttnArgs attn_args(const ckv_page_pool* pool, const ckv_page_batch* batch, const void* q, int32_t n_q_heads,
+                       float sm_scale, void* out) {
+  PageAttnArgs a{};
+  a.s = page_seqs(batch);
+  a.k = static_cast<const char*>(pool->k);
+  a.v = static_cast<const char*>(pool->v);
+  a.k_scale = pool->k_scale;
+  a.v_scale = pool->v_scale;
+  a.page_stride = page_stride_bytes(pool);
+  a.n_pages = pool->n_pages;
+  a.q = q;
+  a.out = out;
+  a.c = pool->page_size;
+  a.log2c = (a.c & (a.c - 1)) == 0 ? __builtin_ctz(a.c) : -1;
+  a.Hkv = pool->n_kv_heads;
+  a.Hq = n_q_heads;
+  a.G = n_q_heads / pool->n_kv_heads;
+  a.c1 = (sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)pool->head_dim)) * 1.4426950408889634f;
+  return a;
+}
+void set_plan(PageAttnArgs& a, const PageAttnPlan& p, void* ws) {
+  a.o_part = static_cast<float*>(ws);
+  a.ml_part = p.bytes ? reinterpret_cast<float2*>(static_cast<char*>(ws) + p.off_ml) : nullptr;
+  a.n_parts = p.bytes ? reinterpret_cast<int32_t*>(static_cast<char*>(ws) + p.off_n) : nullptr;
+  a.slice = p.slice;
+  a.n_splits = p.n_splits;
 }
 
 }  // namespace
@@ -1354,46 +1585,49 @@ ckv_status ckv_page_attn(const ckv_page_pool* pool, const ckv_page_batch* batch,
                          void* out, void* ws, size_t ws_bytes, void* stream) {
   clear_error();
   if (ckv_status s = check_attn(pool, batch, n_q_heads, window, n_sinks, true); s != CKV_OK) return s;
-  if (!(sm_scale >= 0.f) || std::isinf(sm_scale)) CKV_FAIL(CKV_EINVAL, "sm_scale must be finite and >= 0");
+  if (ckv_status s = check_scale(sm_scale); s != CKV_OK) return s;
   if (batch->n_seqs == 0 || batch->n_tokens == 0) return CKV_OK;
-  if (!q || !out) CKV_FAIL(CKV_EINVAL, "NULL pointer argument");
-  if (!aligned16(q) || !aligned16(out) || !aligned16(ws))
-    CKV_FAIL(CKV_EINVAL, "pointers must be 16-byte aligned");
-  if (batch->n_tokens * n_q_heads > (int64_t(1) << 26))
-    CKV_FAIL(CKV_EUNSUPPORTED, "more than 2^26 query rows in one call");
+  if (ckv_status s = check_rows(batch, q, n_q_heads, out, ws); s != CKV_OK) return s;
   const PageAttnPlan p = make_plan(pool, batch, n_q_heads, window, n_sinks);
   if (p.bytes && (!ws || ws_bytes < p.bytes))
     CKV_FAIL(CKV_EINVAL, "workspace too small: %zu < %zu", ws ? ws_bytes : (size_t)0, p.bytes);
-  PageAttnArgs a;
-  a.s = page_seqs(batch);
-  a.k = static_cast<const char*>(pool->k);
-  a.v = static_cast<const char*>(pool->v);
-  a.k_scale = pool->k_scale;
-  a.v_scale = pool->v_scale;
-  a.page_stride = page_stride_bytes(pool);
-  a.n_pages = pool->n_pages;
-  a.q = q;
-  a.out = out;
-  a.o_part = static_cast<float*>(ws);
-  a.ml_part = p.bytes ? reinterpret_cast<float2*>(static_cast<char*>(ws) + p.off_ml) : nullptr;
-  a.n_parts = p.bytes ? reinterpret_cast<int32_t*>(static_cast<char*>(ws) + p.off_n) : nullptr;
-  a.slice = p.slice;
-  a.c = pool->page_size;
-  a.log2c = (a.c & (a.c - 1)) == 0 ? __builtin_ctz(a.c) : -1;
-  a.Hkv = pool->n_kv_heads;
-  a.Hq = n_q_heads;
-  a.G = n_q_heads / pool->n_kv_heads;
+  PageAttnArgs a = attn_args(pool, batch, q, n_q_heads, sm_scale, out);
+  set_plan(a, p, ws);
   a.window = window;
   a.sinks = window > 0 ? n_sinks : 0;
-  a.n_splits = p.n_splits;
-  a.c1 = (sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)pool->head_dim)) * 1.4426950408889634f;
-  const hipStream_t st = (hipStream_t)stream;
-  if (pool->dtype == CKV_DTYPE_F32) return launch_page_attn<64, CKV_DTYPE_F32>(a, p, st);
-  if (pool->dtype == CKV_DTYPE_BF16)
-    return pool->head_dim == 128 ? launch_page_attn<128, CKV_DTYPE_BF16>(a, p, st)
-                                 : launch_page_attn<64, CKV_DTYPE_BF16>(a, p, st);
-  return pool->head_dim == 128 ? launch_page_attn<128, CKV_DTYPE_E4M3>(a, p, st)
-                               : launch_page_attn<64, CKV_DTYPE_E4M3>(a, p, st);
+  return for_pool(pool, [&](auto d, auto t) { return launch_page_attn<d, t>(a, p, (hipStream_t)stream); });
+}
+
+size_t ckv_page_attn_shared_workspace_bytes(const ckv_page_pool* pool, const ckv_page_batch* batch,
+                                            const ckv_page_groups* groups, int32_t n_q_heads) {
+  if (check_attn(pool, batch, n_q_heads, 0, 0, false) != CKV_OK) return 0;
+  if (check_groups(groups, batch, false) != CKV_OK) return 0;
+  return make_shared_plan(pool, batch, groups, n_q_heads).bytes;
+}
+
+ckv_status ckv_page_attn_shared(const ckv_page_pool* pool, const ckv_page_batch* batch,
+                                const ckv_page_groups* groups, const void* q, int32_t n_q_heads,
+                                float sm_scale, void* out, void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  if (ckv_status s = check_attn(pool, batch, n_q_heads, 0, 0, true); s != CKV_OK) return s;
+  if (ckv_status s = check_groups(groups, batch, true); s != CKV_OK) return s;
+  if (ckv_status s = check_scale(sm_scale); s != CKV_OK) return s;
+  if (batch->n_seqs == 0 || batch->n_tokens == 0) return CKV_OK;
+  if (ckv_status s = check_rows(batch, q, n_q_heads, out, ws); s != CKV_OK) return s;
+  const SharedPlan p = make_shared_plan(pool, batch, groups, n_q_heads);
+  if (p.bytes && (!ws || ws_bytes < p.bytes))
+    CKV_FAIL(CKV_EINVAL, "workspace too small: %zu < %zu", ws ? ws_bytes : (size_t)0, p.bytes);
+  PageAttnArgs a = attn_args(pool, batch, q, n_q_heads, sm_scale, out);
+  if (!p.apart) {
+    set_plan(a, p.whole, ws);
+    return for_pool(pool, [&](auto d, auto t) { return launch_page_attn<d, t>(a, p.whole, (hipStream_t)stream); });
+  }
+  a.grp_off = groups->grp_off;
+  a.shared = groups->shared;
+  a.n_groups = groups->n_groups;
+  return for_pool(pool, [&](auto d, auto t) {
+    return launch_shared_attn<d, t>(a, p, static_cast<char*>(ws), (hipStream_t)stream);
+  });
 }
 
 }  // extern "C"

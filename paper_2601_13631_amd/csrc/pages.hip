@@ -145,7 +145,7 @@ template <int D>
 __global__ __launch_bounds__(64) void append_e4m3_kernel(AppendArgs a) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes;
   const int lane = threadIdx.x, g = blockIdx.y;
-  const int b = find_seq(a.s, blockIdx.x, [&](int q) { return append_start(a, q); });
+  const int b = find_seq(a.s.n_seqs, blockIdx.x, [&](int q) { return append_start(a, q); });
   if (b < 0) return;
   const SeqSpan sp = seq_span(a.s, b);
   const int64_t start = (int64_t)sp.len - sp.count;  // position of the call's first token

@@ -22,6 +22,7 @@ constexpr int64_t kMaxGrid = int64_t(1) << 24;
 // memory too); CKV_OK, or the code of the first fault, with its reason recorded.
 ckv_status check_pool(const ckv_page_pool* p, bool with_pointers);
 ckv_status check_batch(const ckv_page_batch* b, bool with_pointers);
+ckv_status check_groups(const ckv_page_groups* g, const ckv_page_batch* b, bool with_pointers);
 
 // A batch as kernels read it.
 struct PageSeqs {
@@ -49,16 +50,16 @@ __device__ __forceinline__ SeqSpan seq_span(const PageSeqs& s, int b) {
   return SeqSpan{lo, (int32_t)max<int64_t>(hi - lo, 0), s.lens[b]};
 }
 
-// The last sequence b with start(b) <= k, -1 if there is none; start must not fall.  A whole
+// The last sequence b of n with start(b) <= k, -1 if there is none; start must not fall.  A whole
 // wave calls it: 64 sequences are looked at at a time (one round of loads for 64 of them, two
 // for 4,096).
 // Work that the sequences have in parts is numbered so: sequence b's parts from start(b) on,
 // where start(b + 1) - start(b) is at least their number and follows from the offsets alone;
 // a number past a sequence's last part has no work.
 template <class F>
-__device__ __forceinline__ int find_seq(const PageSeqs& s, int64_t k, F&& start) {
+__device__ __forceinline__ int find_seq(int n, int64_t k, F&& start) {
   const int lane = threadIdx.x & 63;
-  int lo = 0, n = s.n_seqs;
+  int lo = 0;
   do {
     const int step = (n + 63) / 64;
     const uint64_t at_most = __ballot(lane * step < n && start(lo + min(lane * step, n - 1)) <= k);
