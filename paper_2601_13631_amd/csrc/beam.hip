@@ -120,7 +120,7 @@ __device__ __forceinline__ float element(const uint32_t* w, int e) {
 // where the wave looks at 64 of them at a time and collects those that do.  64 collected are
 // sorted and merged into the list that the lanes hold.  Typically few lanes have any.
 template <bool kBf16>
-__global__ __launch_bounds__(64 * kWaves) void beam_scan_kernel(BeamArgs a) {
+__global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
   constexpr int kPer = kBf16 ? 8 : 4, kBytes = kBf16 ? 2 : 4;  // elements of a piece, bytes of one
   constexpr int kLane = kPieces * kPer;                        // elements of a lane per batch
   constexpr int kWords = 4 * kPieces;
@@ -144,34 +144,39 @@ __global__ __launch_bounds__(64 * kWaves) void beam_scan_kernel(BeamArgs a) {
   const int keep = a.keep;
 
   using Batch = u32x4[kPieces];
+  // Element e of a piece that begins at p0 is of token token_at(p0) + e: a piece that would
+  // reach past the row is the row's last one, where those before p0 count for nothing.
+  auto token_at = [&](int64_t p0) __attribute__((always_inline)) { return min(p0, max(end - kPer, (int64_t)0)); };
   auto load = [&](int64_t batch, Batch& x) __attribute__((always_inline)) {
     const int64_t e0 = batch * kBatch;
-    if (e0 + kBatch <= end) {
+    if (end >= kPer) {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) x[i] = piece_at(base + (e0 + (int64_t)(i * 64 + lane) * kPer) * kBytes);
-      return;
+      for (int i = 0; i < kPieces; ++i) x[i] = piece_at(base + token_at(e0 + (i * 64 + lane) * kPer) * kBytes);
+    } else {  // fewer tokens than a piece: lane 0's
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) x[i] = u32x4{0u, 0u, 0u, 0u};
+      if (lane == 0)
+        for (int e = 0; e < (int)end; ++e) {
+          if constexpr (kBf16)
+            x[0][e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(base)[e] << 16 * (e & 1);
+          else
+            x[0][e] = reinterpret_cast<const uint32_t*>(base)[e];
+        }
     }
+  };
+  auto clear_outside = [&](int64_t batch, Batch& x) __attribute__((always_inline)) {
+    const int64_t e0 = batch * kBatch;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int64_t p0 = e0 + (i * 64 + lane) * kPer;
-      if (p0 + kPer <= end) {
-        x[i] = piece_at(base + p0 * kBytes);
-      } else {
+      const int64_t p0 = e0 + (i * 64 + lane) * kPer, at = token_at(p0);
+      const int from = (int)min(p0 - at, (int64_t)kPer), upto = (int)min(end - at, (int64_t)kPer);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          if constexpr (kBf16) {
-            uint32_t v[2] = {0xff80u, 0xff80u};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int64_t p = p0 + 2 * w + h;
-              if (p < end) v[h] = *reinterpret_cast<const uint16_t*>(base + p * 2);
-            }
-            x[i][w] = v[0] | v[1] << 16;
-          } else {
-            const int64_t p = p0 + w;
-            x[i][w] = p < end ? *reinterpret_cast<const uint32_t*>(base + p * 4) : 0xff800000u;
-          }
-        }
+      for (int e = 0; e < kPer; ++e) {
+        if (e >= from && e < upto) continue;
+        if constexpr (kBf16)
+          x[i][e >> 1] = e & 1 ? (x[i][e >> 1] & 0xffffu) | 0xff800000u : (x[i][e >> 1] & 0xffff0000u) | 0xff80u;
+        else
+          x[i][e] = 0xff800000u;
       }
     }
   };
@@ -199,6 +204,7 @@ __global__ __launch_bounds__(64 * kWaves) void beam_scan_kernel(BeamArgs a) {
     if (batch < b1) load(batch, x);
     for (; batch < b1; batch += kWaves) {
       if (batch + kWaves < b1) load(batch + kWaves, next);
+      if ((batch + 1) * kBatch > end) clear_outside(batch, x);
       if (careful) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
@@ -263,7 +269,7 @@ __global__ __launch_bounds__(64 * kWaves) void beam_scan_kernel(BeamArgs a) {
         for (int at = lane; at - lane < total; at += 64) {
           const int l = min(at / kLane, 63), e = at % kLane, i = e / kPer;
           const float v = element<kBf16>(&words[wave][l][4 * i], e % kPer);
-          const int64_t token = batch * kBatch + (int64_t)(i * 64 + lanes[wave][l]) * kPer + e % kPer;
+          const int64_t token = token_at(batch * kBatch + (int64_t)(i * 64 + lanes[wave][l]) * kPer) + e % kPer;
           const uint64_t k = key_of(v, (int)token);
           const uint64_t yes = __ballot(at < total && k >= least && v > -INFINITY);
           if (!yes) continue;
@@ -327,8 +333,15 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a) 
   const int keep = a.keep;
   for (int b = wave; b < a.n_beams; b += kJoinWaves) {
     const int64_t row = row0 + b, at = row * a.slices;
+    // (all loads together: those of a beam that the scan left out hold anything)
+    const uint64_t* const keys = a.keys + at * keep;
+    const int up = 63 - lane;
+    uint64_t list = lane < keep ? keys[lane] : 0, next = a.slices > 1 && up < keep ? keys[keep + up] : 0;
+    const float ref = lane < a.slices ? a.ref[at + lane] : kLowest;
+    double sum = lane < a.slices ? a.sum[at + lane] : 0;
     const float c = a.scores[row];
-    const bool live = c > -INFINITY, done = live && a.done && a.done[row];
+    const uint8_t ended = a.done ? a.done[row] : 0;
+    const bool live = c > -INFINITY, done = live && ended;
     int n = 0;
     if (done) {
       n = 1;
@@ -337,11 +350,6 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a) 
         tokens[b * keep] = a.eos;
       }
     } else if (live) {
-      const uint64_t* const keys = a.keys + at * keep;
-      const int up = 63 - lane;
-      uint64_t list = lane < keep ? keys[lane] : 0, next = a.slices > 1 && up < keep ? keys[keep + up] : 0;
-      const float ref = lane < a.slices ? a.ref[at + lane] : kLowest;
-      double sum = lane < a.slices ? a.sum[at + lane] : 0;
       float top = ref;
 #pragma unroll
       for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));

@@ -47,28 +47,46 @@ template <int kThreads, class T>
 __device__ __forceinline__ T block_total(T x) {
   return block_all<kThreads>(x, [](T a, T b) { return a + b; });
 }
-// The sum of x over the threads before this one; `total` gets that of all.
+// Inclusive sums over a wave's lanes, by moves between lanes (a row of 16, then the last lane
+// of each row to the next rows).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t moved(int64_t x) {
+  return (int64_t)join64((uint32_t)moved<CTRL, ROWS>((int)(x >> 32)), (uint32_t)moved<CTRL, ROWS>((int)x));
+}
+template <class T>
+__device__ __forceinline__ T wave_upto(T x) {
+  x += moved<kDppRowShr1, 0xF>(x);
+  x += moved<kDppRowShr2, 0xF>(x);
+  x += moved<kDppRowShr4, 0xF>(x);
+  x += moved<kDppRowShr8, 0xF>(x);
+  x += moved<0x142, 0xA>(x);  // lane 15 of rows 0 and 2 to rows 1 and 3
+  x += moved<0x143, 0xC>(x);  // lane 31 to rows 2 and 3
+  return x;
+}
+// The sums of x and y over the threads before this one; `tx` and `ty` get those of all.
 template <int kThreads, class T>
-__device__ __forceinline__ T block_before(T x, T& total) {
-  __shared__ T part[kThreads / 64];
+__device__ __forceinline__ void block_before(T& x, T& y, T& tx, T& ty) {
+  constexpr int kWaves = kThreads / 64;
+  static_assert(kWaves <= 64);
+  __shared__ T part[2][kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  T upto = x;
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) {
-    const T y = __shfl_up(upto, i);
-    if (lane >= i) upto += y;
-  }
-  if (lane == 63) part[wave] = upto;
-  __syncthreads();
-  T below = 0;
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) {
-    if (i < wave) below += part[i];
-    total += part[i];
+  const T ux = wave_upto(x), uy = wave_upto(y);
+  if (lane == 63) {
+    part[0][wave] = ux;
+    part[1][wave] = uy;
   }
   __syncthreads();
-  return below + upto - x;
+  const T px = lane < kWaves ? part[0][lane] : T(0), py = lane < kWaves ? part[1][lane] : T(0);
+  const T wx = wave_upto(px), wy = wave_upto(py);
+  tx = __shfl(wx, kWaves - 1);
+  ty = __shfl(wy, kWaves - 1);
+  x = __shfl(wx - px, wave) + ux - x;
+  y = __shfl(wy - py, wave) + uy - y;
+  __syncthreads();
 }
 
 // ---- share ----------------------------------------------------------------------------
@@ -82,7 +100,9 @@ struct ShareArgs {
 
 // A workgroup per group: its waves go over the sequences in turn, lanes along the table,
 // against the first sequence with tokens.  One more for the sequences of no group.
-constexpr int kShareThreads = 1024, kShareBatch = 8;
+// The loads of a wave's rounds are its time, so four sequences go together: 48 sequences of 970
+// pages 11.4 us one at a time, KSHARE so.
+constexpr int kShareThreads = 1024, kShareBatch = 8, kShareSeqs = 4;
 __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
   const auto begin_of = [&](int g) { return min(max(a.grp_off[g], 0), a.s.n_seqs); };
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -110,21 +130,33 @@ __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
   if (tid == 0) common = slots;
   __syncthreads();
   const int32_t* const first = a.s.table + (int64_t)leader * a.s.table_stride;
-  for (int b = f + wave; b < l && slots > 0; b += kShareThreads / 64) {
-    if (b == leader || seq_span(a.s, b).count == 0) continue;
-    const int32_t* const mine = a.s.table + (int64_t)b * a.s.table_stride;
-    for (int s0 = 0; s0 < slots; s0 += 64 * kShareBatch) {
-      int x[kShareBatch], y[kShareBatch];
+  constexpr int kWavesOf = kShareThreads / 64;
+  for (int b0 = f + wave; b0 < l && slots > 0; b0 += kWavesOf * kShareSeqs) {
+    // (a sequence that is not there or has no tokens: the first one again)
+    const int32_t* mine[kShareSeqs];
+    SeqSpan sp[kShareSeqs];
 #pragma unroll
-      for (int i = 0; i < kShareBatch; ++i) {
-        const int at = min(s0 + 64 * i + lane, slots - 1);
-        x[i] = first[at];
-        y[i] = mine[at];
+    for (int i = 0; i < kShareSeqs; ++i) sp[i] = seq_span(a.s, min(b0 + i * kWavesOf, l - 1));
+#pragma unroll
+    for (int i = 0; i < kShareSeqs; ++i) {
+      const int b = b0 + i * kWavesOf;
+      mine[i] = b < l && sp[i].count > 0 ? a.s.table + (int64_t)b * a.s.table_stride : first;
+    }
+    for (int s0 = 0; s0 < slots; s0 += 64 * kShareBatch) {
+      int x[kShareBatch], y[kShareSeqs][kShareBatch];
+#pragma unroll
+      for (int k = 0; k < kShareBatch; ++k) {
+        const int at = min(s0 + 64 * k + lane, slots - 1);
+        x[k] = first[at];
+#pragma unroll
+        for (int i = 0; i < kShareSeqs; ++i) y[i][k] = mine[i][at];
       }
       int differ = INT32_MAX;
 #pragma unroll
-      for (int i = kShareBatch - 1; i >= 0; --i)
-        if (x[i] != y[i]) differ = min(s0 + 64 * i + lane, slots - 1);
+      for (int k = kShareBatch - 1; k >= 0; --k)
+#pragma unroll
+        for (int i = 0; i < kShareSeqs; ++i)
+          if (x[k] != y[i][k]) differ = min(s0 + 64 * k + lane, slots - 1);
       if (!__any(differ != INT32_MAX)) continue;
       differ = wave_all(differ, lower);
       if (lane == 0) atomicMin(&common, differ);
@@ -154,7 +186,7 @@ struct Tables {
   __device__ __forceinline__ int length(int len) const {
     return (int)min((int64_t)max(len, 0), (int64_t)max_pages * c);
   }
-  __device__ __forceinline__ int pages(int64_t tokens) const { return (int)((tokens + c - 1) / c); }
+  __device__ __forceinline__ int pages(int tokens) const { return (int)((uint32_t)(tokens + c - 1) / (uint32_t)c); }
   __device__ __forceinline__ bool names_page(int e) const { return e >= 0 && e < n_pages; }
 };
 
@@ -275,53 +307,78 @@ struct ExtendArgs {
   int64_t table_blocks;
 };
 
-__device__ __forceinline__ int free_pages(const Tables& t, int64_t p0) {  // of this thread's kPlanPer from p0 on
-  int refs[kPlanPer], n = 0;
+// Use counts of this thread's pages p0 .. p0 + 3; 1 past the last page.
+__device__ __forceinline__ void load_refs(const Tables& t, int64_t p0, int32_t (&refs)[kPlanPer]) {
+  if (t.n_pages >= kPlanPer) {  // (uniform)
+    // the last ones of all at most, of which those before p0 are left out
+    const int64_t at = min(p0, (int64_t)t.n_pages - kPlanPer);
+    const int by = (int)min(p0 - at, (int64_t)kPlanPer);
+    int32_t x[kPlanPer];
+    __builtin_memcpy(x, t.refs + at, sizeof x);
 #pragma unroll
-  for (int i = 0; i < kPlanPer; ++i) refs[i] = t.refs[min(p0 + i, (int64_t)t.n_pages - 1)];
+    for (int i = 0; i < kPlanPer; ++i) refs[i] = x[i];
+    if (by)
 #pragma unroll
-  for (int i = 0; i < kPlanPer; ++i) n += p0 + i < t.n_pages && refs[i] <= 0;
+      for (int i = 0; i < kPlanPer; ++i) refs[i] = i + by < kPlanPer ? x[(i + by) & (kPlanPer - 1)] : 1;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPlanPer; ++i) refs[i] = p0 + i < t.n_pages ? t.refs[p0 + i] : 1;
+  }
+}
+__device__ __forceinline__ int free_of(const int32_t (&refs)[kPlanPer]) {
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanPer; ++i) n += refs[i] <= 0;
   return n;
 }
 
 __global__ __launch_bounds__(kPlanThreads) void extend_count_kernel(ExtendArgs a) {
-  const int n = block_total<kPlanThreads>(free_pages(a.t, (int64_t)blockIdx.x * kPlanPages + threadIdx.x * kPlanPer));
+  int32_t refs[kPlanPer];
+  load_refs(a.t, (int64_t)blockIdx.x * kPlanPages + threadIdx.x * kPlanPer, refs);
+  const int n = block_total<kPlanThreads>(free_of(refs));
   if (threadIdx.x == 0) a.counts[blockIdx.x] = n;
 }
 
-// kCounted: the blocks' counts are there; else every workgroup goes over the use counts below
-// its own pages itself.
+// This thread's share of the free pages of the first `blocks` blocks.  kCounted: their counts
+// are there; else every workgroup goes over their use counts itself, in one round of loads.
 template <bool kCounted>
 __device__ __forceinline__ int free_below(const ExtendArgs& a, int blocks) {
   int n = 0;
   if constexpr (kCounted) {
     for (int i = threadIdx.x; i < blocks; i += kPlanThreads) n += a.counts[i];
   } else {
-#pragma unroll 4
-    for (int i = 0; i < blocks; ++i) n += free_pages(a.t, (int64_t)i * kPlanPages + threadIdx.x * kPlanPer);
+    int32_t refs[kSelfCounted][kPlanPer];
+#pragma unroll
+    for (int i = 0; i < kSelfCounted; ++i)
+      if (i < blocks) load_refs(a.t, (int64_t)i * kPlanPages + threadIdx.x * kPlanPer, refs[i]);
+#pragma unroll
+    for (int i = 0; i < kSelfCounted; ++i) n += i < blocks ? free_of(refs[i]) : 0;
   }
-  return block_total<kPlanThreads>(n);
+  return n;
 }
 
 template <bool kCounted>
 __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a) {
   const Tables& t = a.t;
   if ((int)blockIdx.x < a.plan_blocks) {
-    const int below = free_below<kCounted>(a, blockIdx.x);
     const int64_t p0 = (int64_t)blockIdx.x * kPlanPages + threadIdx.x * kPlanPer;
-    int total, rank = below + block_before<kPlanThreads>(free_pages(t, p0), total);
+    int32_t refs[kPlanPer];
+    load_refs(t, p0, refs);
+    int below = free_below<kCounted>(a, blockIdx.x), rank = free_of(refs), all_below, all;
+    block_before<kPlanThreads>(below, rank, all_below, all);
+    rank += all_below;
 #pragma unroll
     for (int i = 0; i < kPlanPer; ++i) {
       if (p0 + i >= t.n_pages) break;
-      const int refs = t.refs[p0 + i];
-      if (refs <= 0) a.list[rank++] = (int32_t)(p0 + i);
-      if (t.refs_out != t.refs) t.refs_out[p0 + i] = refs;
+      if (refs[i] <= 0) a.list[rank++] = (int32_t)(p0 + i);
+      if (t.refs_out != t.refs) t.refs_out[p0 + i] = refs[i];
     }
     return;
   }
   // the sequences, in their order
-  const int64_t n_free = free_below<kCounted>(a, a.plan_blocks);
-  int64_t needed = 0, asked = 0, taken = 0, tokens = 0, refused = 0;
+  int64_t n_free = free_below<kCounted>(a, a.plan_blocks);
+  int64_t needed = 0, asked = 0, taken = 0, tokens = 0;
+  int refused = 0;  // of this thread's sequences
   if (threadIdx.x == 0) a.o.tok_off[0] = 0;
   for (int b0 = 0; b0 < t.n_seqs; b0 += kPlanThreads) {
     const int b = b0 + threadIdx.x;
@@ -332,45 +389,56 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
       len = t.length(t.lens[b]);
       add = max(a.n_new[b], 0);
       const int held = t.pages(len);
-      const int64_t want = (len + add + t.c - 1) / t.c;
-      no = want > t.max_pages;
+      const int64_t upto = (int64_t)len + add;
+      no = upto > (int64_t)t.max_pages * t.c;
       if (no) {
         add = 0;
       } else if (add > 0) {
-        if (len % t.c) {
+        if (held * t.c != len) {
           tail = t.table[(int64_t)b * t.table_stride + held - 1];
           if (!t.names_page(tail) || t.refs[tail] <= 1) tail = -1;
         }
-        need = want - held + (tail >= 0);
+        need = t.pages((int)upto) - held + (tail >= 0);
       }
     }
-    int64_t total_need, total_add, got;
-    const int64_t need_upto = needed + block_before<kPlanThreads>(need, total_need) + need;
-    const int64_t add_upto = asked + block_before<kPlanThreads>(add, total_add) + add;
-    if ((need > 0 && need_upto > n_free) || (add > 0 && add_upto > a.o.n_tokens)) {
-      no = true;
-      need = add = 0;
-      tail = -1;
+    if (b0 == 0) {
+      int64_t mine = n_free, none = 0, zero;
+      block_before<kPlanThreads>(mine, none, n_free, zero);
     }
-    needed += total_need;
-    asked += total_add;
-    const int64_t rank = taken + block_before<kPlanThreads>(need, got);
-    taken += got;
-    const int64_t row = tokens + block_before<kPlanThreads>(add, got);
-    tokens += got;
-    refused += block_total<kPlanThreads>((int64_t)no);
+    int64_t before = need, row = add, total_need, total_add;
+    block_before<kPlanThreads>(before, row, total_need, total_add);
+    if (needed + total_need > n_free || asked + total_add > a.o.n_tokens) {  // some are refused
+      if ((need > 0 && needed + before + need > n_free) || (add > 0 && asked + row + add > a.o.n_tokens)) {
+        no = true;
+        need = add = 0;
+        tail = -1;
+      }
+      needed += total_need;
+      asked += total_add;
+      before = need;
+      row = add;
+      block_before<kPlanThreads>(before, row, total_need, total_add);
+    } else {
+      needed += total_need;
+      asked += total_add;
+    }
+    refused += no;
     if (b < t.n_seqs) {
-      a.first[b] = (int32_t)rank;
+      a.first[b] = (int32_t)(taken + before);
       a.old_len[b] = len;
-      a.o.tok_off[b + 1] = (int32_t)(row + add);
+      a.o.tok_off[b + 1] = (int32_t)(tokens + row + add);
       a.o.copy_src[b] = tail;
     }
+    taken += total_need;
+    tokens += total_add;
   }
+  if (t.n_seqs == 0) n_free = block_total<kPlanThreads>(n_free);
+  refused = block_total<kPlanThreads>(refused);
   if (threadIdx.x == 0) {
     a.o.counts[0] = (int32_t)tokens;
     a.o.counts[1] = (int32_t)taken;
     a.o.counts[2] = (int32_t)(n_free - taken);
-    a.o.counts[3] = (int32_t)refused;
+    a.o.counts[3] = refused;
   }
 }
 
@@ -384,7 +452,7 @@ __global__ __launch_bounds__(kThreads) void extend_write_kernel(ExtendArgs a) {
     const int b = blockIdx.x / a.table_pieces, piece = blockIdx.x % a.table_pieces;
     const int len = a.old_len[b], add = a.o.tok_off[b + 1] - a.o.tok_off[b], first = a.first[b];
     const int src = a.o.copy_src[b];
-    const int from = t.pages(len) - (src >= 0), upto = add > 0 ? t.pages((int64_t)len + add) : from;
+    const int from = t.pages(len) - (src >= 0), upto = add > 0 ? t.pages(len + add) : from;
     int32_t* const to = t.table_out + (int64_t)b * t.table_out_stride;
     if (piece == 0 && threadIdx.x == 0) {
       t.lens_out[b] = len + add;
