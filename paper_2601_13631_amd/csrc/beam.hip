@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kMost = 64;  // beams of a request, and continuations that are kept: lanes of a wave
 constexpr float kLowest = -3.4028234663852886e38f;
+constexpr double kNoRef = -1e300;  // reference of an empty sum
 
 // A logit and its token as one number: larger for a larger logit, then for a lower token.
 // 0: none; numbers up to kNoKey are of logits that are -infinity.
@@ -87,7 +88,7 @@ struct BeamArgs {
   int64_t row_stride;  // elements
   int32_t n_reqs, n_beams, vocab, keep, eos;
   int32_t slices, slice;  // of a beam, and batches (of 64 lanes' pieces) of one
-  float* ref;             // [rows][slices]
+  double* ref;            // [rows][slices]: the sum is of exp(x - ref)
   double* sum;            // [rows][slices]
   uint64_t* keys;         // [rows][slices][keep], descending, 0 behind the last
   int32_t* parent;
@@ -100,6 +101,13 @@ constexpr int kWaves = 4;
 constexpr int kPieces = 4;  // 16-byte pieces of a lane per batch
 constexpr int64_t kScanBlocks = 1024;  // workgroups of a scan, about: 4 per CU
 constexpr int64_t kMaxScanGrid = int64_t(1) << 24;
+
+// The largest of three; of a NaN and numbers a number, or a NaN (which the sum then shows).
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float m;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(x), "v"(y), "v"(z));
+  return m;
+}
 
 // 16 bytes from any element on.
 __device__ __forceinline__ u32x4 piece_at(const char* p) {
@@ -128,7 +136,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
   __shared__ int32_t lanes[kWaves][64];
   __shared__ uint64_t found[kWaves][2 * 64];
   __shared__ double sums[kWaves];
-  __shared__ float refs[kWaves];
+  __shared__ double refs[kWaves];
   const int64_t row = blockIdx.x / a.slices;
   const int slice = blockIdx.x % a.slices;
   const float c = a.scores[row];
@@ -181,13 +189,18 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
     }
   };
 
-  float ref;
-  double sum;
-  uint64_t list;  // this lane's of the 64 best so far
-  // `careful`: NaN is taken for -infinity and an infinity for the largest number.  They show
-  // in the sum, after which the slice is done again.
+  double ref, sum;  // of exp(x - ref)
+  uint64_t list;    // this lane's of the 64 best so far
+  // The exponent x log2(e) - c is one fused step with c = log2(e) max, rounded: the reference is
+  // c / log2(e) exactly, and what the factor's own rounding leaves, kOff x, is taken back for
+  // x = max, off by kOff (max - x) for the others, a term that is as far below the largest.
+  // `careful`: NaN is taken for -infinity, an infinity for the largest number, and the
+  // exponent is (x - max) log2(e), as c may be past what 32 bits hold.  Such logits show in
+  // the sum, after which the slice is done again.
+  constexpr float kLog2e = 1.4426950408889634f;
+  constexpr double kOff = 1.0 - (double)kLog2e / 1.4426950408889634074;
   for (bool careful = false;; careful = true) {
-    ref = kLowest;
+    float top = careful ? kLowest : -0x1p125f, c = top * kLog2e;
     sum = 0;
     list = 0;
     uint64_t least = kNoKey + 1;  // what the best have at least
@@ -222,28 +235,32 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
             x[i][w] = v;
           }
       }
+      float v[kLane];
       float mx = -INFINITY;
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
         const uint32_t w[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) mx = fmaxf(mx, element<kBf16>(w, e));
+        for (int e = 0; e < kPer; ++e) v[i * kPer + e] = element<kBf16>(w, e);
       }
-      if (__any(mx > ref)) {
+#pragma unroll
+      for (int e = 0; e < kLane; e += 2) mx = max3(mx, v[e], v[e + 1]);
+      if (__any(mx > top)) {
         float to = mx;
 #pragma unroll
         for (int i = 1; i < 64; i <<= 1) to = fmaxf(to, __shfl_xor(to, i));
-        sum *= (double)__builtin_amdgcn_exp2f((ref - to) * 1.4426950408889634f);
-        ref = to;
+        const float by = careful ? (top - to) * kLog2e : c - to * kLog2e;
+        sum *= (double)__builtin_amdgcn_exp2f(by);
+        top = to;
+        c = to * kLog2e;
       }
-      // the difference first: it is exact for logits near the maximum, whose terms count
       float part[4] = {0.f, 0.f, 0.f, 0.f};
+      if (!careful) {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const uint32_t w[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
+        for (int e = 0; e < kLane; ++e) part[e & 3] += __builtin_amdgcn_exp2f(fmaf(v[e], kLog2e, -c));
+      } else {
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-          part[e & 3] += __builtin_amdgcn_exp2f((element<kBf16>(w, e) - ref) * 1.4426950408889634f);
+        for (int e = 0; e < kLane; ++e) part[e & 3] += __builtin_amdgcn_exp2f((v[e] - top) * kLog2e);
       }
       sum += (double)((part[0] + part[1]) + (part[2] + part[3]));
 
@@ -252,11 +269,18 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
       uint64_t hit = __ballot(mx >= at_least);
       if (hit) {
         if (__builtin_popcountll(hit) >= keep) {
-          // keep lanes have an element each that is no less than the keep-th lane's largest
-          const float kth = value_of(lane_of(sorted<false>(key_of(mx, lane)), keep - 1));
-          hit = __ballot(mx >= kth && mx >= at_least);
-          const uint64_t bound = key_of(kth, 0x7fffffff);
+          // keep lanes have an element each that is no less than the keep-th lane's largest, or
+          // than a number a little below it: bit by bit the largest that keep lanes reach
+          const uint32_t mine = (uint32_t)(key_of(mx, 0) >> 32);
+          uint32_t kth = 0;
+#pragma unroll
+          for (int bit = 31; bit >= (kBf16 ? 16 : 12); --bit) {
+            const uint32_t to = kth | 1u << bit;
+            if (__builtin_popcountll(__ballot(mine >= to)) >= keep) kth = to;
+          }
+          const uint64_t bound = (uint64_t)kth << 32;
           least = bound > least ? bound : least;
+          hit = __ballot(mine >= (uint32_t)(least >> 32));
         }
         if (hit >> lane & 1) {
           const int at = __builtin_popcountll(hit & ((1ull << lane) - 1));
@@ -268,10 +292,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
         const int total = __builtin_popcountll(hit) * kLane;
         for (int at = lane; at - lane < total; at += 64) {
           const int l = min(at / kLane, 63), e = at % kLane, i = e / kPer;
-          const float v = element<kBf16>(&words[wave][l][4 * i], e % kPer);
+          const float y = element<kBf16>(&words[wave][l][4 * i], e % kPer);
           const int64_t token = token_at(batch * kBatch + (int64_t)(i * 64 + lanes[wave][l]) * kPer) + e % kPer;
-          const uint64_t k = key_of(v, (int)token);
-          const uint64_t yes = __ballot(at < total && k >= least && v > -INFINITY);
+          const uint64_t k = key_of(y, (int)token);
+          const uint64_t yes = __ballot(at < total && k >= least && y > -INFINITY);
           if (!yes) continue;
           if (yes >> lane & 1) found[wave][n_found + __builtin_popcountll(yes & ((1ull << lane) - 1))] = k;
           n_found += __builtin_popcountll(yes);
@@ -291,7 +315,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
     if (n_found > 0) flush(n_found);
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
-    if (careful || !__any(!__builtin_isfinite(sum))) break;
+    ref = sum == 0 ? kNoRef : careful ? (double)top : (double)c * 0.69314718055994530942 + kOff * (double)top;
+    if (careful || !__any(!__builtin_isfinite(sum) || (sum == 0 && list != 0))) break;
   }
 
   // the waves' parts
@@ -304,13 +329,13 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
   }
   __syncthreads();
   if (wave > 0) return;
-  float top = refs[0];
+  ref = refs[lane & (kWaves - 1)];
+  double top = ref;
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, refs[w]);
-  sum = 0;
+  for (int i = 1; i < kWaves; i <<= 1) top = fmax(top, __shfl_xor(top, i));
+  sum = sums[lane & (kWaves - 1)] * exp(ref - top);
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w)
-    sum += sums[w] * (double)__builtin_amdgcn_exp2f((refs[w] - top) * 1.4426950408889634f);
+  for (int i = 1; i < kWaves; i <<= 1) sum += __shfl_xor(sum, i);
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) list = largest(list, lists[w][63 - lane]);
   const int64_t at = row * a.slices + slice;
@@ -337,7 +362,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a) 
     const uint64_t* const keys = a.keys + at * keep;
     const int up = 63 - lane;
     uint64_t list = lane < keep ? keys[lane] : 0, next = a.slices > 1 && up < keep ? keys[keep + up] : 0;
-    const float ref = lane < a.slices ? a.ref[at + lane] : kLowest;
+    const double ref = lane < a.slices ? a.ref[at + lane] : kNoRef;
     double sum = lane < a.slices ? a.sum[at + lane] : 0;
     const float c = a.scores[row];
     const uint8_t ended = a.done ? a.done[row] : 0;
@@ -350,10 +375,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a) 
         tokens[b * keep] = a.eos;
       }
     } else if (live) {
-      float top = ref;
+      double top = ref;
 #pragma unroll
-      for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
-      sum *= exp((double)ref - (double)top);
+      for (int i = 1; i < 64; i <<= 1) top = fmax(top, __shfl_xor(top, i));
+      sum *= exp(ref - top);
 #pragma unroll
       for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
       for (int s = 1; s < a.slices; ++s) {
@@ -364,10 +389,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a) 
       // A whole number of 2^-40, finer than the exponentials are: what is added to it in 64 bits
       // (logits and scores below 2^12 that are whole numbers of it as well) is added exactly, so
       // that scores which are equal by arithmetic compare equal.
-      const double all = rint(((double)top + log(sum)) * 0x1p40) * 0x1p-40;
+      // (Past 2^20 the logarithm is not to be lost in the reference.)
+      const double rest = log(sum), all = rint((top + rest) * 0x1p40) * 0x1p-40;
+      const bool far = fabs(top) > 0x1p20;
       n = __builtin_popcountll(__ballot(lane < keep && list != 0));
       if (lane < n) {
-        scores[b * keep + lane] = ((double)value_of(list) - all) + (double)c;
+        const double x = (double)value_of(list);
+        scores[b * keep + lane] = (far ? (x - top) - rest : x - all) + (double)c;
         tokens[b * keep + lane] = token_of_key(list);
       }
     }
@@ -424,7 +452,7 @@ BeamPlan make_beam_plan(const ckv_beams* b) {
   const int64_t want = std::max<int64_t>(1, std::min(most, ceil_div(kScanBlocks, std::max<int64_t>(rows, 1))));
   p.slice = (int32_t)ceil_div(batches, want);
   p.slices = (int32_t)ceil_div(batches, p.slice);
-  p.off_sum = align_up((size_t)rows * p.slices * sizeof(float), 256);
+  p.off_sum = align_up((size_t)rows * p.slices * sizeof(double), 256);
   p.off_keys = align_up(p.off_sum + (size_t)rows * p.slices * sizeof(double), 256);
   p.bytes = align_up(p.off_keys + (size_t)rows * p.slices * b->keep * sizeof(uint64_t), 256);
   return p;
@@ -475,7 +503,7 @@ ckv_status ckv_beam_select(const ckv_beams* beams, int32_t* parent, int32_t* tok
   char* const w = static_cast<char*>(ws);
   const BeamArgs a{static_cast<const char*>(beams->logits), beams->scores, beams->done,
                    beams->row_stride ? beams->row_stride : beams->vocab, beams->n_reqs, beams->n_beams,
-                   beams->vocab, beams->keep, beams->eos, p.slices, p.slice, reinterpret_cast<float*>(w),
+                   beams->vocab, beams->keep, beams->eos, p.slices, p.slice, reinterpret_cast<double*>(w),
                    reinterpret_cast<double*>(w + p.off_sum), reinterpret_cast<uint64_t*>(w + p.off_keys),
                    parent, token, score, done};
   const int64_t grid = (int64_t)beams->n_reqs * beams->n_beams * p.slices;

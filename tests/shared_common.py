@@ -171,10 +171,11 @@ def select_model(logits, scores, done, keep, eos):
             m = row.max()
             if m == -np.inf:
                 continue
-            lse = m + math.log(math.fsum(np.exp(row - m)))
+            rest = math.log(math.fsum(np.exp(row - m)))
             # (more than are kept of one beam are of no use)
             best = np.lexsort((np.arange(vocab), -row))[:keep]
-            offers += [(-((row[v] - lse) + c), b, -row[v], int(v), int(v == eos)) for v in best if row[v] > -np.inf]
+            offers += [(-math.fsum((row[v], -m, -rest, c)), b, -row[v], int(v), int(v == eos)) for v in best
+                       if row[v] > -np.inf]
         for i, (s, b, _, v, d) in enumerate(sorted(offers)[:keep]):
             parent[r, i], token[r, i], score[r, i], ended[r, i] = r * beams + b, v, -s, d
     return parent, token, score, ended
