@@ -8,6 +8,8 @@
 //   beam_join_kernel   a workgroup per request: the slices of each beam, then the beams
 // The scan is bound by reading the logits.
 
+#include <type_traits>
+
 #include "ckv_internal.h"
 
 namespace ckv {
@@ -123,224 +125,250 @@ __device__ __forceinline__ float element(const uint32_t* w, int e) {
   return __uint_as_float(w[e]);
 }
 
-// A wave goes over its batches, the next one's loads under way.  Of a batch, lanes take their
-// largest element; lanes that may hold one of the keep best put their elements into LDS,
-// where the wave looks at 64 of them at a time and collects those that do.  64 collected are
-// sorted and merged into the list that the lanes hold.  Typically few lanes have any.
-template <bool kBf16>
+// A wave goes over its batches, the next ones' loads under way, and takes of each the sum of the
+// exponentials and every lane's largest element: no more, so that the memory is kept busy.
+// Then keep lanes or so have all that can be among its keep largest: the lanes whose largest is
+// no less than the keep-th largest of the lanes'.  Their elements are read again (from the L2),
+// and those that are no less are collected in LDS.  64 collected are sorted and merged into the
+// list that the lanes hold: mostly a workgroup's waves together find fewer, and one sort at
+// the end does.
+// kTiny: fewer tokens than a piece.
+template <bool kBf16, bool kTiny>
 __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
   constexpr int kPer = kBf16 ? 8 : 4, kBytes = kBf16 ? 2 : 4;  // elements of a piece, bytes of one
-  constexpr int kLane = kPieces * kPer;                        // elements of a lane per batch
-  constexpr int kWords = 4 * kPieces;
-  __shared__ uint32_t words[kWaves][64][kWords];  // elements of the lanes looked at
+  constexpr int64_t kBatch = 64 * kPieces * kPer;
   __shared__ int32_t lanes[kWaves][64];
-  __shared__ uint64_t found[kWaves][2 * 64];
-  __shared__ double sums[kWaves];
-  __shared__ double refs[kWaves];
+  __shared__ uint64_t found[kWaves][64 * (1 + kPer)];  // a piece of every lane has room behind 63
+  __shared__ double sums[kWaves], refs[kWaves];
+  __shared__ int32_t counts[kWaves];
   const int64_t row = blockIdx.x / a.slices;
   const int slice = blockIdx.x % a.slices;
-  const float c = a.scores[row];
-  if (!(c > -INFINITY) || (a.done && a.done[row])) return;  // offers no token: the join knows
+  const float cum = a.scores[row];
+  if (!(cum > -INFINITY) || (a.done && a.done[row])) return;  // offers no token: the join knows
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Pieces count from the row's begin, wherever that lies: rows of equal logits are then added up
   // alike, and their scores tie as they should.
   const char* const base = a.logits + row * a.row_stride * kBytes;
   const int64_t end = a.vocab;
-  constexpr int64_t kBatch = 64 * kLane;
   const int64_t batches = (end + kBatch - 1) / kBatch;
-  const int64_t b0 = (int64_t)slice * a.slice, b1 = min(b0 + a.slice, batches);
+  const int64_t b0 = (int64_t)slice * a.slice + wave, b1 = min((int64_t)(slice + 1) * a.slice, batches);
+  const int n_batches = b0 < b1 ? (int)((b1 - b0 + kWaves - 1) / kWaves) : 0;  // this wave's: b0, b0 + kWaves ..
   const int keep = a.keep;
 
-  using Batch = u32x4[kPieces];
   // Element e of a piece that begins at p0 is of token token_at(p0) + e: a piece that would
   // reach past the row is the row's last one, where those before p0 count for nothing.
-  auto token_at = [&](int64_t p0) __attribute__((always_inline)) { return min(p0, max(end - kPer, (int64_t)0)); };
-  auto load = [&](int64_t batch, Batch& x) __attribute__((always_inline)) {
-    const int64_t e0 = batch * kBatch;
-    if (end >= kPer) {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) x[i] = piece_at(base + token_at(e0 + (i * 64 + lane) * kPer) * kBytes);
-    } else {  // fewer tokens than a piece: lane 0's
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) x[i] = u32x4{0u, 0u, 0u, 0u};
-      if (lane == 0)
-        for (int e = 0; e < (int)end; ++e) {
-          if constexpr (kBf16)
-            x[0][e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(base)[e] << 16 * (e & 1);
-          else
-            x[0][e] = reinterpret_cast<const uint32_t*>(base)[e];
-        }
-    }
+  using Batch = u32x4[kPieces];
+  auto piece_of = [&](int64_t batch, int i, int l) __attribute__((always_inline)) {
+    return batch * kBatch + (int64_t)(i * 64 + l) * kPer;
   };
-  auto clear_outside = [&](int64_t batch, Batch& x) __attribute__((always_inline)) {
-    const int64_t e0 = batch * kBatch;
+  auto token_at = [&](int64_t p0) __attribute__((always_inline)) { return kTiny ? 0 : min(p0, end - kPer); };
+  auto load = [&](int64_t p0) __attribute__((always_inline)) {
+    if constexpr (!kTiny) return piece_at(base + token_at(p0) * kBytes);
+    u32x4 x{0u, 0u, 0u, 0u};
+    for (int e = 0; e < (int)end; ++e) {
+      if constexpr (kBf16)
+        x[e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(base)[e] << 16 * (e & 1);
+      else
+        x[e] = reinterpret_cast<const uint32_t*>(base)[e];
+    }
+    return x;
+  };
+  // -infinity outside the piece's own tokens and, if `careful`, for NaN; the largest number for an infinity.
+  auto mend = [&](int64_t p0, bool outside, bool careful, u32x4& x) __attribute__((always_inline)) {
+    const int64_t at = token_at(p0);
+    const int from = (int)min(p0 - at, (int64_t)kPer), upto = (int)min(end - at, (int64_t)kPer);
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int64_t p0 = e0 + (i * 64 + lane) * kPer, at = token_at(p0);
-      const int from = (int)min(p0 - at, (int64_t)kPer), upto = (int)min(end - at, (int64_t)kPer);
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        if (e >= from && e < upto) continue;
-        if constexpr (kBf16)
-          x[i][e >> 1] = e & 1 ? (x[i][e >> 1] & 0xffffu) | 0xff800000u : (x[i][e >> 1] & 0xffff0000u) | 0xff80u;
-        else
-          x[i][e] = 0xff800000u;
+    for (int e = 0; e < kPer; ++e) {
+      const bool drop = outside && (e < from || e >= upto);
+      if constexpr (kBf16) {
+        uint32_t h = x[e >> 1] >> 16 * (e & 1) & 0xffffu;
+        if (careful) h = (h & 0x7fffu) > 0x7f80u ? 0xff80u : h == 0x7f80u ? 0x7f7fu : h;
+        h = drop ? 0xff80u : h;
+        x[e >> 1] = e & 1 ? (x[e >> 1] & 0xffffu) | h << 16 : (x[e >> 1] & 0xffff0000u) | h;
+      } else {
+        uint32_t h = x[e];
+        if (careful) h = (h & 0x7fffffffu) > 0x7f800000u ? 0xff800000u : h == 0x7f800000u ? 0x7f7fffffu : h;
+        x[e] = drop ? 0xff800000u : h;
       }
     }
   };
 
   double ref, sum;  // of exp(x - ref)
-  uint64_t list;    // this lane's of the 64 best so far
+  float mx;         // this lane's largest
   // The exponent x log2(e) - c is one fused step with c = log2(e) max, rounded: the reference is
   // c / log2(e) exactly, and what the factor's own rounding leaves, kOff x, is taken back for
   // x = max, off by kOff (max - x) for the others, a term that is as far below the largest.
-  // `careful`: NaN is taken for -infinity, an infinity for the largest number, and the
-  // exponent is (x - max) log2(e), as c may be past what 32 bits hold.  Such logits show in
-  // the sum, after which the slice is done again.
+  // `careful`: as in mend, and the exponent is (x - max) log2(e), as c may be past what 32 bits
+  // hold.  Such logits show in the sum, after which the slice is done again.
   constexpr float kLog2e = 1.4426950408889634f;
   constexpr double kOff = 1.0 - (double)kLog2e / 1.4426950408889634074;
-  for (bool careful = false;; careful = true) {
-    float top = careful ? kLowest : -0x1p125f, c = top * kLog2e;
+  float top, c;
+  auto clear = [&](float from) __attribute__((always_inline)) {
+    top = from;
+    c = top * kLog2e;
     sum = 0;
-    list = 0;
-    uint64_t least = kNoKey + 1;  // what the best have at least
-    int n_found = 0;
-    auto flush = [&](int n) __attribute__((always_inline)) {  // the n <= 64 first ones found
+    mx = -INFINITY;
+  };
+  auto take = [&](const Batch& x, auto careful) __attribute__((always_inline)) {
+    float v[kPieces * kPer];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const uint32_t w[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) v[i * kPer + e] = element<kBf16>(w, e);
+    }
+#pragma unroll
+    for (int e = 0; e < kPieces * kPer; e += 2) mx = max3(mx, v[e], v[e + 1]);
+    if (__any(mx > top)) {
+      float to = mx;
+#pragma unroll
+      for (int i = 1; i < 64; i <<= 1) to = fmaxf(to, __shfl_xor(to, i));
+      sum *= (double)__builtin_amdgcn_exp2f(careful ? (top - to) * kLog2e : c - to * kLog2e);
+      top = to;
+      c = to * kLog2e;
+    }
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < kPieces * kPer; ++e)
+      part[e & 3] += __builtin_amdgcn_exp2f(careful ? (v[e] - top) * kLog2e : fmaf(v[e], kLog2e, -c));
+    sum += (double)((part[0] + part[1]) + (part[2] + part[3]));
+  };
+  auto take_slow = [&](int n, auto careful) __attribute__((always_inline)) {
+    const int64_t batch = b0 + (int64_t)n * kWaves;
+    Batch x;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      x[i] = load(piece_of(batch, i, lane));
+      mend(piece_of(batch, i, lane), true, careful, x[i]);
+    }
+    take(x, careful);
+  };
+  auto all_lanes = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
+  };
+  clear(-0x1p125f);
+  {
+    // whole batches, two of them under way; the lanes' addresses are a common one and 16 bytes each
+    const int n_whole = n_batches - (b0 + (int64_t)n_batches * kWaves - kWaves + 1 > end / kBatch ? 1 : 0);
+    auto fetch = [&](int n, Batch& x) __attribute__((always_inline)) {  // (past the last: that one again)
+      const char* from = base + (b0 + (int64_t)min(n, n_whole - 1) * kWaves) * (kBatch * kBytes);
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) x[i] = piece_at(from + (uint32_t)(lane * 16) + i * 1024);
+    };
+    constexpr std::false_type plain{};
+    if (n_batches > 0 && n_whole > 0) {
+      Batch x, y, z;
+      fetch(0, x);
+      fetch(1, y);
+      for (int n = 0;; n += 3) {
+        fetch(n + 2, z);
+        take(x, plain);
+        if (n + 1 >= n_whole) break;
+        fetch(n + 3, x);
+        take(y, plain);
+        if (n + 2 >= n_whole) break;
+        fetch(n + 4, y);
+        take(z, plain);
+        if (n + 3 >= n_whole) break;
+      }
+    }
+    if (n_whole < n_batches) take_slow(n_batches - 1, plain);
+    all_lanes();
+  }
+  ref = (double)c * 0.69314718055994530942 + kOff * (double)top;
+  const bool careful = __any(!__builtin_isfinite(sum) || (sum == 0 && mx > -INFINITY));
+  if (careful) {
+    clear(kLowest);
+    for (int n = 0; n < n_batches; ++n) take_slow(n, std::true_type{});
+    all_lanes();
+    ref = (double)top;
+  }
+  if (sum == 0) ref = kNoRef;
+
+  // Bit by bit the largest number that keep lanes' largest reach, or one a little below it (as
+  // upper halves of keys); every number above -infinity where fewer lanes have any.
+  const uint32_t mine = (uint32_t)(key_of(mx, 0) >> 32);
+  uint32_t kth = 0;
+#pragma unroll
+  for (int bit = 31; bit >= (kBf16 ? 16 : 12); --bit) {
+    const uint32_t to = kth | 1u << bit;
+    if (__builtin_popcountll(__ballot(mine >= to)) >= keep) kth = to;
+  }
+  uint64_t least = max((uint64_t)kth << 32, kNoKey + 1);  // what the best have at least
+  uint64_t list = 0;                                      // this lane's of the 64 best so far
+  int n_found = 0;
+  bool flushed = false;  // the list has some
+  const uint64_t hit = __ballot(mine >= (uint32_t)(least >> 32));
+  if (hit >> lane & 1) lanes[wave][__builtin_amdgcn_mbcnt_hi(hit >> 32, __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0))] = lane;
+  wave_sync();
+  const int per_lane = n_batches * kPieces, total = __builtin_popcountll(hit) * per_lane;
+  for (int at = lane; at - lane < total; at += 64) {
+    const int l = min(at / max(per_lane, 1), 63), piece = at % max(per_lane, 1);
+    const int64_t p0 = piece_of(b0 + (int64_t)(piece / kPieces) * kWaves, piece % kPieces, lanes[wave][l]);
+    u32x4 x{0u, 0u, 0u, 0u};
+    if (at < total) {
+      x = load(p0);
+      mend(p0, true, careful, x);
+    }
+    const uint32_t w[4] = {x[0], x[1], x[2], x[3]};
+    const int first = (int)token_at(p0);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const uint64_t k = key_of(element<kBf16>(w, e), first + e);
+      const uint64_t yes = __ballot(at < total && k >= least);
+      if (!yes) continue;
+      if (yes >> lane & 1)
+        found[wave][n_found + __builtin_amdgcn_mbcnt_hi(yes >> 32, __builtin_amdgcn_mbcnt_lo((uint32_t)yes, 0))] = k;
+      n_found += __builtin_popcountll(yes);
+    }
+    while (n_found >= 64) {  // the last 64 found
+      n_found -= 64;
       wave_sync();
-      list = largest(list, sorted<true>(lane < n ? found[wave][lane] : 0));
+      list = largest(list, sorted<true>(found[wave][n_found + lane]));
       wave_sync();
       const uint64_t last = lane_of(list, keep - 1);
       least = last > least ? last : least;
-    };
-    Batch x, next;
-    int64_t batch = b0 + wave;
-    if (batch < b1) load(batch, x);
-    for (; batch < b1; batch += kWaves) {
-      if (batch + kWaves < b1) load(batch + kWaves, next);
-      if ((batch + 1) * kBatch > end) clear_outside(batch, x);
-      if (careful) {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint32_t v = x[i][w];
-            if constexpr (kBf16) {
-              uint32_t h[2] = {v & 0xffffu, v >> 16};
-#pragma unroll
-              for (int j = 0; j < 2; ++j) h[j] = (h[j] & 0x7fffu) > 0x7f80u ? 0xff80u : h[j] == 0x7f80u ? 0x7f7fu : h[j];
-              v = h[0] | h[1] << 16;
-            } else {
-              v = (v & 0x7fffffffu) > 0x7f800000u ? 0xff800000u : v == 0x7f800000u ? 0x7f7fffffu : v;
-            }
-            x[i][w] = v;
-          }
-      }
-      float v[kLane];
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const uint32_t w[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) v[i * kPer + e] = element<kBf16>(w, e);
-      }
-#pragma unroll
-      for (int e = 0; e < kLane; e += 2) mx = max3(mx, v[e], v[e + 1]);
-      if (__any(mx > top)) {
-        float to = mx;
-#pragma unroll
-        for (int i = 1; i < 64; i <<= 1) to = fmaxf(to, __shfl_xor(to, i));
-        const float by = careful ? (top - to) * kLog2e : c - to * kLog2e;
-        sum *= (double)__builtin_amdgcn_exp2f(by);
-        top = to;
-        c = to * kLog2e;
-      }
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
-      if (!careful) {
-#pragma unroll
-        for (int e = 0; e < kLane; ++e) part[e & 3] += __builtin_amdgcn_exp2f(fmaf(v[e], kLog2e, -c));
-      } else {
-#pragma unroll
-        for (int e = 0; e < kLane; ++e) part[e & 3] += __builtin_amdgcn_exp2f((v[e] - top) * kLog2e);
-      }
-      sum += (double)((part[0] + part[1]) + (part[2] + part[3]));
-
-      // (the threshold as a logit: a little wide where tokens decide)
-      const float at_least = value_of(least);
-      uint64_t hit = __ballot(mx >= at_least);
-      if (hit) {
-        if (__builtin_popcountll(hit) >= keep) {
-          // keep lanes have an element each that is no less than the keep-th lane's largest, or
-          // than a number a little below it: bit by bit the largest that keep lanes reach
-          const uint32_t mine = (uint32_t)(key_of(mx, 0) >> 32);
-          uint32_t kth = 0;
-#pragma unroll
-          for (int bit = 31; bit >= (kBf16 ? 16 : 12); --bit) {
-            const uint32_t to = kth | 1u << bit;
-            if (__builtin_popcountll(__ballot(mine >= to)) >= keep) kth = to;
-          }
-          const uint64_t bound = (uint64_t)kth << 32;
-          least = bound > least ? bound : least;
-          hit = __ballot(mine >= (uint32_t)(least >> 32));
-        }
-        if (hit >> lane & 1) {
-          const int at = __builtin_popcountll(hit & ((1ull << lane) - 1));
-          lanes[wave][at] = lane;
-#pragma unroll
-          for (int i = 0; i < kPieces; ++i) *reinterpret_cast<u32x4*>(&words[wave][at][4 * i]) = x[i];
-        }
-        wave_sync();
-        const int total = __builtin_popcountll(hit) * kLane;
-        for (int at = lane; at - lane < total; at += 64) {
-          const int l = min(at / kLane, 63), e = at % kLane, i = e / kPer;
-          const float y = element<kBf16>(&words[wave][l][4 * i], e % kPer);
-          const int64_t token = token_at(batch * kBatch + (int64_t)(i * 64 + lanes[wave][l]) * kPer) + e % kPer;
-          const uint64_t k = key_of(y, (int)token);
-          const uint64_t yes = __ballot(at < total && k >= least && y > -INFINITY);
-          if (!yes) continue;
-          if (yes >> lane & 1) found[wave][n_found + __builtin_popcountll(yes & ((1ull << lane) - 1))] = k;
-          n_found += __builtin_popcountll(yes);
-          if (n_found >= 64) {
-            flush(64);
-            n_found -= 64;
-            const uint64_t rest = found[wave][64 + lane];
-            wave_sync();
-            found[wave][lane] = rest;
-          }
-        }
-        wave_sync();
-      }
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) x[i] = next[i];
+      flushed = true;
     }
-    if (n_found > 0) flush(n_found);
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) sum += __shfl_xor(sum, i);
-    ref = sum == 0 ? kNoRef : careful ? (double)top : (double)c * 0.69314718055994530942 + kOff * (double)top;
-    if (careful || !__any(!__builtin_isfinite(sum) || (sum == 0 && list != 0))) break;
   }
 
-  // the waves' parts
-  __syncthreads();
-  uint64_t(&lists)[kWaves][64] = *reinterpret_cast<uint64_t(*)[kWaves][64]>(&words[0][0][0]);
-  lists[wave][lane] = list;
+  // The waves' parts.  What they found is mostly 64 keys at most: one wave then sorts it all.
   if (lane == 0) {
     sums[wave] = sum;
     refs[wave] = ref;
+    counts[wave] = flushed ? 65 : n_found;
   }
   __syncthreads();
-  if (wave > 0) return;
-  ref = refs[lane & (kWaves - 1)];
-  double top = ref;
+  int before[kWaves + 1] = {0};
 #pragma unroll
-  for (int i = 1; i < kWaves; i <<= 1) top = fmax(top, __shfl_xor(top, i));
-  sum = sums[lane & (kWaves - 1)] * exp(ref - top);
+  for (int w = 0; w < kWaves; ++w) before[w + 1] = before[w] + counts[w];
+  if (before[kWaves] > 64) {  // (the same for all waves)
+    list = largest(list, sorted<true>(lane < n_found ? found[wave][lane] : 0));
+    wave_sync();
+    found[wave][lane] = list;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) list = largest(list, found[w][63 - lane]);
+  } else {
+    if (wave > 0) return;
+    uint64_t k = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      if (lane >= before[w] && lane < before[w + 1]) k = found[w][lane - before[w]];
+    list = sorted<false>(k);
+  }
+  ref = refs[lane & (kWaves - 1)];
+  double most = ref;
+#pragma unroll
+  for (int i = 1; i < kWaves; i <<= 1) most = fmax(most, __shfl_xor(most, i));
+  sum = sums[lane & (kWaves - 1)] * exp(ref - most);
 #pragma unroll
   for (int i = 1; i < kWaves; i <<= 1) sum += __shfl_xor(sum, i);
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) list = largest(list, lists[w][63 - lane]);
   const int64_t at = row * a.slices + slice;
   if (lane == 0) {
-    a.ref[at] = top;
+    a.ref[at] = most;
     a.sum[at] = sum;
   }
   if (lane < keep) a.keys[at * keep + lane] = list;
@@ -509,10 +537,10 @@ ckv_status ckv_beam_select(const ckv_beams* beams, int32_t* parent, int32_t* tok
   const int64_t grid = (int64_t)beams->n_reqs * beams->n_beams * p.slices;
   if (grid >= kMaxScanGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
   const hipStream_t st = (hipStream_t)stream;
-  if (beams->dtype == CKV_DTYPE_BF16)
-    hipLaunchKernelGGL(beam_scan_kernel<true>, dim3((unsigned)grid), dim3(64 * kWaves), 0, st, a);
-  else
-    hipLaunchKernelGGL(beam_scan_kernel<false>, dim3((unsigned)grid), dim3(64 * kWaves), 0, st, a);
+  const auto kernel = beams->dtype == CKV_DTYPE_BF16
+                          ? (beams->vocab < 8 ? beam_scan_kernel<true, true> : beam_scan_kernel<true, false>)
+                          : (beams->vocab < 4 ? beam_scan_kernel<false, true> : beam_scan_kernel<false, false>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWaves), 0, st, a);
   CKV_HIP(hipGetLastError());
   const size_t lds = (size_t)a.n_beams * (a.keep * (sizeof(double) + sizeof(int32_t)) + sizeof(int32_t));
   hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)beams->n_reqs), dim3(64 * kJoinWaves), lds, st, a);
