@@ -270,11 +270,14 @@ __device__ __forceinline__ uint32_t finite_codes(uint32_t w) {
 // sequence of 1,000 tokens takes 6.6 us: four dependent round trips, two steps per wave of 0.9,
 // the waves' join 0.4.
 // kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page).
-template <int D, int T, bool kSmall, int kWaves, int P>
+// kBlocks: 16-row blocks of a workgroup, which share the keys as loaded, converted and turned over
+// (their query rows then come from LDS).
+template <int D, int T, bool kSmall, int kWaves, int P, int kBlocks>
 __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(PageAttnArgs a) {
   using E = Elem<T>;
   using QT = typename E::Q;
   constexpr bool kF32 = T == CKV_DTYPE_F32, kE4 = T == CKV_DTYPE_E4M3;
+  static_assert(kBlocks == 1 || !kF32);
   constexpr int kVec = D / 16;                    // elements of a V row per lane, and products of O
   constexpr int kRow = D * E::kBytes;             // bytes of a K row in LDS
   constexpr int kPieces = kRow / 64;              // 16-byte pieces of a K row per lane
@@ -329,37 +332,64 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
   for (int y = 0; y < kPieces; ++y) k_at[y] = (uint32_t)(n16 * kRow + (((j4 + 4 * y) ^ swz(n16)) * 16));
   const uint32_t v_col = (uint32_t)(4 * j4 * row_bytes + g_bytes + n16 * kVec * E::kBytes);
 
-  for (int rb = blockIdx.y; rb * kRows < rows; rb += gridDim.y) {
-    const int r_first = rb * kRows, r_last = min(rows, r_first + kRows) - 1;
+  constexpr int kQRow = D + 8;  // of the query rows in LDS: 16 lanes in a column of pieces meet all banks
+  __shared__ __attribute__((aligned(16))) uint16_t lds_q[kBlocks > 1 ? kBlocks * kRows * kQRow : 1];
+
+  for (int rb = blockIdx.y; rb * (kRows * kBlocks) < rows; rb += gridDim.y) {
+    const int r_first = rb * (kRows * kBlocks), r_last = min(rows, r_first + kRows * kBlocks) - 1;
     const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
     const Steps steps = steps_of<P>(a, p0, p1, unit.first, kv_end);
     const int per = steps.n / n_parts, over = steps.n % n_parts;  // the first `over` splits: one more
     const int begin = split * per + min(split, over), end = begin + per + (split < over ? 1 : 0);
 
-    // this lane's row: its query (position p) and head
-    const int r = min(r_first + n16, r_last);
-    const int64_t tok = sp.first + r / a.G;
-    const int head = g * a.G + r % a.G, p = p_base + r / a.G;
-    const QT* q = static_cast<const QT*>(a.q) + (tok * a.Hq + head) * D;
+    // this lane's row of each block: its query (position p) and head
+    int p[kBlocks];
+    const QT* q[kBlocks];
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) {
+      const int r = min(r_first + kRows * k + n16, r_last);
+      const int64_t tok = sp.first + r / a.G;
+      const int head = g * a.G + r % a.G;
+      p[k] = p_base + r / a.G;
+      q[k] = static_cast<const QT*>(a.q) + (tok * a.Hq + head) * D;
+    }
     // Q^T operands in the order of the K pieces
     f32x4 qf[kF32 ? kPieces : 1];
-    bf16x8 qb[kF32 ? 1 : D / 32];
+    bf16x8 qb[kF32 || kBlocks > 1 ? 1 : D / 32];
+    const auto q_piece = [&](int i) { return kE4 ? 64 * (i >> 1) + 16 * j4 + 8 * (i & 1) : 32 * i + 8 * j4; };
     if constexpr (kF32) {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) qf[i] = *reinterpret_cast<const f32x4*>(q + 16 * i + 4 * j4);
-    } else if constexpr (kE4) {
+      for (int i = 0; i < kPieces; ++i) qf[i] = *reinterpret_cast<const f32x4*>(q[0] + 16 * i + 4 * j4);
+    } else if constexpr (kBlocks == 1) {
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        qb[i] = *reinterpret_cast<const bf16x8*>(q + 64 * (i >> 1) + 16 * j4 + 8 * (i & 1));
+      for (int i = 0; i < D / 32; ++i) qb[i] = *reinterpret_cast<const bf16x8*>(q[0] + q_piece(i));
     } else {
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) qb[i] = *reinterpret_cast<const bf16x8*>(q + 32 * i + 8 * j4);
+      // each wave brings some of the rows
+      constexpr int kSegsQ = D / 8;
+      for (int i = threadIdx.x; i < kBlocks * kRows * kSegsQ; i += 64 * kWaves) {
+        const int r = min(r_first + i / kSegsQ, r_last);
+        const QT* from = static_cast<const QT*>(a.q) + ((sp.first + r / a.G) * a.Hq + g * a.G + r % a.G) * D;
+        *reinterpret_cast<u32x4*>(lds_q + i / kSegsQ * kQRow + i % kSegsQ * 8) =
+            *reinterpret_cast<const u32x4*>(from + i % kSegsQ * 8);
+      }
+      __syncthreads();
     }
+    const auto query = [&](int k, int i) __attribute__((always_inline)) {
+      if constexpr (kBlocks == 1)
+        return qb[i];
+      else
+        return *reinterpret_cast<const bf16x8*>(lds_q + (kRows * k + n16) * kQRow + q_piece(i));
+    };
 
-    f32x4 o[kVec];
+    f32x4 o[kBlocks][kVec];
+    float ref[kBlocks], l[kBlocks];
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float ref = kNone, l = 0.f;
+    for (int k = 0; k < kBlocks; ++k) {
+      ref[k] = kNone;
+      l[k] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) o[k][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 
     // The table entries of a step's groups of keys.
     constexpr int kGroup = kSmall ? 8 : 16;
@@ -468,9 +498,11 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
           }
         }
       }
-      f32x4 s[2];
+      f32x4 s[kBlocks][2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s[k][i] = f32x4{0.f, 0.f, 0.f, 0.f};
       if constexpr (kF32) {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y)
@@ -478,22 +510,26 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
           for (int z = 0; z < 4; ++z)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-              s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[i][y][z]), qf[y][z], s[i], 0, 0, 0);
-      } else if constexpr (kE4) {
-#pragma unroll
-        for (int y = 0; y < D / 32; ++y)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                bf16_of_codes(kw[i][y >> 1][2 * (y & 1)], kw[i][y >> 1][2 * (y & 1) + 1], ks[i]), qb[y],
-                s[i], 0, 0, 0);
+              s[0][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[i][y][z]), qf[y][z], s[0][i], 0, 0, 0);
       } else {
 #pragma unroll
-        for (int y = 0; y < D / 32; ++y)
+        for (int y = 0; y < D / 32; ++y) {
+          bf16x8 kb[2];
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-            s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kw[i][y]), qb[y],
-                                                           s[i], 0, 0, 0);
+          for (int i = 0; i < 2; ++i) {
+            if constexpr (kE4)
+              kb[i] = bf16_of_codes(kw[i][y >> 1][2 * (y & 1)], kw[i][y >> 1][2 * (y & 1) + 1], ks[i]);
+            else
+              kb[i] = __builtin_bit_cast(bf16x8, kw[i][y]);
+          }
+#pragma unroll
+          for (int k = 0; k < kBlocks; ++k) {
+            const bf16x8 qy = query(k, y);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              s[k][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[i], qy, s[k][i], 0, 0, 0);
+          }
+        }
       }
       // what some row of the block must not see
       const int last = pos0 + kTile;
@@ -511,8 +547,10 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
           for (int y = 0; y < 4; ++y) {
             const int pos = pos0 + 16 * i + 4 * j4 + y;
             const bool there = names_page(a, page) && pos < kv_end;
-            if (!(there && pos <= p && (a.window <= 0 || pos > p - a.window || pos < a.sinks)))
-              s[i][y] = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < kBlocks; ++k)
+              if (!(there && pos <= p[k] && (a.window <= 0 || pos > p[k] - a.window || pos < a.sinks)))
+                s[k][i][y] = -INFINITY;
             // a weight of 0 does not undo a NaN: rows that no query of the block sees are cleared
             if (!(there && pos <= p1 && (pos > lo || pos < a.sinks)))
 #pragma unroll
@@ -520,30 +558,40 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
           }
         }
       }
-      float mx = -INFINITY;
+      u32x4 pb[kF32 ? 1 : kBlocks];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int k = 0; k < kBlocks; ++k) {
+        float mx = -INFINITY;
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          s[i][y] *= a.c1;
-          mx = fmaxf(mx, s[i][y]);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            s[k][i][y] *= a.c1;
+            mx = fmaxf(mx, s[k][i][y]);
+          }
+        if (__any(mx > ref[k] + kSlack)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          const float to = fmaxf(mx, ref[k]), f = __builtin_amdgcn_exp2f(ref[k] - to);
+          ref[k] = to;
+          l[k] *= f;
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) o[k][i] *= f;
         }
-      if (__any(mx > ref + kSlack)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float to = fmaxf(mx, ref), f = __builtin_amdgcn_exp2f(ref - to);
-        ref = to;
-        l *= f;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) o[i] *= f;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            s[k][i][y] = __builtin_amdgcn_exp2f(s[k][i][y] - ref[k]);
+            if constexpr (kF32) l[k] += s[k][i][y];
+          }
+        if constexpr (!kF32)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pb[k][i] = bf16_pair(s[k][i >> 1][2 * (i & 1)], s[k][i >> 1][2 * (i & 1) + 1]);
+            l[k] = add_pair(pb[k][i], l[k]);
+          }
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          s[i][y] = __builtin_amdgcn_exp2f(s[i][y] - ref);
-          if constexpr (kF32) l += s[i][y];
-        }
       if constexpr (kF32) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -551,14 +599,8 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
           for (int y = 0; y < 4; ++y)
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-              o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][y][e]), s[i][y], o[e], 0, 0, 0);
+              o[0][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][y][e]), s[0][i][y], o[0][e], 0, 0, 0);
       } else {
-        u32x4 pb;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          pb[i] = bf16_pair(s[i >> 1][2 * (i & 1)], s[i >> 1][2 * (i & 1) + 1]);
-          l = add_pair(pb[i], l);
-        }
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           u32x4 vt;  // element e of the 8 keys
@@ -576,8 +618,10 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
               vt[i] = __builtin_amdgcn_perm(r1[e >> 1], r0[e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
             }
           }
-          o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt),
-                                                         __builtin_bit_cast(bf16x8, pb), o[e], 0, 0, 0);
+#pragma unroll
+          for (int k = 0; k < kBlocks; ++k)
+            o[k][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt),
+                                                              __builtin_bit_cast(bf16x8, pb[k]), o[k][e], 0, 0, 0);
         }
       }
     };
@@ -665,55 +709,59 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
       }
     }
 
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    __syncthreads();  // every wave is through with its K rows
-    // o[x][v] holds element kVec (4 j4 + v) + x of row n16
 #pragma unroll
-    for (int v = 0; v < 4; ++v)
+    for (int k = 0; k < kBlocks; ++k) {
+      l[k] += __shfl_xor(l[k], 16);
+      l[k] += __shfl_xor(l[k], 32);
+      __syncthreads();  // every wave is through with its K rows (the block before is written)
+      // o[x][v] holds element kVec (4 j4 + v) + x of row n16
 #pragma unroll
-      for (int x = 0; x < kVec; ++x) joined.o[wave][n16][kVec * (4 * j4 + v) + x] = o[x][v];
-    if (lane < kRows) joined.ml[wave][lane] = make_float2(ref, l);
-    __syncthreads();
-    // 16 threads per row, D / 16 elements each
-    const int row = threadIdx.x >> 4, col = (threadIdx.x & 15) * kVec;
-    const int rr = r_first + row;
-    if (row < kRows && rr <= r_last) {
-      float M = kNone, L = 0.f, f[kWaves], acc[kVec];
+      for (int v = 0; v < 4; ++v)
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, joined.ml[w][row].x);
+        for (int x = 0; x < kVec; ++x) joined.o[wave][n16][kVec * (4 * j4 + v) + x] = o[k][x][v];
+      if (lane < kRows) joined.ml[wave][lane] = make_float2(ref[k], l[k]);
+      __syncthreads();
+      // 16 threads per row, D / 16 elements each
+      const int row = threadIdx.x >> 4, col = (threadIdx.x & 15) * kVec;
+      const int rr = r_first + kRows * k + row;
+      if (row < kRows && rr <= r_last) {
+        float M = kNone, L = 0.f, f[kWaves], acc[kVec];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(joined.ml[w][row].x - M);
-        L += f[w] * joined.ml[w][row].y;
-      }
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, joined.ml[w][row].x);
 #pragma unroll
-      for (int x = 0; x < kVec; ++x) {
-        acc[x] = 0.f;
+        for (int w = 0; w < kWaves; ++w) {
+          f[w] = __builtin_amdgcn_exp2f(joined.ml[w][row].x - M);
+          L += f[w] * joined.ml[w][row].y;
+        }
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) acc[x] += f[w] * joined.o[w][row][col + x];
-      }
-      const int64_t at = (sp.first + rr / a.G) * a.Hq + g * a.G + rr % a.G;
-      if (P == kShared || n_parts > 1 || (P == kOwn && unit.first > 0)) {
-        const int64_t prow = (int64_t)split * a.s.n_tokens * a.Hq + at;
-        float* dst = a.o_part + prow * D + col;
+        for (int x = 0; x < kVec; ++x) {
+          acc[x] = 0.f;
 #pragma unroll
-        for (int x = 0; x < kVec; x += 4)
-          *reinterpret_cast<f32x4*>(dst + x) = f32x4{acc[x], acc[x + 1], acc[x + 2], acc[x + 3]};
-        if (col == 0) a.ml_part[prow] = make_float2(M, L);
-      } else {
-        const float inv = L > 0.f ? 1.f / L : 0.f;
-        QT y[kVec];
+          for (int w = 0; w < kWaves; ++w) acc[x] += f[w] * joined.o[w][row][col + x];
+        }
+        const int64_t at = (sp.first + rr / a.G) * a.Hq + g * a.G + rr % a.G;
+        if (P == kShared || n_parts > 1 || (P == kOwn && unit.first > 0)) {
+          const int64_t prow = (int64_t)split * a.s.n_tokens * a.Hq + at;
+          float* dst = a.o_part + prow * D + col;
 #pragma unroll
-        for (int x = 0; x < kVec; ++x) y[x] = (QT)(acc[x] * inv);
-        char* dst = reinterpret_cast<char*>(static_cast<QT*>(a.out) + at * D + col);
-        if constexpr (sizeof y == 16)
-          *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(y);
-        else
-          *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(y);
+          for (int x = 0; x < kVec; x += 4)
+            *reinterpret_cast<f32x4*>(dst + x) = f32x4{acc[x], acc[x + 1], acc[x + 2], acc[x + 3]};
+          if (col == 0) a.ml_part[prow] = make_float2(M, L);
+        } else {
+          const float inv = L > 0.f ? 1.f / L : 0.f;
+          QT y[kVec];
+#pragma unroll
+          for (int x = 0; x < kVec; ++x) y[x] = (QT)(acc[x] * inv);
+          char* dst = reinterpret_cast<char*>(static_cast<QT*>(a.out) + at * D + col);
+          if constexpr (sizeof y == 16)
+            *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(y);
+          else
+            *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(y);
+        }
       }
     }
-    if (rb + (int)gridDim.y < (rows + kRows - 1) / kRows) __syncthreads();  // read, before the next block's K rows come
+    if (rb + (int)gridDim.y < (rows + kRows * kBlocks - 1) / (kRows * kBlocks))
+      __syncthreads();  // read, before the next block's K rows come
   }
 }
 
@@ -1307,12 +1355,14 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
 }
 
 // Bytes of shared pages read again and again that are worth the parts' launch and join.
+constexpr int64_t kMidBlocks = 512;
 constexpr int64_t kWorthParts = int64_t(24) << 20;
 
 struct PageAttnPlan {
   bool wide;       // page_tile_kernel
   int n_splits, slice;
-  int row_blocks;  // page_rows_kernel: grid y
+  int row_blocks;  // page_rows_kernel: grid y, and its kBlocks
+  int per_block;
   int64_t blocks;  // page_tile_kernel: blocks of rows, at most
   size_t off_ml, off_n, bytes;
 };
@@ -1330,11 +1380,14 @@ int64_t longest(const ckv_page_pool* pool, const ckv_page_batch* b) {
 // The launch for n_units units of up to `most` of the n_tokens tokens, which see up to `len`
 // keys; tile_blocks: about how many blocks of 128 rows they are.
 PageAttnPlan plan_units(const ckv_page_pool* pool, int Hq, int n_units, int64_t n_tokens, int64_t most, int64_t len,
-                        int64_t tile_blocks, int window, int sinks) {
+                        int64_t tile_blocks, int window, int sinks, bool many_blocks) {
   PageAttnPlan p{};
   const int G = Hq / pool->n_kv_heads;
   // (both sides: top of the file; one kernel for the call, by its longest sequence)
-  p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32;
+  p.per_block = 1;
+  if (many_blocks && pool->dtype != CKV_DTYPE_F32 && most * G > kRows && most * G <= 4 * kRows)
+    p.per_block = (int)ceil_div(most * G, kRows);
+  p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32 && p.per_block == 1;
   if (p.wide) {
     p.blocks = n_tokens * G / tile::kBlockRows + n_units;
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + ceil_div(tile::kBlockRows, G) + sinks + 16);
@@ -1362,14 +1415,14 @@ PageAttnPlan plan_units(const ckv_page_pool* pool, int Hq, int n_units, int64_t 
       }
     }
   } else {
-    p.row_blocks = (int)std::min<int64_t>(65535, std::max<int64_t>(1, ceil_div(most * G, kRows)));
+    p.row_blocks = (int)std::min<int64_t>(65535, std::max<int64_t>(1, ceil_div(most * G, kRows * p.per_block)));
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + most + sinks + 2 * kTile);
     const int64_t steps = ceil_div(len, kTile);
     const int64_t wgs = (int64_t)n_units * pool->n_kv_heads * p.row_blocks;
     // Splits of 16 steps or more (a sequence of 1,026 steps: 14.0 us; of 12: 15.8, of 24: 14.5),
     // up to 4,096 workgroups, so that sequences of unequal lengths spread over the chip (64
     // of 1,024 to 16,384 tokens: 165 us; up to 2,048: 183, up to 8,192: 170).
-    p.n_splits = (int)std::max<int64_t>(1, std::min(4096 / std::max<int64_t>(wgs, 1), steps / 16));
+    p.n_splits = (int)std::max<int64_t>(1, std::min((p.per_block > 1 ? kMidBlocks : 4096) / std::max<int64_t>(wgs, 1), steps / 16));
     p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
   }
   if (n_tokens * Hq >= kMaxGrid) p.n_splits = 1;  // (the join has a workgroup per row)
@@ -1380,7 +1433,7 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
   // (sequences' last blocks are taken as full: many short ones are more workgroups than this)
   const int64_t blocks = b->n_tokens * (Hq / pool->n_kv_heads) / tile::kBlockRows + 1;
   PageAttnPlan p = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most_tokens(b->max_tokens, b->n_tokens, b->n_seqs),
-                              longest(pool, b), blocks, window, sinks);
+                              longest(pool, b), blocks, window, sinks, false);
   const size_t rows = (size_t)b->n_tokens * Hq;
   if (p.n_splits > 1) {
     p.off_ml = align_up((size_t)p.n_splits * rows * pool->head_dim * sizeof(float), 256);
@@ -1415,10 +1468,10 @@ SharedPlan make_shared_plan(const ckv_page_pool* pool, const ckv_page_batch* b, 
     return std::min(b->n_tokens * G / tile::kBlockRows + units, units * ceil_div(most_of * G, tile::kBlockRows));
   };
   const int64_t most_group = most_tokens(g->max_tokens, b->n_tokens, g->n_groups);
-  p.shared = plan_units(pool, Hq, g->n_groups, b->n_tokens, most_group, shared_len, blocks(g->n_groups, most_group), 0, 0);
+  p.shared = plan_units(pool, Hq, g->n_groups, b->n_tokens, most_group, shared_len, blocks(g->n_groups, most_group), 0, 0, true);
   // (own keys: what the longest sequence has behind the longest prefix, a page at least)
   const int64_t own_len = std::max<int64_t>(len - shared_len, pool->page_size);
-  p.own = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most, own_len, blocks(b->n_seqs, most), 0, 0);
+  p.own = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most, own_len, blocks(b->n_seqs, most), 0, 0, false);
   const size_t rows = (size_t)b->n_tokens * Hq, places = (size_t)p.shared.n_splits + p.own.n_splits;
   p.off_ml = align_up(places * rows * pool->head_dim * sizeof(float), 256);
   p.off_shared = align_up(p.off_ml + places * rows * sizeof(float2), 256);
@@ -1459,9 +1512,14 @@ ckv_status launch_units(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) 
     // A launch of at most a workgroup per CU has 8 waves in each, whose fewer steps follow
     // one another (16 sequences of 4 tokens: 13.1 -> 11.7 us, fp32 prompts 8.7 -> 8.0); where
     // there are more, 4 (48 sequences: 80 us, with 8: 94).
-    const bool eight = wgs * p.row_blocks <= 256;
-    const auto kernel = a.c == 8 ? (eight ? page_rows_kernel<D, T, true, 8, P> : page_rows_kernel<D, T, true, 4, P>)
-                                 : (eight ? page_rows_kernel<D, T, false, 8, P> : page_rows_kernel<D, T, false, 4, P>);
+    const bool eight = wgs * p.row_blocks <= 256 && p.per_block == 1;
+    auto kernel = a.c == 8 ? (eight ? page_rows_kernel<D, T, true, 8, P, 1> : page_rows_kernel<D, T, true, 4, P, 1>)
+                           : (eight ? page_rows_kernel<D, T, false, 8, P, 1> : page_rows_kernel<D, T, false, 4, P, 1>);
+    if constexpr (P == kShared && T != CKV_DTYPE_F32) {
+      if (p.per_block == 2) kernel = a.c == 8 ? page_rows_kernel<D, T, true, 4, P, 2> : page_rows_kernel<D, T, false, 4, P, 2>;
+      if (p.per_block == 3) kernel = a.c == 8 ? page_rows_kernel<D, T, true, 4, P, 3> : page_rows_kernel<D, T, false, 4, P, 3>;
+      if (p.per_block == 4) kernel = a.c == 8 ? page_rows_kernel<D, T, true, 4, P, 4> : page_rows_kernel<D, T, false, 4, P, 4>;
+    }
     hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)p.row_blocks), dim3(eight ? 512 : 256), 0, st, a);
   }
   CKV_HIP(hipGetLastError());
