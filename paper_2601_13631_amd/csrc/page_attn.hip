@@ -272,8 +272,31 @@ __device__ __forceinline__ uint32_t finite_codes(uint32_t w) {
 // kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page).
 // kBlocks: 16-row blocks of a workgroup, which share the keys as loaded, converted and turned over
 // (their query rows then come from LDS).
-template <int D, int T, bool kSmall, int kWaves, int P, int kBlocks>
-__global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(PageAttnArgs a) {
+// Where its waves' K rows lie in LDS, after the last step their outputs with references and sums,
+// and the query rows: its own memory, or that of another kernel's part in one launch.
+template <int D, int T, int kWaves, int kBlocks>
+struct RowsLds {
+  // 8 waves have about two steps each (a launch of so few workgroups has splits of 16): both
+  // are loaded before the first is waited for (one sequence of 32,801 tokens in 8 bits 14.5 ->
+  // 14.1 us, 16 of up to 8,000 11.4 -> 11.1).
+  static constexpr bool kPairs = kWaves == 8;
+  static constexpr int kBuf = (kPairs ? 2 : 1) * kTile * D * Elem<T>::kBytes;  // of a wave
+  static constexpr int kOut = kRows * (D + 4) * (int)sizeof(float);
+  static constexpr int kJoined = kWaves * (kOut + kRows * (int)sizeof(float2));
+  static constexpr int kQRow = D + 8;  // of the query rows: 16 lanes in a column of pieces meet all banks
+  static constexpr int kQ = kBlocks > 1 ? kBlocks * kRows * kQRow * 2 : 0;
+  static constexpr int kBytes = kJoined > kWaves * kBuf ? kJoined : kWaves * kBuf;
+  char* lds;
+  uint16_t* q;
+  __device__ __forceinline__ char* mine_k(int wave) const { return lds + wave * kBuf; }
+  __device__ __forceinline__ float* mine_o(int wave) const { return o(wave); }
+  __device__ __forceinline__ float* o(int w) const { return reinterpret_cast<float*>(lds + w * kOut); }
+  __device__ __forceinline__ float2* ml(int w) const { return reinterpret_cast<float2*>(lds + kWaves * kOut) + w * kRows; }
+};
+
+// (bx, by) of a grid gy high.
+template <int D, int T, bool kSmall, int kWaves, int P, int kBlocks, class Lds>
+__device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, uint32_t by, uint32_t gy, const Lds& lds) {
   using E = Elem<T>;
   using QT = typename E::Q;
   constexpr bool kF32 = T == CKV_DTYPE_F32, kE4 = T == CKV_DTYPE_E4M3;
@@ -286,9 +309,9 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
   // The KV heads of one slice of keys are neighbours on one XCD, where together they read
   // whole token rows.  The slices go round the XCDs, every sequence's first ones before the
   // second ones and so on, turned by one from split to split: long sequences spread.
-  const uint32_t pair = blockIdx.x / 8 / a.Hkv * 8 + (blockIdx.x & 7), units = n_units<P>(a);
+  const uint32_t pair = bx / 8 / a.Hkv * 8 + (bx & 7), units = n_units<P>(a);
   if (pair >= units * a.n_splits) return;
-  const int g = (int)(blockIdx.x / 8 % a.Hkv), split = (int)(pair / units);
+  const int g = (int)(bx / 8 % a.Hkv), split = (int)(pair / units);
   const int b = (int)((pair + split) % units);
   const int lane = threadIdx.x & 63, n16 = lane & 15, j4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -303,24 +326,12 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
   // this sequence's own number of splits, by its length
   const int all_steps = steps_of<P>(a, p_base, p_base + sp.count - 1, unit.first, kv_end).n;
   const int n_parts = parts_of<P>(a, unit, all_steps);
-  if ((P != kWhole || a.n_splits > 1) && split == 0 && g == 0 && blockIdx.y == 0)
+  if ((P != kWhole || a.n_splits > 1) && split == 0 && g == 0 && by == 0)
     for (int i = threadIdx.x; i < sp.count; i += 64 * kWaves) a.n_parts[sp.first + i] = parts_note<P>(unit, n_parts);
   if (split >= n_parts) return;
 
-  // the waves' K buffers, and after the last step their outputs
-  struct Joined {
-    float o[kWaves][kRows][D + 4];
-    float2 ml[kWaves][kRows];
-  };
-  // 8 waves have about two steps each (a launch of so few workgroups has splits of 16): both
-  // are loaded before the first is waited for (one sequence of 32,801 tokens in 8 bits 14.5 ->
-  // 14.1 us, 16 of up to 8,000 11.4 -> 11.1).
   constexpr bool kPairs = kWaves == 8;
-  constexpr int kBuf = (kPairs ? 2 : 1) * kTile * kRow;  // of a wave
-  constexpr int kLds = sizeof(Joined) > kWaves * kBuf ? sizeof(Joined) : kWaves * kBuf;
-  __shared__ __attribute__((aligned(16))) char lds[kLds];
-  Joined& joined = *reinterpret_cast<Joined*>(lds);
-  char* lds_k = lds + wave * kBuf;
+  char* const lds_k = lds.mine_k(wave);
   // A load to LDS moves kLoadRows rows, lane l 16 bytes of row l / kSegs: the segment at
   // position s of row r is segment s ^ swz(r), so that 16 lanes that read one piece of 16
   // rows each meet 64 different banks.
@@ -332,10 +343,9 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
   for (int y = 0; y < kPieces; ++y) k_at[y] = (uint32_t)(n16 * kRow + (((j4 + 4 * y) ^ swz(n16)) * 16));
   const uint32_t v_col = (uint32_t)(4 * j4 * row_bytes + g_bytes + n16 * kVec * E::kBytes);
 
-  constexpr int kQRow = D + 8;  // of the query rows in LDS: 16 lanes in a column of pieces meet all banks
-  __shared__ __attribute__((aligned(16))) uint16_t lds_q[kBlocks > 1 ? kBlocks * kRows * kQRow : 1];
+  constexpr int kQRow = D + 8;
 
-  for (int rb = blockIdx.y; rb * (kRows * kBlocks) < rows; rb += gridDim.y) {
+  for (int rb = by; rb * (kRows * kBlocks) < rows; rb += gy) {
     const int r_first = rb * (kRows * kBlocks), r_last = min(rows, r_first + kRows * kBlocks) - 1;
     const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
     const Steps steps = steps_of<P>(a, p0, p1, unit.first, kv_end);
@@ -369,7 +379,7 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
       for (int i = threadIdx.x; i < kBlocks * kRows * kSegsQ; i += 64 * kWaves) {
         const int r = min(r_first + i / kSegsQ, r_last);
         const QT* from = static_cast<const QT*>(a.q) + ((sp.first + r / a.G) * a.Hq + g * a.G + r % a.G) * D;
-        *reinterpret_cast<u32x4*>(lds_q + i / kSegsQ * kQRow + i % kSegsQ * 8) =
+        *reinterpret_cast<u32x4*>(lds.q + i / kSegsQ * kQRow + i % kSegsQ * 8) =
             *reinterpret_cast<const u32x4*>(from + i % kSegsQ * 8);
       }
       __syncthreads();
@@ -378,7 +388,7 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
       if constexpr (kBlocks == 1)
         return qb[i];
       else
-        return *reinterpret_cast<const bf16x8*>(lds_q + (kRows * k + n16) * kQRow + q_piece(i));
+        return *reinterpret_cast<const bf16x8*>(lds.q + (kRows * k + n16) * kQRow + q_piece(i));
     };
 
     f32x4 o[kBlocks][kVec];
@@ -718,8 +728,8 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
 #pragma unroll
       for (int v = 0; v < 4; ++v)
 #pragma unroll
-        for (int x = 0; x < kVec; ++x) joined.o[wave][n16][kVec * (4 * j4 + v) + x] = o[k][x][v];
-      if (lane < kRows) joined.ml[wave][lane] = make_float2(ref[k], l[k]);
+        for (int x = 0; x < kVec; ++x) lds.mine_o(wave)[n16 * (D + 4) + kVec * (4 * j4 + v) + x] = o[k][x][v];
+      if (lane < kRows) lds.ml(wave)[lane] = make_float2(ref[k], l[k]);
       __syncthreads();
       // 16 threads per row, D / 16 elements each
       const int row = threadIdx.x >> 4, col = (threadIdx.x & 15) * kVec;
@@ -727,17 +737,17 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
       if (row < kRows && rr <= r_last) {
         float M = kNone, L = 0.f, f[kWaves], acc[kVec];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, joined.ml[w][row].x);
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, lds.ml(w)[row].x);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          f[w] = __builtin_amdgcn_exp2f(joined.ml[w][row].x - M);
-          L += f[w] * joined.ml[w][row].y;
+          f[w] = __builtin_amdgcn_exp2f(lds.ml(w)[row].x - M);
+          L += f[w] * lds.ml(w)[row].y;
         }
 #pragma unroll
         for (int x = 0; x < kVec; ++x) {
           acc[x] = 0.f;
 #pragma unroll
-          for (int w = 0; w < kWaves; ++w) acc[x] += f[w] * joined.o[w][row][col + x];
+          for (int w = 0; w < kWaves; ++w) acc[x] += f[w] * lds.o(w)[row * (D + 4) + col + x];
         }
         const int64_t at = (sp.first + rr / a.G) * a.Hq + g * a.G + rr % a.G;
         if (P == kShared || n_parts > 1 || (P == kOwn && unit.first > 0)) {
@@ -760,9 +770,16 @@ __global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(Page
         }
       }
     }
-    if (rb + (int)gridDim.y < (rows + kRows * kBlocks - 1) / (kRows * kBlocks))
+    if (rb + (int)gy < (rows + kRows * kBlocks - 1) / (kRows * kBlocks))
       __syncthreads();  // read, before the next block's K rows come
   }
+}
+
+template <int D, int T, bool kSmall, int kWaves, int P>
+__global__ __launch_bounds__(64 * kWaves, 8 / kWaves) void page_rows_kernel(PageAttnArgs a) {
+  using Lds = RowsLds<D, T, kWaves, 1>;
+  __shared__ __attribute__((aligned(16))) char lds[Lds::kBytes];
+  rows_part<D, T, kSmall, kWaves, P, 1>(a, blockIdx.x, blockIdx.y, gridDim.y, Lds{lds, nullptr});
 }
 
 // The numerators exp2(c1 s - m) of 32 keys in 16 / E + 2 steps, which are issued between
@@ -807,20 +824,19 @@ __device__ __forceinline__ void rounded_step(f32x16& s, float c1, float m, float
 // products to the exponentials), pages found by the lanes for the 64 groups of 8 stages at
 // once (for a stage: 258 us where this took 243), masks and their conditions in the stages
 // that need some only (243 -> 235), and conversions beside the first run of products.
+// k0 .. v1: kKeys * D numbers in LDS each.
 template <int D, int T, int P>
-__global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
+__device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, uint16_t* k0, uint16_t* k1, uint16_t* v0,
+                                          uint16_t* v1) {
   using namespace tile;
   using St = Stage<D>;
   constexpr int kKeys = tile::kTile;
   constexpr bool kE4 = T == CKV_DTYPE_E4M3;
-  __shared__ __attribute__((aligned(16))) uint16_t k0[kKeys * D], k1[kKeys * D];
-  __shared__ __attribute__((aligned(16))) uint16_t v0[kKeys * D], v1[kKeys * D];
-
   // Blocks of rows that read the same keys (of one head and split: a stream) share an
   // XCD's L2: eight streams at a time, one per XCD.  Of the streams left over, 1, 2 or 4
   // have 8, 4 or 2 XCDs each, their blocks in turn; 3, 5, 6 or 7 are cut into eight runs of
   // blocks.  The last rows see the most keys: first.
-  const uint32_t streams = a.Hkv * a.n_splits, xcd = blockIdx.x & 7, idx = blockIdx.x >> 3;
+  const uint32_t streams = a.Hkv * a.n_splits, xcd = bx & 7, idx = bx >> 3;
   const uint32_t whole = streams / 8 * a.n_blocks, rest = streams % 8;
   uint32_t stream, blk;
   if (idx < whole) {
@@ -1261,6 +1277,60 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
   }
 }
 
+template <int D, int T, int P>
+__global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
+  __shared__ __attribute__((aligned(16))) uint16_t k0[tile::kTile * D], k1[tile::kTile * D];
+  __shared__ __attribute__((aligned(16))) uint16_t v0[tile::kTile * D], v1[tile::kTile * D];
+  tile_part<D, T, P>(a, blockIdx.x, k0, k1, v0, v1);
+}
+
+// The shared keys and the sequences' own in one launch, the shared ones first: the own keys, few
+// and read by workgroups of a few steps each, then fill what the others leave idle.
+// kBlocks: of rows_part for the shared keys; 0: tile_part, in whose memory the own ones' waves
+// have a buffer each.
+struct TileRowsLds {
+  char* mine;  // this wave's
+  uint16_t *k0, *k1, *v0, *v1;
+  float2* sums;
+  uint16_t* q;
+  __device__ __forceinline__ char* mine_k(int) const { return mine; }
+  __device__ __forceinline__ float* mine_o(int) const { return reinterpret_cast<float*>(mine); }
+  __device__ __forceinline__ float* o(int w) const {  // (w: a constant)
+    return reinterpret_cast<float*>(w == 0 ? k0 : w == 1 ? k1 : w == 2 ? v0 : v1);
+  }
+  __device__ __forceinline__ float2* ml(int w) const { return sums + w * kRows; }
+};
+template <int D, int T, bool kSmall, int kBlocks>
+__global__ __launch_bounds__(256, 2) void page_parts_kernel(PageAttnArgs shared, PageAttnArgs own, uint32_t shared_x,
+                                                            uint32_t shared_y, uint32_t own_x, uint32_t own_y) {
+  // (x is a multiple of 8: the XCDs stay in turn)
+  const bool is_shared = blockIdx.x < shared_x * shared_y;
+  const uint32_t i = is_shared ? blockIdx.x : blockIdx.x - shared_x * shared_y;
+  if constexpr (kBlocks == 0) {
+    static_assert(kTile * D * Elem<T>::kBytes <= tile::kTile * D * 2 && kRows * (D + 4) * 4 <= tile::kTile * D * 2);
+    __shared__ __attribute__((aligned(16))) uint16_t k0[tile::kTile * D], k1[tile::kTile * D];
+    __shared__ __attribute__((aligned(16))) uint16_t v0[tile::kTile * D], v1[tile::kTile * D];
+    __shared__ float2 sums[4 * kRows];
+    if (is_shared)
+      tile_part<D, T, kShared>(shared, i, k0, k1, v0, v1);
+    else {
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      uint16_t* const mine = wave == 0 ? k0 : wave == 1 ? k1 : wave == 2 ? v0 : v1;
+      rows_part<D, T, kSmall, 4, kOwn, 1>(own, i % own_x, i / own_x, own_y,
+                                          TileRowsLds{reinterpret_cast<char*>(mine), k0, k1, v0, v1, sums, nullptr});
+    }
+  } else {
+    using Lds = RowsLds<D, T, 4, kBlocks>;
+    using OwnLds = RowsLds<D, T, 4, 1>;
+    __shared__ __attribute__((aligned(16))) char lds[Lds::kBytes];
+    __shared__ __attribute__((aligned(16))) uint16_t q[Lds::kQ / 2 + 8];
+    if (is_shared)
+      rows_part<D, T, kSmall, 4, kShared, kBlocks>(shared, i % shared_x, i / shared_x, shared_y, Lds{lds, q});
+    else
+      rows_part<D, T, kSmall, 4, kOwn, 1>(own, i % own_x, i / own_x, own_y, OwnLds{lds, nullptr});
+  }
+}
+
 // Joins the splits of a row: kGroups groups of D / 4 threads take them in turn, 4 elements
 // a thread, and meet in LDS, all in a fixed order.  One group (and several rows per
 // workgroup) up to kJoinBatch splits, whose loads are all in flight together; else the
@@ -1354,8 +1424,11 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
     *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(y);
 }
 
+constexpr int kFewRows = 32;  // rows of a sequence that page_rows_kernel takes (top of the file)
+// Workgroups that read shared keys for 17 to 48 rows: as many as run at once, since a split's
+// outputs are written and read again (eight groups of eight in 8 bits: 77 us, with 1,024 82).
+constexpr int64_t kSharedBlocks = 512;
 // Bytes of shared pages read again and again that are worth the parts' launch and join.
-constexpr int64_t kMidBlocks = 512;
 constexpr int64_t kWorthParts = int64_t(24) << 20;
 
 struct PageAttnPlan {
@@ -1378,16 +1451,15 @@ int64_t longest(const ckv_page_pool* pool, const ckv_page_batch* b) {
 }
 
 // The launch for n_units units of up to `most` of the n_tokens tokens, which see up to `len`
-// keys; tile_blocks: about how many blocks of 128 rows they are.
+// keys; tile_blocks: about how many blocks of 128 rows they are; few_rows: rows of a unit up to which
+// page_rows_kernel's steps are taken.
 PageAttnPlan plan_units(const ckv_page_pool* pool, int Hq, int n_units, int64_t n_tokens, int64_t most, int64_t len,
-                        int64_t tile_blocks, int window, int sinks, bool many_blocks) {
+                        int64_t tile_blocks, int window, int sinks, int few_rows, bool shared) {
   PageAttnPlan p{};
   const int G = Hq / pool->n_kv_heads;
   // (both sides: top of the file; one kernel for the call, by its longest sequence)
-  p.per_block = 1;
-  if (many_blocks && pool->dtype != CKV_DTYPE_F32 && most * G > kRows && most * G <= 4 * kRows)
-    p.per_block = (int)ceil_div(most * G, kRows);
-  p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > 32 && p.per_block == 1;
+  p.wide = pool->dtype != CKV_DTYPE_F32 && most * G > few_rows;
+  p.per_block = !shared || p.wide || pool->dtype == CKV_DTYPE_F32 ? 1 : (int)std::max<int64_t>(2, ceil_div(most * G, kRows));
   if (p.wide) {
     p.blocks = n_tokens * G / tile::kBlockRows + n_units;
     if (window > 0) len = std::min<int64_t>(len, (int64_t)window + ceil_div(tile::kBlockRows, G) + sinks + 16);
@@ -1422,7 +1494,7 @@ PageAttnPlan plan_units(const ckv_page_pool* pool, int Hq, int n_units, int64_t 
     // Splits of 16 steps or more (a sequence of 1,026 steps: 14.0 us; of 12: 15.8, of 24: 14.5),
     // up to 4,096 workgroups, so that sequences of unequal lengths spread over the chip (64
     // of 1,024 to 16,384 tokens: 165 us; up to 2,048: 183, up to 8,192: 170).
-    p.n_splits = (int)std::max<int64_t>(1, std::min((p.per_block > 1 ? kMidBlocks : 4096) / std::max<int64_t>(wgs, 1), steps / 16));
+    p.n_splits = (int)std::max<int64_t>(1, std::min((shared ? kSharedBlocks : 4096) / std::max<int64_t>(wgs, 1), steps / 16));
     p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
   }
   if (n_tokens * Hq >= kMaxGrid) p.n_splits = 1;  // (the join has a workgroup per row)
@@ -1433,7 +1505,7 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
   // (sequences' last blocks are taken as full: many short ones are more workgroups than this)
   const int64_t blocks = b->n_tokens * (Hq / pool->n_kv_heads) / tile::kBlockRows + 1;
   PageAttnPlan p = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most_tokens(b->max_tokens, b->n_tokens, b->n_seqs),
-                              longest(pool, b), blocks, window, sinks, false);
+                              longest(pool, b), blocks, window, sinks, kFewRows, false);
   const size_t rows = (size_t)b->n_tokens * Hq;
   if (p.n_splits > 1) {
     p.off_ml = align_up((size_t)p.n_splits * rows * pool->head_dim * sizeof(float), 256);
@@ -1467,11 +1539,13 @@ SharedPlan make_shared_plan(const ckv_page_pool* pool, const ckv_page_batch* b, 
   const auto blocks = [&](int units, int64_t most_of) {
     return std::min(b->n_tokens * G / tile::kBlockRows + units, units * ceil_div(most_of * G, tile::kBlockRows));
   };
-  const int64_t most_group = most_tokens(g->max_tokens, b->n_tokens, g->n_groups);
-  p.shared = plan_units(pool, Hq, g->n_groups, b->n_tokens, most_group, shared_len, blocks(g->n_groups, most_group), 0, 0, true);
   // (own keys: what the longest sequence has behind the longest prefix, a page at least)
   const int64_t own_len = std::max<int64_t>(len - shared_len, pool->page_size);
-  p.own = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most, own_len, blocks(b->n_seqs, most), 0, 0, false);
+  p.own = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most, own_len, blocks(b->n_seqs, most), 0, 0, kFewRows, false);
+  const int64_t most_group = most_tokens(g->max_tokens, b->n_tokens, g->n_groups);
+  const int few_rows = p.own.wide ? 0 : pool->dtype == CKV_DTYPE_BF16 && pool->head_dim == 128 ? 32 : 48;
+  p.shared = plan_units(pool, Hq, g->n_groups, b->n_tokens, most_group, shared_len, blocks(g->n_groups, most_group), 0, 0,
+                        few_rows, true);
   const size_t rows = (size_t)b->n_tokens * Hq, places = (size_t)p.shared.n_splits + p.own.n_splits;
   p.off_ml = align_up(places * rows * pool->head_dim * sizeof(float), 256);
   p.off_shared = align_up(p.off_ml + places * rows * sizeof(float2), 256);
@@ -1494,34 +1568,54 @@ ckv_status check_attn(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq
   return CKV_OK;
 }
 
+// Workgroups of a plan's launch: x by y, x a multiple of 8.
+struct Grid {
+  int64_t x, y;
+};
+ckv_status grid_of(PageAttnArgs& a, const PageAttnPlan& p, int units, Grid& g) {
+  if (p.wide) {
+    const int64_t streams = (int64_t)a.Hkv * a.n_splits;
+    const int64_t rest = streams % 8;
+    g = Grid{8 * (streams / 8 * p.blocks + ceil_div(rest * p.blocks, 8)), 1};
+    a.n_blocks = (uint32_t)p.blocks;
+  } else {
+    g = Grid{(int64_t)align_up((size_t)units * a.n_splits, 8) * a.Hkv, p.row_blocks};
+  }
+  if (g.x >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
+  return CKV_OK;
+}
+
 template <int D, int T, int P>
 ckv_status launch_units(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) {
-  const int units = P == kShared ? a.n_groups : a.s.n_seqs;
+  Grid g;
+  if (ckv_status s = grid_of(a, p, P == kShared ? a.n_groups : a.s.n_seqs, g); s != CKV_OK) return s;
   if (p.wide) {
-    if constexpr (T != CKV_DTYPE_F32) {
-      const int64_t streams = (int64_t)a.Hkv * a.n_splits;
-      const int64_t rest = streams % 8;
-      const int64_t grid = 8 * (streams / 8 * p.blocks + ceil_div(rest * p.blocks, 8));
-      if (grid >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
-      a.n_blocks = (uint32_t)p.blocks;
-      hipLaunchKernelGGL((page_tile_kernel<D, T, P>), dim3((unsigned)grid), dim3(256), 0, st, a);
-    }
-  } else {
-    const int64_t wgs = (int64_t)align_up((size_t)units * a.n_splits, 8) * a.Hkv;
-    if (wgs >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
+    if constexpr (T != CKV_DTYPE_F32)
+      hipLaunchKernelGGL((page_tile_kernel<D, T, P>), dim3((unsigned)g.x), dim3(256), 0, st, a);
+  } else if constexpr (P == kWhole) {
     // A launch of at most a workgroup per CU has 8 waves in each, whose fewer steps follow
     // one another (16 sequences of 4 tokens: 13.1 -> 11.7 us, fp32 prompts 8.7 -> 8.0); where
     // there are more, 4 (48 sequences: 80 us, with 8: 94).
-    const bool eight = wgs * p.row_blocks <= 256 && p.per_block == 1;
-    auto kernel = a.c == 8 ? (eight ? page_rows_kernel<D, T, true, 8, P, 1> : page_rows_kernel<D, T, true, 4, P, 1>)
-                           : (eight ? page_rows_kernel<D, T, false, 8, P, 1> : page_rows_kernel<D, T, false, 4, P, 1>);
-    if constexpr (P == kShared && T != CKV_DTYPE_F32) {
-      if (p.per_block == 2) kernel = a.c == 8 ? page_rows_kernel<D, T, true, 4, P, 2> : page_rows_kernel<D, T, false, 4, P, 2>;
-      if (p.per_block == 3) kernel = a.c == 8 ? page_rows_kernel<D, T, true, 4, P, 3> : page_rows_kernel<D, T, false, 4, P, 3>;
-      if (p.per_block == 4) kernel = a.c == 8 ? page_rows_kernel<D, T, true, 4, P, 4> : page_rows_kernel<D, T, false, 4, P, 4>;
-    }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)p.row_blocks), dim3(eight ? 512 : 256), 0, st, a);
+    const bool eight = g.x * g.y <= 256;
+    const auto kernel = a.c == 8 ? (eight ? page_rows_kernel<D, T, true, 8, P> : page_rows_kernel<D, T, true, 4, P>)
+                                 : (eight ? page_rows_kernel<D, T, false, 8, P> : page_rows_kernel<D, T, false, 4, P>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)g.x, (unsigned)g.y), dim3(eight ? 512 : 256), 0, st, a);
   }
+  CKV_HIP(hipGetLastError());
+  return CKV_OK;
+}
+
+// The shared keys and, of few rows each, the sequences' own.
+template <int D, int T, int kBlocks>
+ckv_status launch_parts(PageAttnArgs& shared, PageAttnArgs& own, const SharedPlan& p, hipStream_t st) {
+  Grid x, y;
+  if (ckv_status s = grid_of(shared, p.shared, shared.n_groups, x); s != CKV_OK) return s;
+  if (ckv_status s = grid_of(own, p.own, own.s.n_seqs, y); s != CKV_OK) return s;
+  const int64_t first = x.x * x.y, all = first + y.x * y.y;
+  if (all >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
+  const auto kernel = own.c == 8 ? page_parts_kernel<D, T, true, kBlocks> : page_parts_kernel<D, T, false, kBlocks>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)all), dim3(256), 0, st, shared, own, (uint32_t)x.x, (uint32_t)x.y,
+                     (uint32_t)y.x, (uint32_t)y.y);
   CKV_HIP(hipGetLastError());
   return CKV_OK;
 }
@@ -1557,13 +1651,27 @@ ckv_status launch_shared_attn(PageAttnArgs& a, const SharedPlan& p, char* ws, hi
   a.n_parts = shared_parts;
   a.n_splits = p.shared.n_splits;
   a.slice = p.shared.slice;
-  if (ckv_status s = launch_units<D, T, kShared>(a, p.shared, st); s != CKV_OK) return s;
-  a.o_part = o_part + (size_t)p.shared.n_splits * rows * D;
-  a.ml_part = ml_part + (size_t)p.shared.n_splits * rows;
-  a.n_parts = reinterpret_cast<int32_t*>(ws + p.off_own);
-  a.n_splits = p.own.n_splits;
-  a.slice = p.own.slice;
-  if (ckv_status s = launch_units<D, T, kOwn>(a, p.own, st); s != CKV_OK) return s;
+  PageAttnArgs own = a;
+  own.o_part = o_part + (size_t)p.shared.n_splits * rows * D;
+  own.ml_part = ml_part + (size_t)p.shared.n_splits * rows;
+  own.n_parts = reinterpret_cast<int32_t*>(ws + p.off_own);
+  own.n_splits = p.own.n_splits;
+  own.slice = p.own.slice;
+  ckv_status s = CKV_OK;
+  if constexpr (T == CKV_DTYPE_F32) {
+    s = launch_parts<D, T, 1>(a, own, p, st);
+  } else if (p.own.wide) {
+    s = launch_units<D, T, kShared>(a, p.shared, st);
+    if (s == CKV_OK) s = launch_units<D, T, kOwn>(own, p.own, st);
+  } else if (p.shared.wide) {
+    s = launch_parts<D, T, 0>(a, own, p, st);
+  } else if (p.shared.per_block == 2) {
+    s = launch_parts<D, T, 2>(a, own, p, st);
+  } else if constexpr (T == CKV_DTYPE_E4M3 || D == 64) {
+    s = launch_parts<D, T, 3>(a, own, p, st);
+  }
+  if (s != CKV_OK) return s;
+  a.n_parts = own.n_parts;
   a.o_part = o_part;
   a.ml_part = ml_part;
   a.shared_parts = shared_parts;
