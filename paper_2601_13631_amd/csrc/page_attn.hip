@@ -1341,10 +1341,13 @@ template <int D, class QT, int kGroups, bool kParts>
 __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
   constexpr int kCols = D / 4, kRowsPer = 256 / kCols / kGroups;
   const int64_t n_rows = a.s.n_tokens * a.Hq;
-  const int64_t row = (int64_t)blockIdx.x * kRowsPer + threadIdx.x / (kCols * kGroups);
+  int64_t row = (int64_t)blockIdx.x * kRowsPer + threadIdx.x / (kCols * kGroups);
+  // A workgroup that has one row leaves as a whole; of several rows, joined in groups, all stay.
+  constexpr bool kStay = kGroups > 1 && kRowsPer > 1;
+  bool mine = row < n_rows;
+  if (!kStay && !mine) return;
+  if (kStay) row = min(row, n_rows - 1);
   const int tok = (int)row / a.Hq;  // (at most 2^26 rows)
-  // (with several groups, a workgroup has one row: it leaves as a whole)
-  if (row >= n_rows) return;
   const int col = threadIdx.x % kCols * 4, grp = threadIdx.x / kCols % kGroups;
   float2 ml[kJoinBatch];
   f32x4 x[kJoinBatch];
@@ -1365,7 +1368,8 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
     own_from = a.shared_splits;
     n_parts = own_from + min(own & (kAfterShared - 1), a.n_splits - own_from);
     n_shared = own & kAfterShared ? min(shared, own_from) : 0;
-    if (tok < first_tok || tok >= end_tok || (!(own & kAfterShared) && n_parts - own_from <= 1)) return;
+    if (tok < first_tok || tok >= end_tok || (!(own & kAfterShared) && n_parts - own_from <= 1)) mine = false;
+    if (!kStay && !mine) return;
   } else {
     n_parts = min(a.n_parts[tok], a.n_splits);
     if (tok < first_tok || tok >= end_tok || n_parts <= 1) return;  // of no sequence, or written already
@@ -1396,21 +1400,22 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
     }
   }
   if constexpr (kGroups > 1) {
-    __shared__ f32x4 part[kGroups][kCols];
-    __shared__ float2 part_ml[kGroups];
-    part[grp][threadIdx.x % kCols] = acc;
-    if (col == 0) part_ml[grp] = make_float2(M, L);
+    __shared__ f32x4 part[kRowsPer][kGroups][kCols];
+    __shared__ float2 part_ml[kRowsPer][kGroups];
+    const int at = threadIdx.x / (kCols * kGroups), c = threadIdx.x % kCols;
+    part[at][grp][c] = acc;
+    if (col == 0) part_ml[at][grp] = make_float2(M, L);
     __syncthreads();
-    if (grp > 0) return;
+    if (grp > 0 || (kRowsPer > 1 && !mine)) return;
 #pragma unroll
-    for (int k = 1; k < kGroups; ++k) M = fmaxf(M, part_ml[k].x);
+    for (int k = 1; k < kGroups; ++k) M = fmaxf(M, part_ml[at][k].x);
     L = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {
-      const float w = __builtin_amdgcn_exp2f(part_ml[k].x - M);
-      L += part_ml[k].y * w;
-      acc += part[k][threadIdx.x] * w;
+      const float w = __builtin_amdgcn_exp2f(part_ml[at][k].x - M);
+      L += part_ml[at][k].y * w;
+      acc += part[at][k][c] * w;
     }
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -1626,10 +1631,17 @@ ckv_status launch_join(const PageAttnArgs& a, hipStream_t st) {
   using QT = typename Elem<T>::Q;
   constexpr int kUnits = 256 / (D / 4);
   const int64_t rows = a.s.n_tokens * a.Hq;
-  if (a.n_splits <= kJoinBatch)
-    hipLaunchKernelGGL((page_combine_kernel<D, QT, 1, kParts>), dim3((unsigned)ceil_div(rows, kUnits)), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((page_combine_kernel<D, QT, kUnits, kParts>), dim3((unsigned)rows), dim3(256), 0, st, a);
+  // Groups that take kJoinBatch places each at once, no more than there are places for: loads past
+  // the last place are made all the same (2,560 rows of 9 places: 10 us with 8 groups, JOIN with 2).
+  int groups = 1;
+  while (groups < kUnits && groups * kJoinBatch < a.n_splits) groups *= kParts ? 2 : kUnits;
+  auto kernel = groups == 1 ? page_combine_kernel<D, QT, 1, kParts> : page_combine_kernel<D, QT, kUnits, kParts>;
+  if constexpr (kParts) {
+    if (groups == 2) kernel = page_combine_kernel<D, QT, 2, true>;
+    if (groups == 4) kernel = page_combine_kernel<D, QT, 4, true>;
+    if (groups == 8) kernel = page_combine_kernel<D, QT, 8, true>;
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(rows * groups, kUnits)), dim3(256), 0, st, a);
   CKV_HIP(hipGetLastError());
   return CKV_OK;
 }

@@ -22,36 +22,13 @@ ckv_status check_groups(const ckv_page_groups* g, const ckv_page_batch* b, bool 
 
 namespace {
 
-// ---- block-wide reductions ----------------------------------------------------------
+// ---- block-wide sums ------------------------------------------------------------------
 
-template <class T, class F>
-__device__ __forceinline__ T wave_all(T x, F&& f) {
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) x = f(x, __shfl_xor(x, i));
-  return x;
-}
-// Every thread of the workgroup gets f over all of them.
-template <int kThreads, class T, class F>
-__device__ __forceinline__ T block_all(T x, F&& f) {
-  __shared__ T part[kThreads / 64];
-  x = wave_all(x, f);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = part[0];
-#pragma unroll
-  for (int i = 1; i < kThreads / 64; ++i) x = f(x, part[i]);
-  __syncthreads();
-  return x;
-}
-template <int kThreads, class T>
-__device__ __forceinline__ T block_total(T x) {
-  return block_all<kThreads>(x, [](T a, T b) { return a + b; });
-}
 // Inclusive sums over a wave's lanes, by moves between lanes (a row of 16, then the last lane
 // of each row to the next rows).
 template <int CTRL, int ROWS>
-__device__ __forceinline__ int moved(int x) {
-  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+__device__ __forceinline__ int moved(int x, int none = 0) {
+  return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xF, false);
 }
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int64_t moved(int64_t x) {
@@ -67,25 +44,48 @@ __device__ __forceinline__ T wave_upto(T x) {
   x += moved<0x143, 0xC>(x);  // lane 31 to rows 2 and 3
   return x;
 }
-// The sums of x and y over the threads before this one; `tx` and `ty` get those of all.
-template <int kThreads, class T>
-__device__ __forceinline__ void block_before(T& x, T& y, T& tx, T& ty) {
+// The least of a wave's lanes, for all of them.
+__device__ __forceinline__ int wave_least(int x) {
+  x = min(x, moved<kDppRowShr1, 0xF>(x, INT32_MAX));
+  x = min(x, moved<kDppRowShr2, 0xF>(x, INT32_MAX));
+  x = min(x, moved<kDppRowShr4, 0xF>(x, INT32_MAX));
+  x = min(x, moved<kDppRowShr8, 0xF>(x, INT32_MAX));
+  x = min(x, moved<0x142, 0xA>(x, INT32_MAX));
+  x = min(x, moved<0x143, 0xC>(x, INT32_MAX));
+  return __builtin_amdgcn_readlane(x, 63);
+}
+// The sum of x over all threads, for all of them.
+template <int kThreads>
+__device__ __forceinline__ int block_total(int x) {
+  __shared__ int part[kThreads / 64];
+  x = wave_upto(x);
+  if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = x;
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  x = wave_upto(lane < kThreads / 64 ? part[lane] : 0);
+  __syncthreads();
+  return __builtin_amdgcn_readlane(x, 63);
+}
+// Each x becomes its sum over the threads before this one; `total` gets those of all.
+template <int kThreads, int N, class T>
+__device__ __forceinline__ void block_before(T (&x)[N], T (&total)[N]) {
   constexpr int kWaves = kThreads / 64;
   static_assert(kWaves <= 64);
-  __shared__ T part[2][kWaves];
+  __shared__ T part[N][kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const T ux = wave_upto(x), uy = wave_upto(y);
-  if (lane == 63) {
-    part[0][wave] = ux;
-    part[1][wave] = uy;
+  T upto[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    upto[i] = wave_upto(x[i]);
+    if (lane == 63) part[i][wave] = upto[i];
   }
   __syncthreads();
-  const T px = lane < kWaves ? part[0][lane] : T(0), py = lane < kWaves ? part[1][lane] : T(0);
-  const T wx = wave_upto(px), wy = wave_upto(py);
-  tx = __shfl(wx, kWaves - 1);
-  ty = __shfl(wy, kWaves - 1);
-  x = __shfl(wx - px, wave) + ux - x;
-  y = __shfl(wy - py, wave) + uy - y;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const T p = lane < kWaves ? part[i][lane] : T(0), w = wave_upto(p);
+    total[i] = __shfl(w, kWaves - 1);
+    x[i] = __shfl(w - p, wave) + upto[i] - x[i];
+  }
   __syncthreads();
 }
 
@@ -102,7 +102,7 @@ struct ShareArgs {
 // against the first sequence with tokens.  One more for the sequences of no group.
 // The loads of a wave's rounds are its time, so four sequences go together: 48 sequences of 970
 // pages 11.4 us one at a time, KSHARE so.
-constexpr int kShareThreads = 1024, kShareBatch = 8, kShareSeqs = 4;
+constexpr int kShareThreads = 1024, kShareBatch = 16, kShareSeqs = 4;
 __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
   const auto begin_of = [&](int g) { return min(max(a.grp_off[g], 0), a.s.n_seqs); };
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -114,7 +114,8 @@ __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
     return;
   }
   const int f = begin_of(g), l = begin_of(g + 1);
-  __shared__ int common;
+  constexpr int kWavesOf = kShareThreads / 64;
+  __shared__ int common, part[2][kWavesOf];
   int leader = INT32_MAX, least = INT32_MAX;
   for (int b = f + tid; b < l; b += kShareThreads) {
     const SeqSpan sp = seq_span(a.s, b);
@@ -122,15 +123,20 @@ __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
     leader = min(leader, b);
     least = min(least, sp.len - sp.count + 1);
   }
-  const auto lower = [](int x, int y) { return min(x, y); };
-  leader = block_all<kShareThreads>(leader, lower);
-  least = block_all<kShareThreads>(least, lower);
+  leader = wave_least(leader);
+  least = wave_least(least);
+  if (lane == 0) {
+    part[0][wave] = leader;
+    part[1][wave] = least;
+  }
+  __syncthreads();
+  leader = wave_least(lane < kWavesOf ? part[0][lane] : INT32_MAX);
+  least = wave_least(lane < kWavesOf ? part[1][lane] : INT32_MAX);
   const int seen = leader == INT32_MAX ? 0 : (int)min((int64_t)max(least, 0), (int64_t)a.s.max_pages * a.c);
   const int slots = (seen + a.c - 1) / a.c;
   if (tid == 0) common = slots;
   __syncthreads();
   const int32_t* const first = a.s.table + (int64_t)leader * a.s.table_stride;
-  constexpr int kWavesOf = kShareThreads / 64;
   for (int b0 = f + wave; b0 < l && slots > 0; b0 += kWavesOf * kShareSeqs) {
     // (a sequence that is not there or has no tokens: the first one again)
     const int32_t* mine[kShareSeqs];
@@ -158,7 +164,7 @@ __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
         for (int i = 0; i < kShareSeqs; ++i)
           if (x[k] != y[i][k]) differ = min(s0 + 64 * k + lane, slots - 1);
       if (!__any(differ != INT32_MAX)) continue;
-      differ = wave_all(differ, lower);
+      differ = wave_least(differ);
       if (lane == 0) atomicMin(&common, differ);
       break;
     }
@@ -271,20 +277,20 @@ __global__ __launch_bounds__(kThreads) void fork_copy_kernel(ForkArgs a) {
 __global__ __launch_bounds__(kThreads) void fork_count_kernel(ForkArgs a) {
   const Tables& t = a.t;
   const int b = blockIdx.x / a.table_pieces, piece = blockIdx.x % a.table_pieces;
-  const int held = t.pages(t.length(t.lens[b]));
-  if (piece * kPiece >= held) return;
-  int children = 0;
-  for (int i = threadIdx.x; i < t.n_out; i += kThreads) children += a.parents[i] == b;
-  const int by = block_total<kThreads>(children) - 1;
-  if (by == 0) return;
   const int32_t* const from = t.table + (int64_t)b * t.table_stride;
+  const int len = t.lens[b];
+  int e[kPiece / kThreads];  // (all loads together, past the held ones too)
 #pragma unroll
-  for (int k = 0; k < kPiece / kThreads; ++k) {
-    const int at = piece * kPiece + k * kThreads + (int)threadIdx.x;
-    if (at >= held) break;
-    const int e = from[at];
-    if (t.names_page(e)) atomicAdd(&t.refs_out[e], by);
-  }
+  for (int k = 0; k < kPiece / kThreads; ++k)
+    e[k] = from[min(piece * kPiece + k * kThreads + (int)threadIdx.x, t.max_pages - 1)];
+  int children = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < t.n_out; i += kThreads) children += a.parents[i] == b;
+  const int held = t.pages(t.length(len)), by = block_total<kThreads>(children) - 1;
+  if (by == 0) return;
+#pragma unroll
+  for (int k = 0; k < kPiece / kThreads; ++k)
+    if (piece * kPiece + k * kThreads + (int)threadIdx.x < held && t.names_page(e[k])) atomicAdd(&t.refs_out[e[k]], by);
 }
 
 // ---- extend -------------------------------------------------------------------------------
@@ -364,9 +370,9 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
     const int64_t p0 = (int64_t)blockIdx.x * kPlanPages + threadIdx.x * kPlanPer;
     int32_t refs[kPlanPer];
     load_refs(t, p0, refs);
-    int below = free_below<kCounted>(a, blockIdx.x), rank = free_of(refs), all_below, all;
-    block_before<kPlanThreads>(below, rank, all_below, all);
-    rank += all_below;
+    int sums[2] = {free_below<kCounted>(a, blockIdx.x), free_of(refs)}, all[2];
+    block_before<kPlanThreads>(sums, all);
+    int rank = all[0] + sums[1];
 #pragma unroll
     for (int i = 0; i < kPlanPer; ++i) {
       if (p0 + i >= t.n_pages) break;
@@ -401,38 +407,33 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
         need = t.pages((int)upto) - held + (tail >= 0);
       }
     }
-    if (b0 == 0) {
-      int64_t mine = n_free, none = 0, zero;
-      block_before<kPlanThreads>(mine, none, n_free, zero);
-    }
-    int64_t before = need, row = add, total_need, total_add;
-    block_before<kPlanThreads>(before, row, total_need, total_add);
-    if (needed + total_need > n_free || asked + total_add > a.o.n_tokens) {  // some are refused
-      if ((need > 0 && needed + before + need > n_free) || (add > 0 && asked + row + add > a.o.n_tokens)) {
+    int64_t x[3] = {need, add, b0 == 0 ? n_free : 0}, total[3];
+    block_before<kPlanThreads>(x, total);
+    if (b0 == 0) n_free = total[2];
+    const int64_t need_before = needed, add_before = asked;
+    needed += total[0];
+    asked += total[1];
+    if (needed > n_free || asked > a.o.n_tokens) {  // some are refused
+      if ((need > 0 && need_before + x[0] + need > n_free) || (add > 0 && add_before + x[1] + add > a.o.n_tokens)) {
         no = true;
         need = add = 0;
         tail = -1;
       }
-      needed += total_need;
-      asked += total_add;
-      before = need;
-      row = add;
-      block_before<kPlanThreads>(before, row, total_need, total_add);
-    } else {
-      needed += total_need;
-      asked += total_add;
+      x[0] = need;
+      x[1] = add;
+      block_before<kPlanThreads>(x, total);
     }
     refused += no;
     if (b < t.n_seqs) {
-      a.first[b] = (int32_t)(taken + before);
+      a.first[b] = (int32_t)(taken + x[0]);
       a.old_len[b] = len;
-      a.o.tok_off[b + 1] = (int32_t)(tokens + row + add);
+      a.o.tok_off[b + 1] = (int32_t)(tokens + x[1] + add);
       a.o.copy_src[b] = tail;
     }
-    taken += total_need;
-    tokens += total_add;
+    taken += total[0];
+    tokens += total[1];
   }
-  if (t.n_seqs == 0) n_free = block_total<kPlanThreads>(n_free);
+  if (t.n_seqs == 0) n_free = block_total<kPlanThreads>((int)n_free);
   refused = block_total<kPlanThreads>(refused);
   if (threadIdx.x == 0) {
     a.o.counts[0] = (int32_t)tokens;
