@@ -1434,7 +1434,7 @@ constexpr int kFewRows = 32;  // rows of a sequence that page_rows_kernel takes 
 // outputs are written and read again (eight groups of eight in 8 bits: 77 us, with 1,024 82).
 constexpr int64_t kSharedBlocks = 512;
 // Bytes of shared pages read again and again that are worth the parts' launch and join.
-constexpr int64_t kWorthParts = int64_t(24) << 20;
+constexpr int64_t kWorthParts = int64_t(40) << 20;
 
 struct PageAttnPlan {
   bool wide;       // page_tile_kernel
@@ -1459,7 +1459,7 @@ int64_t longest(const ckv_page_pool* pool, const ckv_page_batch* b) {
 // keys; tile_blocks: about how many blocks of 128 rows they are; few_rows: rows of a unit up to which
 // page_rows_kernel's steps are taken.
 PageAttnPlan plan_units(const ckv_page_pool* pool, int Hq, int n_units, int64_t n_tokens, int64_t most, int64_t len,
-                        int64_t tile_blocks, int window, int sinks, int few_rows, bool shared) {
+                        int64_t tile_blocks, int window, int sinks, int few_rows, bool shared, int64_t split_steps = 16) {
   PageAttnPlan p{};
   const int G = Hq / pool->n_kv_heads;
   // (both sides: top of the file; one kernel for the call, by its longest sequence)
@@ -1499,18 +1499,20 @@ PageAttnPlan plan_units(const ckv_page_pool* pool, int Hq, int n_units, int64_t 
     // Splits of 16 steps or more (a sequence of 1,026 steps: 14.0 us; of 12: 15.8, of 24: 14.5),
     // up to 4,096 workgroups, so that sequences of unequal lengths spread over the chip (64
     // of 1,024 to 16,384 tokens: 165 us; up to 2,048: 183, up to 8,192: 170).
-    p.n_splits = (int)std::max<int64_t>(1, std::min((shared ? kSharedBlocks : 4096) / std::max<int64_t>(wgs, 1), steps / 16));
+    p.n_splits = (int)std::max<int64_t>(1, std::min((shared ? kSharedBlocks : 4096) / std::max<int64_t>(wgs, 1), steps / split_steps));
     p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
   }
   if (n_tokens * Hq >= kMaxGrid) p.n_splits = 1;  // (the join has a workgroup per row)
   return p;
 }
 
-PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq, int window, int sinks) {
+PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int Hq, int window, int sinks,
+                       int64_t split_steps = 16) {
   // (sequences' last blocks are taken as full: many short ones are more workgroups than this)
   const int64_t blocks = b->n_tokens * (Hq / pool->n_kv_heads) / tile::kBlockRows + 1;
   PageAttnPlan p = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most_tokens(b->max_tokens, b->n_tokens, b->n_seqs),
-                              longest(pool, b), blocks, window, sinks, kFewRows, false);
+                              longest(pool, b), blocks, window, sinks, kFewRows, false,
+                              split_steps);
   const size_t rows = (size_t)b->n_tokens * Hq;
   if (p.n_splits > 1) {
     p.off_ml = align_up((size_t)p.n_splits * rows * pool->head_dim * sizeof(float), 256);
@@ -1537,7 +1539,18 @@ SharedPlan make_shared_plan(const ckv_page_pool* pool, const ckv_page_batch* b, 
                         page_elem_bytes(pool->dtype);
   p.apart = g->n_groups > 0 && saved >= kWorthParts;
   if (!p.apart) {
-    p.whole = make_plan(pool, b, Hq, 0, 0);
+    // A few short sequences: a step for each of a workgroup's 8 waves where that is a workgroup per CU
+    // at most (15 sequences of 1,100 keys in fp32, splits of 16 steps 14.2 us, of 8 11.3; two of 4,000 in
+    // bf16 11.4 and 10.5); at head_dim 64 in 16 and 8 bits five steps a wave before the join is worth
+    // its launch (four sequences of 1,040 keys: 16 steps 9.9 us, 8 9.2, all of them 8.4; of 1,640 10.1, 10.0
+    // with all).
+    const int64_t steps = ceil_div(len, kTile);
+    int64_t split_steps = 16;
+    if (pool->dtype != CKV_DTYPE_F32 && pool->head_dim == 64 && steps <= 40)
+      split_steps = steps + 1;
+    else if ((int64_t)b->n_seqs * pool->n_kv_heads * ceil_div(most * G, kRows) * ceil_div(steps, 8) <= 256)
+      split_steps = 8;
+    p.whole = make_plan(pool, b, Hq, 0, 0, split_steps);
     p.bytes = p.whole.bytes;
     return p;
   }
