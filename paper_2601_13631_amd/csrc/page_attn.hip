@@ -62,6 +62,7 @@ struct PageAttnArgs {
   const int32_t* grp_off;  // [n_groups + 1]
   const int32_t* shared;   // [n_groups] tokens, [n_groups] leaders, [n_seqs] tokens
   int n_groups;
+  int n_wgs;               // workgroups of few rows for the shared keys of one KV head, about
   const int32_t* shared_parts;  // the join: splits of the shared keys by token
   int shared_splits;            //   and the places that they have
 };
@@ -117,9 +118,24 @@ __device__ __forceinline__ Unit unit_of(const PageAttnArgs& a, int u) {
 // Splits of a unit of so many steps.  A whole sequence without a key has one, which writes its
 // rows' zeros; a part that another one completes has none.
 template <int P>
-__device__ __forceinline__ int parts_of(const PageAttnArgs& a, const Unit& x, int steps) {
+__device__ __forceinline__ int parts_of(const PageAttnArgs& a, const Unit& x, int steps, int slice) {
   const int least = P == kWhole || (P == kOwn && x.first == 0) ? 1 : 0;
-  return min(max((steps + a.slice - 1) / a.slice, least), a.n_splits);
+  return min(max((steps + slice - 1) / slice, least), a.n_splits);
+}
+// Steps of a split of shared keys, so that the groups' splits together are a.n_wgs at most (for
+// one KV head), as many as run at once, however unequal the groups are; a.slice at least.
+__device__ __forceinline__ int shared_slice(const PageAttnArgs& a) {
+  int64_t steps = 0;
+  for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
+    const int g = g0 + (int)(threadIdx.x & 63);
+    int x = g < a.n_groups ? shared_tokens(a, g) / kTile : 0;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) x += __shfl_xor(x, i);
+    steps += x;
+  }
+  const int more = a.n_wgs - a.n_groups;  // splits beside each group's first
+  if (more <= 0) return 1 << 30;
+  return __builtin_amdgcn_readfirstlane((int)max((steps + more - 1) / more, (int64_t)a.slice));
 }
 // What the join reads of a token's sequence: its splits and, of kOwn, whether shared ones go before.
 constexpr int kAfterShared = 1 << 30;
@@ -325,7 +341,7 @@ __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, ui
   const int p_base = unit.p_base;
   // this sequence's own number of splits, by its length
   const int all_steps = steps_of<P>(a, p_base, p_base + sp.count - 1, unit.first, kv_end).n;
-  const int n_parts = parts_of<P>(a, unit, all_steps);
+  const int n_parts = parts_of<P>(a, unit, all_steps, P == kShared ? shared_slice(a) : a.slice);
   if ((P != kWhole || a.n_splits > 1) && split == 0 && g == 0 && by == 0)
     for (int i = threadIdx.x; i < sp.count; i += 64 * kWaves) a.n_parts[sp.first + i] = parts_note<P>(unit, n_parts);
   if (split >= n_parts) return;
@@ -871,7 +887,7 @@ __device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, ui
   const int p_base = unit.p_base;
   const int p0 = p_base + r_first / a.G, p1 = p_base + r_last / a.G;
   const int all_steps = (groups_of<P>(a, p_base, p_base + sp.count - 1, unit.first, kv_end).n + 7) / 8;
-  const int n_parts = parts_of<P>(a, unit, all_steps);
+  const int n_parts = parts_of<P>(a, unit, all_steps, a.slice);
   if ((P != kWhole || a.n_splits > 1) && split == 0 && g == 0)
     for (int i = r_first / a.G + (int)threadIdx.x; i <= r_last / a.G; i += 256)
       a.n_parts[sp.first + i] = parts_note<P>(unit, n_parts);
@@ -1430,9 +1446,11 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
 }
 
 constexpr int kFewRows = 32;  // rows of a sequence that page_rows_kernel takes (top of the file)
-// Workgroups that read shared keys for 17 to 48 rows: as many as run at once, since a split's
-// outputs are written and read again (eight groups of eight in 8 bits: 77 us, with 1,024 82).
-constexpr int64_t kSharedBlocks = 512;
+// Workgroups that read shared keys for 17 to 48 rows: most of the 512 that run at once, which leaves
+// room for the sequences' own keys (eight groups of eight in 8 bits, 8,192 to 16,384 shared tokens: 320
+// of them 68.7 us, 384 63.7, 416 59.3, 448 61.7, 512 68.5; in bf16 28 heads on 4, groups of four: 52.5,
+// 49.4, 49.2, 51.4, 52.9).
+constexpr int64_t kSharedBlocks = 416;
 // Bytes of shared pages read again and again that are worth the parts' launch and join.
 constexpr int64_t kWorthParts = int64_t(40) << 20;
 
@@ -1441,6 +1459,7 @@ struct PageAttnPlan {
   int n_splits, slice;
   int row_blocks;  // page_rows_kernel: grid y, and its kBlocks
   int per_block;
+  int n_wgs;
   int64_t blocks;  // page_tile_kernel: blocks of rows, at most
   size_t off_ml, off_n, bytes;
 };
@@ -1499,8 +1518,12 @@ PageAttnPlan plan_units(const ckv_page_pool* pool, int Hq, int n_units, int64_t 
     // Splits of 16 steps or more (a sequence of 1,026 steps: 14.0 us; of 12: 15.8, of 24: 14.5),
     // up to 4,096 workgroups, so that sequences of unequal lengths spread over the chip (64
     // of 1,024 to 16,384 tokens: 165 us; up to 2,048: 183, up to 8,192: 170).
-    p.n_splits = (int)std::max<int64_t>(1, std::min((shared ? kSharedBlocks : 4096) / std::max<int64_t>(wgs, 1), steps / split_steps));
-    p.slice = (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
+    // Of shared keys a unit has places for twice the mean of kSharedBlocks, and takes as many as the
+    // others leave (shared_slice).
+    const int64_t most_wgs = shared ? kSharedBlocks * (n_units > 1 ? 2 : 1) : 4096;
+    p.n_splits = (int)std::max<int64_t>(1, std::min(most_wgs / std::max<int64_t>(wgs, 1), steps / split_steps));
+    p.slice = shared ? 16 : (int)std::max<int64_t>(1, ceil_div(steps, p.n_splits));
+    p.n_wgs = (int)(kSharedBlocks / std::max<int64_t>(1, (int64_t)pool->n_kv_heads * p.row_blocks));
   }
   if (n_tokens * Hq >= kMaxGrid) p.n_splits = 1;  // (the join has a workgroup per row)
   return p;
@@ -1676,6 +1699,7 @@ ckv_status launch_shared_attn(PageAttnArgs& a, const SharedPlan& p, char* ws, hi
   a.n_parts = shared_parts;
   a.n_splits = p.shared.n_splits;
   a.slice = p.shared.slice;
+  a.n_wgs = p.shared.n_wgs;
   PageAttnArgs own = a;
   own.o_part = o_part + (size_t)p.shared.n_splits * rows * D;
   own.ml_part = ml_part + (size_t)p.shared.n_splits * rows;
