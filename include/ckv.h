@@ -845,8 +845,9 @@ ckv_status ckv_page_extend(const ckv_page_tables* tables, const int32_t* n_new,
  * larger logit, then the lower token.  Scores are held in 64 bits (the exponentials under
  * the logarithm in 32, their sums in 64) and rounded once.  -inf and NaN logits offer
  * nothing and add nothing; an infinity counts as the largest finite number.
- *   parent  r * n_beams + b; token; score; done: 1 for eos and for who was done.  Where
- *           fewer are offered: -1, -1, -inf, 0
+ *   parent  r * n_beams + b; token; score; done (may be NULL): 1 for eos and for who was
+ *           done.  Where fewer are offered: -1, -1, -inf, 0.  [n_reqs][keep], other buffers
+ *           than the beams' own
  *   ws      ckv_beam_select_workspace_bytes(...) bytes for the same beams */
 typedef struct ckv_beams {
   const void* logits;    /* device, rows r * n_beams + b of vocab elements, aligned to one */

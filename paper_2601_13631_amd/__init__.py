@@ -538,6 +538,12 @@ def _together(t, *handles) -> int:
     return device
 
 
+def _current(device: int) -> int:
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"the call's tensors are on device {device}, not the current one")
+    return device
+
+
 def _stream_on(device: int, stream) -> int | None:
     """``_stream`` where the current device is known."""
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
@@ -752,7 +758,7 @@ def page_share(page_size: int, batch: PageBatch, groups: PageGroups, stream=None
     """``ckv_page_share``: what each group's sequences share, for :func:`page_attn_shared` in
     every layer; again whenever the table, the lengths or the offsets have changed."""
     groups._fits(batch)
-    device = _together(groups.grp_off, groups, batch)
+    device = _current(_together(groups.grp_off, groups, batch))
     _check(_lib.ckv_page_share(_int32(page_size, "page_size"), batch._c, groups._c, _stream_on(device, stream)),
            "ckv_page_share")
 
@@ -902,9 +908,7 @@ def page_extend(step: PageStep, ws, stream=None) -> None:
     """``ckv_page_extend``: pages for every sequence's ``n_new`` tokens, and what the step's token rows
     are; then :func:`page_copy` of ``copy_src`` to ``copy_dst``, and :func:`page_append`.  ``ws``: a uint8
     tensor of :func:`page_extend_workspace_bytes` bytes."""
-    device = _together(step.n_new, step)
-    if device != torch._C._cuda_getDevice():
-        raise ValueError(f"the step is on device {device}, not the current one")
+    device = _current(_together(step.n_new, step))
     ws_ptr, nbytes = _workspace(ws, step.n_new)
     _check(_lib.ckv_page_extend(step._c, _ptr(step.n_new), step._step, ws_ptr, nbytes, _stream_on(device, stream)),
            "ckv_page_extend")
@@ -917,6 +921,8 @@ def _beams(logits, keep: int, scores=None, done=None, eos: int = -1) -> _Beams:
     if logits.dim() != 3 or logits.dtype not in _LOGIT_DTYPES:
         raise ValueError("logits must be a float32 or bfloat16 tensor [n_reqs, n_beams, vocab]")
     n_reqs, n_beams, vocab = logits.shape
+    if not -1 <= eos < 1 << 31:
+        raise ValueError(f"eos must be -1 or a token (it is {eos})")
     if logits.numel() > 0 and vocab > 1 and logits.stride(2) != 1:
         raise ValueError("a beam's logits must be contiguous")
     # (a dimension of one has no stride that counts)

@@ -525,6 +525,8 @@ ckv_status ckv_beam_select(const ckv_beams* beams, int32_t* parent, int32_t* tok
   if (ckv_status s = check_beams(beams, true); s != CKV_OK) return s;
   if (beams->n_reqs == 0) return CKV_OK;
   if (!parent || !token || !score || !ws) CKV_FAIL(CKV_EINVAL, "NULL pointer argument");
+  if (score == beams->scores || (done && done == beams->done))
+    CKV_FAIL(CKV_EINVAL, "the outputs must be other buffers than the beams'");
   const BeamPlan p = make_beam_plan(beams);
   if (ws_bytes < p.bytes) CKV_FAIL(CKV_EINVAL, "workspace too small: %zu < %zu", ws_bytes, p.bytes);
   if (!aligned16(ws)) CKV_FAIL(CKV_EINVAL, "pointers must be 16-byte aligned");

@@ -125,6 +125,8 @@ __device__ __forceinline__ int parts_of(const PageAttnArgs& a, const Unit& x, in
 // Steps of a split of shared keys, so that the groups' splits together are a.n_wgs at most (for
 // one KV head), as many as run at once, however unequal the groups are; a.slice at least.
 __device__ __forceinline__ int shared_slice(const PageAttnArgs& a) {
+  const int more = a.n_wgs - a.n_groups;  // splits beside each group's first
+  if (more <= 0) return 1 << 30;
   int64_t steps = 0;
   for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
     const int g = g0 + (int)(threadIdx.x & 63);
@@ -133,8 +135,6 @@ __device__ __forceinline__ int shared_slice(const PageAttnArgs& a) {
     for (int i = 1; i < 64; i <<= 1) x += __shfl_xor(x, i);
     steps += x;
   }
-  const int more = a.n_wgs - a.n_groups;  // splits beside each group's first
-  if (more <= 0) return 1 << 30;
   return __builtin_amdgcn_readfirstlane((int)max((steps + more - 1) / more, (int64_t)a.slice));
 }
 // What the join reads of a token's sequence: its splits and, of kOwn, whether shared ones go before.

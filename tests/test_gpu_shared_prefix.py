@@ -46,14 +46,15 @@ CASES = [
 WIDE = 1 << 18
 
 
-@pytest.mark.parametrize("hints", ["exact", "wide", "wrong"])
+@pytest.mark.parametrize("hints", ["exact", "wide", "rows", "wrong"])
 @pytest.mark.parametrize("i", range(len(CASES)))
 def test_attention(i, hints):
     cache, heads, page, groups, loose = CASES[i]
     c = GroupCache(cache, heads, page, groups, loose, seed=i, wide=0 if hints == "exact" else WIDE // page)
     c.poison()
-    pool, batch = c.device(**{"exact": {}, "wide": dict(max_len=0), "wrong": dict(max_tokens=3, max_len=WIDE)}[hints])
-    g = c.device_groups(batch, **{"exact": {}, "wide": dict(max_tokens=0, max_shared=0),
+    pool, batch = c.device(**{"exact": {}, "wide": dict(max_len=0), "rows": dict(max_len=0),
+                             "wrong": dict(max_tokens=3, max_len=WIDE)}[hints])
+    g = c.device_groups(batch, **{"exact": {}, "wide": dict(max_tokens=0, max_shared=0), "rows": dict(max_shared=0),
                                   "wrong": dict(max_tokens=20, max_shared=WIDE - 100)}[hints])
     of_group, leader, of_seq = c.shared()
     got = g.shared.cpu().numpy()
@@ -129,6 +130,42 @@ def test_groups_that_are_none():
                                 torch.zeros(ckv.page_share_ints(len(off) - 1, 8), dtype=torch.int32, device=DEV))
         ckv.page_share(16, batch, groups)
         check_attention(c, attend_shared(pool, batch, groups, q))
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_share_of_many(seed):
+    """Groups of hundreds of sequences, thousands of pages, tables that part anywhere or not at all."""
+    import paper_2601_13631_amd as ckv
+    rng = np.random.default_rng(seed)
+    page, width = int(rng.choice((8, 16, 96))), int(rng.choice((3, 70, 1500, 5000)))
+    sizes = rng.integers(0, 300, 5) if width < 1000 else rng.integers(0, 40, 5)
+    n = int(sizes.sum()) + 3
+    first = np.concatenate([[2], 2 + np.cumsum(sizes)])
+    table = rng.integers(-1, 50, (n, width)).astype(np.int32)
+    lens, new = rng.integers(1, width * page + 40, n), rng.integers(0, 4, n)
+    for f, l in zip(first, first[1:]):
+        table[f:l] = table[f] if l > f else 0
+        if rng.random() < 0.7:
+            lens[f:l] = width * page - rng.integers(0, 9, l - f)
+        for b in rng.integers(f, l, 2) if l > f and rng.random() < 0.7 else ():
+            table[b, int(rng.integers(0, width))] += 1
+    off = np.concatenate([[0], np.cumsum(new)])
+    want_g, want_s = [], np.zeros(n, int)
+    for f, l in zip(first, first[1:]):
+        active = [b for b in range(f, l) if new[b]]
+        e = 0
+        if active:
+            agree = (table[active] == table[active[0]]).all(0)
+            common = width if agree.all() else int(np.argmin(agree))
+            e = max(min(common * page, min(lens[b] - new[b] + 1 for b in active)), 0) // 32 * 32
+        want_g.append(e)
+        want_s[f:l] = e
+    t = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.int32)).to(DEV)  # noqa: E731
+    batch = ckv.PageBatch(t(table), t(lens), t(off), int(off[-1]))
+    shared = torch.full((ckv.page_share_ints(5, n),), -9, dtype=torch.int32, device=DEV)
+    ckv.page_share(page, batch, ckv.PageGroups(t(first), shared))
+    got = shared.cpu().numpy()
+    assert (got[:5] == want_g).all() and (got[10:] == want_s).all()
 
 
 def draw(seed):

@@ -159,11 +159,19 @@ def test_bad_beams(over, status):
 def test_bad_select():
     need = ckv._lib.ckv_beam_select_workspace_bytes(beams())
     assert need > 0 and ckv._lib.ckv_beam_select_workspace_bytes(beams(keep=65)) == 0
-    for args in ((None, P, P, P, P, need), (P, None, P, P, P, need), (P, P, None, P, P, need), (P, P, P, P, None, need),
-                 (P, P, P, P, P, need - 1), (P, P, P, P, P + 8, need)):
+    Q = 2 * P
+    for args in ((None, P, Q, P, P, need), (P, None, Q, P, P, need), (P, P, None, P, P, need), (P, P, Q, P, None, need),
+                 (P, P, Q, P, P, need - 1), (P, P, Q, P, P + 8, need)):
         parent, token, score, done, ws, nbytes = args
         assert ckv._lib.ckv_beam_select(beams(), parent, token, score, done, ws, nbytes, None) == ckv.EINVAL
     assert ckv._lib.ckv_beam_select(None, P, P, P, P, P, need, None) == ckv.EINVAL
+    # outputs in the inputs' buffers
+    for over, score, done in ((dict(scores=P), P, 2 * P), (dict(scores=P, done=2 * P, eos=3), 3 * P, 2 * P)):
+        assert ckv._lib.ckv_beam_select(beams(**over), P, P, score, done, P, need, None) == ckv.EINVAL
+        assert "buffers" in ckv.last_error()
+    for eos in (-2, 1 << 31, 1 << 40):
+        with pytest.raises(ValueError, match="eos"):
+            ckv._beams(torch.zeros(1, 2, 30), 2, eos=eos)
 
 
 def test_nothing_to_do():
