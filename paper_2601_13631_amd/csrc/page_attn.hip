@@ -1668,7 +1668,7 @@ ckv_status launch_join(const PageAttnArgs& a, hipStream_t st) {
   constexpr int kUnits = 256 / (D / 4);
   const int64_t rows = a.s.n_tokens * a.Hq;
   // Groups that take kJoinBatch places each at once, no more than there are places for: loads past
-  // the last place are made all the same (2,560 rows of 9 places: 10 us with 8 groups, JOIN with 2).
+  // the last place are made all the same (2,560 rows of 9 places: 9.9 us with 8 groups, 5.4 with 2).
   int groups = 1;
   while (groups < kUnits && groups * kJoinBatch < a.n_splits) groups *= kParts ? 2 : kUnits;
   auto kernel = groups == 1 ? page_combine_kernel<D, QT, 1, kParts> : page_combine_kernel<D, QT, kUnits, kParts>;

@@ -100,8 +100,9 @@ struct ShareArgs {
 
 // A workgroup per group: its waves go over the sequences in turn, lanes along the table,
 // against the first sequence with tokens.  One more for the sequences of no group.
-// The loads of a wave's rounds are its time, so four sequences go together: 48 sequences of 970
-// pages 11.4 us one at a time, KSHARE so.
+// Its time is that of the loads' rounds, one after the other: the offsets, the lengths, the tables
+// (four sequences of a wave together: 48 sequences of 970 pages 8.8 us, one at a time 11.4; four of 65
+// pages 3.7).
 constexpr int kShareThreads = 1024, kShareBatch = 16, kShareSeqs = 4;
 __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
   const auto begin_of = [&](int g) { return min(max(a.grp_off[g], 0), a.s.n_seqs); };
