@@ -314,23 +314,18 @@ struct ExtendArgs {
   int64_t table_blocks;
 };
 
-// Use counts of this thread's pages p0 .. p0 + 3; 1 past the last page.
+// Use counts of four pages, this thread's p0 .. p0 + 3 or, where they would reach past the last
+// page, the last four of all (n_pages is at least 4): no branch keeps one load waiting for another.
+// `first` gets which of them are this thread's, from first on.
+__device__ __forceinline__ void load_four(const Tables& t, int p0, int32_t (&refs)[kPlanPer], int& first) {
+  const uint32_t at = (uint32_t)min(p0, t.n_pages - kPlanPer);  // (2^26 pages at most)
+  first = min(p0 - (int)at, kPlanPer);
+  __builtin_memcpy(refs, reinterpret_cast<const char*>(t.refs) + at * 4, sizeof refs);
+}
+// The same in their places; 1 past the last page.
 __device__ __forceinline__ void load_refs(const Tables& t, int64_t p0, int32_t (&refs)[kPlanPer]) {
-  if (t.n_pages >= kPlanPer) {  // (uniform)
-    // the last ones of all at most, of which those before p0 are left out
-    const int64_t at = min(p0, (int64_t)t.n_pages - kPlanPer);
-    const int by = (int)min(p0 - at, (int64_t)kPlanPer);
-    int32_t x[kPlanPer];
-    __builtin_memcpy(x, t.refs + at, sizeof x);
 #pragma unroll
-    for (int i = 0; i < kPlanPer; ++i) refs[i] = x[i];
-    if (by)
-#pragma unroll
-      for (int i = 0; i < kPlanPer; ++i) refs[i] = i + by < kPlanPer ? x[(i + by) & (kPlanPer - 1)] : 1;
-  } else {
-#pragma unroll
-    for (int i = 0; i < kPlanPer; ++i) refs[i] = p0 + i < t.n_pages ? t.refs[p0 + i] : 1;
-  }
+  for (int i = 0; i < kPlanPer; ++i) refs[i] = p0 + i < t.n_pages ? t.refs[p0 + i] : 1;
 }
 __device__ __forceinline__ int free_of(const int32_t (&refs)[kPlanPer]) {
   int n = 0;
@@ -347,19 +342,27 @@ __global__ __launch_bounds__(kPlanThreads) void extend_count_kernel(ExtendArgs a
 }
 
 // This thread's share of the free pages of the first `blocks` blocks.  kCounted: their counts
-// are there; else every workgroup goes over their use counts itself, in one round of loads.
+// are there; else every workgroup goes over their use counts itself.
 template <bool kCounted>
 __device__ __forceinline__ int free_below(const ExtendArgs& a, int blocks) {
+  const Tables& t = a.t;
   int n = 0;
   if constexpr (kCounted) {
     for (int i = threadIdx.x; i < blocks; i += kPlanThreads) n += a.counts[i];
   } else {
-    int32_t refs[kSelfCounted][kPlanPer];
+    constexpr int kAtOnce = 8;  // (32 registers of the 128 that 16 waves leave each)
+#pragma unroll 1
+    for (int i0 = 0; i0 < blocks; i0 += kAtOnce) {
+      int32_t refs[kAtOnce][kPlanPer];
+      int first[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < kSelfCounted; ++i)
-      if (i < blocks) load_refs(a.t, (int64_t)i * kPlanPages + threadIdx.x * kPlanPer, refs[i]);
+      for (int i = 0; i < kAtOnce; ++i)
+        load_four(t, min(i0 + i, blocks - 1) * kPlanPages + (int)threadIdx.x * kPlanPer, refs[i], first[i]);
 #pragma unroll
-    for (int i = 0; i < kSelfCounted; ++i) n += i < blocks ? free_of(refs[i]) : 0;
+      for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+        for (int k = 0; k < kPlanPer; ++k) n += i0 + i < blocks && k >= first[i] && refs[i][k] <= 0;
+    }
   }
   return n;
 }
@@ -383,7 +386,7 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
     return;
   }
   // the sequences, in their order
-  int64_t n_free = free_below<kCounted>(a, a.plan_blocks);
+  int64_t n_free = free_below<kCounted>(a, a.plan_blocks);  // (this thread's share; of all from the first sums on)
   int64_t needed = 0, asked = 0, taken = 0, tokens = 0;
   int refused = 0;  // of this thread's sequences
   if (threadIdx.x == 0) a.o.tok_off[0] = 0;
@@ -393,8 +396,9 @@ __global__ __launch_bounds__(kPlanThreads) void extend_plan_kernel(ExtendArgs a)
     int len = 0, tail = -1;
     bool no = false;
     if (b < t.n_seqs) {
-      len = t.length(t.lens[b]);
-      add = max(a.n_new[b], 0);
+      const int said = t.lens[b], more = a.n_new[b];
+      len = t.length(said);
+      add = max(more, 0);
       const int held = t.pages(len);
       const int64_t upto = (int64_t)len + add;
       no = upto > (int64_t)t.max_pages * t.c;
@@ -686,7 +690,7 @@ ckv_status ckv_page_extend(const ckv_page_tables* tables, const int32_t* n_new, 
   const int64_t grid = a.table_blocks + (rows ? ceil_div(step->n_tokens, kThreads) : 0);
   if (grid >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
   const hipStream_t st = (hipStream_t)stream;
-  if (a.plan_blocks <= kSelfCounted) {
+  if (a.plan_blocks <= kSelfCounted && a.t.n_pages >= kPlanPer) {
     hipLaunchKernelGGL(extend_plan_kernel<false>, dim3(a.plan_blocks + 1), dim3(kPlanThreads), 0, st, a);
   } else {
     hipLaunchKernelGGL(extend_count_kernel, dim3(a.plan_blocks), dim3(kPlanThreads), 0, st, a);
