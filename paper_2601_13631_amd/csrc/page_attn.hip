@@ -22,6 +22,14 @@
 // with a window of 4,096 in bf16 80 us, 4.6 TB/s; 512 tokens on 32,768 others, 28 heads on 4:
 // 239 to 254 us by the card, 955 to 1,010 TFLOP/s, in bf16 and 8 bits alike (a matrix product of
 // 8,192 reaches 1,210 to 1,230); five prompts of up to 2,048 tokens with a window of 1,000 130 us, 766.
+//
+// Groups of sequences that share their first pages (page_parts_kernel): the softmax is taken in two
+// parts, over the shared keys for all rows of a group at once and over each sequence's own keys
+// behind them, each against its own reference; the join of the splits makes one of both, for any
+// references.  48 sequences on 30,011 shared tokens in bf16, 28 heads on 4: 51 us a layer, where each
+// sequence by itself reads 3 GB; eight groups of eight on up to 16,384 in 8 bits, 40 heads on 8: 60 us,
+// 3.3 TB/s of bytes read once; 24 prompts of up to 48 tokens on 32,768 in 8 bits: 335 us, 1,000 TFLOP/s,
+// apart 541.
 
 #include <type_traits>
 
@@ -269,26 +277,7 @@ __device__ __forceinline__ uint32_t finite_codes(uint32_t w) {
   return (w & ~(top * 0x7fu)) | top * 0x77u;
 }
 
-// Few rows: a workgroup owns 16 query rows of one KV head and one split of their
-// steps, its 4 or 8 waves step by step in turn:
-//   S^T = K Q^T    MFMA 16x16 (bf16: x32, fp32: x4), two groups of 16 keys; lane l
-//                  then holds row l % 16 and keys 4 (l / 16) + 0..3 of each group
-//   O^T += V^T P^T the contraction's 8 (bf16) keys per lane are those it holds, so
-//                  P^T goes from the softmax registers to the MFMA as it is; lane l
-//                  loads D/16 elements from l % 16 * D/16 on of its 8 keys' V rows, and
-//                  product i of D/16 takes element i of each (8 keys x D/16 elements
-//                  are turned over in registers).
-// V rows go straight to registers, 16 lanes a row.  The K operand wants neighbouring
-// lanes in different rows, which read so cost the cache an access per 16 bytes: K rows go
-// whole to LDS, a step ahead, into a buffer of the wave's own (64 sequences in 8 bits: 173 us
-// with K read to registers, 165 so).  The waves' outputs are joined through LDS.
-// Bound by memory, and by latency where there is little of it: a decoding step of one
-// sequence of 1,000 tokens takes 6.6 us: four dependent round trips, two steps per wave of 0.9,
-// the waves' join 0.4.
-// kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page).
-// kBlocks: 16-row blocks of a workgroup, which share the keys as loaded, converted and turned over
-// (their query rows then come from LDS).
-// Where its waves' K rows lie in LDS, after the last step their outputs with references and sums,
+// Few rows: where the waves' K rows lie in LDS, after the last step their outputs with references and sums,
 // and the query rows: its own memory, or that of another kernel's part in one launch.
 template <int D, int T, int kWaves, int kBlocks>
 struct RowsLds {
@@ -310,7 +299,30 @@ struct RowsLds {
   __device__ __forceinline__ float2* ml(int w) const { return reinterpret_cast<float2*>(lds + kWaves * kOut) + w * kRows; }
 };
 
-// (bx, by) of a grid gy high.
+// Few rows: a workgroup owns 16 query rows of one KV head and one split of their
+// steps, its 4 or 8 waves step by step in turn:
+//   S^T = K Q^T    MFMA 16x16 (bf16: x32, fp32: x4), two groups of 16 keys; lane l
+//                  then holds row l % 16 and keys 4 (l / 16) + 0..3 of each group
+//   O^T += V^T P^T the contraction's 8 (bf16) keys per lane are those it holds, so
+//                  P^T goes from the softmax registers to the MFMA as it is; lane l
+//                  loads D/16 elements from l % 16 * D/16 on of its 8 keys' V rows, and
+//                  product i of D/16 takes element i of each (8 keys x D/16 elements
+//                  are turned over in registers).
+// V rows go straight to registers, 16 lanes a row.  The K operand wants neighbouring
+// lanes in different rows, which read so cost the cache an access per 16 bytes: K rows go
+// whole to LDS, a step ahead, into a buffer of the wave's own (64 sequences in 8 bits: 173 us
+// with K read to registers, 165 so).  The waves' outputs are joined through LDS.
+// Bound by memory, and by latency where there is little of it: a decoding step of one
+// sequence of 1,000 tokens takes 6.6 us: four dependent round trips, two steps per wave of 0.9,
+// the waves' join 0.4.
+// kSmall: pages of 8 tokens, four in a step (else at least 16 keys share a page).
+// kBlocks: 16-row blocks of a workgroup, which share the keys as loaded, converted and turned over;
+// their query rows then come from LDS.  Up to 48 rows of a group go so (32 in bf16 at head_dim 128,
+// where three blocks take every register): eight groups of 40 rows in 8 bits, with 1,024 workgroups
+// each, shared keys alone 67 us in 128-row tiles, 52 in three blocks; four groups' 42 rows in bf16
+// 63 in tiles, 68 in three blocks.  More rows in several such workgroups: 336 rows 49 to 53 us where
+// the tiles take 44.
+// The workgroup is (bx, by) of a grid gy high.
 template <int D, int T, bool kSmall, int kWaves, int P, int kBlocks, class Lds>
 __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, uint32_t by, uint32_t gy, const Lds& lds) {
   using E = Elem<T>;
@@ -1301,7 +1313,10 @@ __global__ __launch_bounds__(256, 2) void page_tile_kernel(PageAttnArgs a) {
 }
 
 // The shared keys and the sequences' own in one launch, the shared ones first: the own keys, few
-// and read by workgroups of a few steps each, then fill what the others leave idle.
+// and read by workgroups of a few steps each, then fill what the others leave idle (48 sequences on
+// a document: two launches 55.5 us a layer, one 45.8; eight groups of eight 77 and 67).
+// Bound by latency where a group has few rows: a wave has one step of keys under way, 2,048 waves 16
+// MB, and they wait for 7,000 cycles a step.
 // kBlocks: of rows_part for the shared keys; 0: tile_part, in whose memory the own ones' waves
 // have a buffer each.
 struct TileRowsLds {

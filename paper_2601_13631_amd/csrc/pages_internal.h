@@ -50,7 +50,7 @@ __device__ __forceinline__ SeqSpan seq_span(const PageSeqs& s, int b) {
   return SeqSpan{lo, (int32_t)max<int64_t>(hi - lo, 0), s.lens[b]};
 }
 
-// The last sequence b of n with start(b) <= k, -1 if there is none; start must not fall.  A whole
+// The last b of n sequences (or groups) with start(b) <= k, -1 if there is none; start must not fall.  A whole
 // wave calls it: 64 sequences are looked at at a time (one round of loads for 64 of them, two
 // for 4,096).
 // Work that the sequences have in parts is numbered so: sequence b's parts from start(b) on,
