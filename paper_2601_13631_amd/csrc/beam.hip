@@ -254,14 +254,15 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
   clear(-0x1p125f);
   {
     // whole batches, two of them under way; the lanes' addresses are a common one and 16 bytes each
-    const int n_whole = n_batches - (b0 + (int64_t)n_batches * kWaves - kWaves + 1 > end / kBatch ? 1 : 0);
+    const int64_t last = b0 + (int64_t)(n_batches - 1) * kWaves;
+    const int n_whole = n_batches > 0 && (last + 1) * kBatch > end ? n_batches - 1 : n_batches;
     auto fetch = [&](int n, Batch& x) __attribute__((always_inline)) {  // (past the last: that one again)
       const char* from = base + (b0 + (int64_t)min(n, n_whole - 1) * kWaves) * (kBatch * kBytes);
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) x[i] = piece_at(from + (uint32_t)(lane * 16) + i * 1024);
     };
     constexpr std::false_type plain{};
-    if (n_batches > 0 && n_whole > 0) {
+    if (n_whole > 0) {
       Batch x, y, z;
       fetch(0, x);
       fetch(1, y);

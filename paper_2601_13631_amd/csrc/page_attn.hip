@@ -1667,7 +1667,12 @@ ckv_status launch_parts(PageAttnArgs& shared, PageAttnArgs& own, const SharedPla
   Grid x, y;
   if (ckv_status s = grid_of(shared, p.shared, shared.n_groups, x); s != CKV_OK) return s;
   if (ckv_status s = grid_of(own, p.own, own.s.n_seqs, y); s != CKV_OK) return s;
-  const int64_t first = x.x * x.y, all = first + y.x * y.y;
+  // (a workgroup goes on to the row blocks that a lower grid leaves)
+  if (x.x * x.y + y.x * y.y >= kMaxGrid) {
+    x.y = std::min(x.y, std::max<int64_t>(1, kMaxGrid / 2 / x.x - 1));
+    y.y = std::min(y.y, std::max<int64_t>(1, kMaxGrid / 2 / y.x - 1));
+  }
+  const int64_t all = x.x * x.y + y.x * y.y;
   if (all >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
   const auto kernel = own.c == 8 ? page_parts_kernel<D, T, true, kBlocks> : page_parts_kernel<D, T, false, kBlocks>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)all), dim3(256), 0, st, shared, own, (uint32_t)x.x, (uint32_t)x.y,
