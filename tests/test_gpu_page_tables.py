@@ -133,6 +133,24 @@ def test_extend_when_pages_run_out():
         assert (got[k] == np.asarray(want[k])).all(), k
 
 
+@pytest.mark.parametrize("given", [(), ("slots",), ("positions", "seqs")])
+def test_extend_writes_what_is_asked_for(given):
+    import paper_2601_13631_amd as ckv
+    rng = np.random.default_rng(8)
+    table, lens, refs = tables(rng, 30, 6, 400, 16)
+    n_new = rng.integers(0, 20, 30)
+    total = int(n_new.sum()) + 300
+    t, l, r, off, src, dst, counts = (dev(x) for x in (table, lens, refs, np.zeros(31), np.zeros(30), np.zeros(30),
+                                                       np.zeros(4)))
+    rows = {k: torch.zeros(total, dtype=torch.int64 if k == "slots" else torch.int32, device=DEV) for k in given}
+    step = ckv.PageStep(16, t, t, l, l, r, r, dev(n_new), off, src, dst, counts, n_tokens=total, **rows)
+    ckv.page_extend(step, torch.zeros(ckv.page_extend_workspace_bytes(400, 30), dtype=torch.uint8, device=DEV))
+    want = extend_model(16, table, lens, refs, n_new, total)
+    for k, x in {"table": t, "lens": l, "refs": r, "tok_off": off, "copy_src": src, "copy_dst": dst, "counts": counts,
+                 **rows}.items():
+        assert (x.cpu().numpy() == np.asarray(want[k])).all(), k
+
+
 def test_tables_replay():
     """A captured fork and step, replayed on other tables."""
     import paper_2601_13631_amd as ckv
@@ -273,6 +291,14 @@ def test_select_keeps_empty_places_empty():
     check_select(x, scores, None, 4, -1)
     scores[0, 1] = -4.0
     check_select(x, scores, torch.ones(2, 3, dtype=torch.uint8), 4, 49)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_select_rows_far_apart(kind):
+    """Rows more than 2^31 elements and 4 GiB from the first."""
+    g = torch.Generator().manual_seed(6)
+    check_select((torch.randn(1, 4, 3001, generator=g) * 3).to(T[kind]), torch.tensor([[-1.0, -2.0, -0.5, -1.5]]), None, 6,
+                 -1, gap=(3 << 28) + 1)
 
 
 def test_select_replay():

@@ -168,6 +168,17 @@ def test_share_of_many(seed):
     assert (got[:5] == want_g).all() and (got[10:] == want_s).all()
 
 
+@pytest.mark.parametrize("cache,heads", [("bf16", H7), ("e4m3", H14)])
+def test_pages_far_apart(cache, heads):
+    """Pages more than 4 GiB from the pool's begin."""
+    c = GroupCache(cache, heads, 16, [(80, [(1, 3), (1, 20), (2, 40)])], seed=4, wide=WIDE // 16,
+                   gap=(700 << 20) if cache == "e4m3" else 350 << 20)
+    assert (c.n_pages - 1) * c.gap > 1 << 32
+    c.poison()
+    pool, batch = c.device(max_len=0)
+    check_attention(c, attend_shared(pool, batch, c.device_groups(batch, max_shared=0), c.q.to(DEV)))
+
+
 def draw(seed):
     rng = np.random.default_rng(3000 + seed)
     cache = ("bf16", "e4m3", "bf16", "e4m3", "f32")[seed % 5]
