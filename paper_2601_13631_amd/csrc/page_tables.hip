@@ -4,7 +4,7 @@
 // Integers throughout: page numbers, lengths, use counts.  A call moves a megabyte or two at
 // most, in the L2s' reach: launches and the dependent loads of a workgroup (a length, a table
 // entry, that page's count) are what it takes.  Sums are of integers, so atomics leave the
-// same result in any order.  Measured: shares of four sequences 3.6 us, of 48 on 30,000 tokens 9; a
+// same result in any order.  Measured: shares of four sequences 3.4 us, of 48 on 30,000 tokens 8.8; a
 // fork of 256 sequences of 500 pages 7.8 (3.0 and 4.3 in its two kernels); a step of as many on
 // 65,536 pages 11.4 (7.9 and 3.7), 40 prompts of up to 6,000 tokens 9.8.
 
@@ -102,9 +102,8 @@ struct ShareArgs {
 
 // A workgroup per group: its waves go over the sequences in turn, lanes along the table,
 // against the first sequence with tokens.  One more for the sequences of no group.
-// Its time is that of the loads' rounds, one after the other: the offsets, the lengths, the tables
-// (four sequences of a wave together: 48 sequences of 970 pages 8.8 us, one at a time 11.4; four of 65
-// pages 3.7).
+// Its time is that of the loads' rounds, one after the other (offsets, lengths, tables: four sequences of
+// 65 pages 3.4 us), and of one CU's misses (48 of 970 pages 8.8; a sequence of a wave at a time 11.4).
 constexpr int kShareThreads = 1024, kShareBatch = 16, kShareSeqs = 4;
 __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
   const auto begin_of = [&](int g) { return min(max(a.grp_off[g], 0), a.s.n_seqs); };
@@ -118,38 +117,32 @@ __global__ __launch_bounds__(kShareThreads) void share_kernel(ShareArgs a) {
   }
   const int f = begin_of(g), l = begin_of(g + 1);
   constexpr int kWavesOf = kShareThreads / 64;
-  __shared__ int common, part[2][kWavesOf];
+  __shared__ int common;
+  // Every wave goes over the group's sequences itself, 64 at a time: no wave waits for another.
   int leader = INT32_MAX, least = INT32_MAX;
-  for (int b = f + tid; b < l; b += kShareThreads) {
+  uint64_t active = 0;  // of the first 64
+  for (int b0 = f; b0 < l; b0 += 64) {
+    const int b = min(b0 + lane, l - 1);
     const SeqSpan sp = seq_span(a.s, b);
-    if (sp.count == 0) continue;
-    leader = min(leader, b);
-    least = min(least, sp.len - sp.count + 1);
+    const uint64_t some = __ballot(b0 + lane < l && sp.count > 0);
+    least = min(least, some >> lane & 1 ? sp.len - sp.count + 1 : INT32_MAX);
+    if (some && leader == INT32_MAX) leader = b0 + __builtin_ctzll(some);
+    if (b0 == f) active = some;
   }
-  leader = wave_least(leader);
   least = wave_least(least);
-  if (lane == 0) {
-    part[0][wave] = leader;
-    part[1][wave] = least;
-  }
-  __syncthreads();
-  leader = wave_least(lane < kWavesOf ? part[0][lane] : INT32_MAX);
-  least = wave_least(lane < kWavesOf ? part[1][lane] : INT32_MAX);
   const int seen = leader == INT32_MAX ? 0 : (int)min((int64_t)max(least, 0), (int64_t)a.s.max_pages * a.c);
   const int slots = (seen + a.c - 1) / a.c;
   if (tid == 0) common = slots;
   __syncthreads();
-  const int32_t* const first = a.s.table + (int64_t)leader * a.s.table_stride;
+  const int32_t* const first = a.s.table + (int64_t)min(leader, a.s.n_seqs - 1) * a.s.table_stride;
   for (int b0 = f + wave; b0 < l && slots > 0; b0 += kWavesOf * kShareSeqs) {
     // (a sequence that is not there or has no tokens: the first one again)
     const int32_t* mine[kShareSeqs];
-    SeqSpan sp[kShareSeqs];
-#pragma unroll
-    for (int i = 0; i < kShareSeqs; ++i) sp[i] = seq_span(a.s, min(b0 + i * kWavesOf, l - 1));
 #pragma unroll
     for (int i = 0; i < kShareSeqs; ++i) {
       const int b = b0 + i * kWavesOf;
-      mine[i] = b < l && sp[i].count > 0 ? a.s.table + (int64_t)b * a.s.table_stride : first;
+      const bool there = b < l && (b - f < 64 ? active >> (b - f & 63) & 1 : seq_span(a.s, min(b, l - 1)).count > 0);
+      mine[i] = there ? a.s.table + (int64_t)b * a.s.table_stride : first;
     }
     for (int s0 = 0; s0 < slots; s0 += 64 * kShareBatch) {
       int x[kShareBatch], y[kShareSeqs][kShareBatch];
