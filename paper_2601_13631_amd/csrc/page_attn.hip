@@ -1466,8 +1466,12 @@ constexpr int kFewRows = 32;  // rows of a sequence that page_rows_kernel takes 
 // of them 68.7 us, 384 63.7, 416 59.3, 448 61.7, 512 68.5; in bf16 28 heads on 4, groups of four: 52.5,
 // 49.4, 49.2, 51.4, 52.9).
 constexpr int64_t kSharedBlocks = 416;
-// Bytes of shared pages read again and again that are worth the parts' launch and join.
-constexpr int64_t kWorthParts = int64_t(40) << 20;
+// Bytes of shared pages read again and again that are worth the parts' launch and join.  Decoding, 28 heads
+// on 4 in bf16: 4 sequences on 4,000 tokens (25 MB) apart 12.7 us, in parts 14.7; 2 groups of 2 on 8,000 in 8
+// bits, 40 heads on 8 (33 MB) 18.6, 17.2; 4 on 8,000 (49 MB) 18.6, 15.1; 8 on 4,000 (57 MB) 18.7, 15.2; but 16 on
+// 2,000 (61 MB) 13.1, 15.5.  Prompts gain by fuller tiles only: 8 of 30 tokens on 4,000 (57 MB) 34.7, 39.6; 8
+// of 30 on 16,000 in 8 bits (114 MB) 73.9, 69.7; 16 of 8 on 16,000 (491 MB) 79.1, 45.2.
+constexpr int64_t kWorthParts = int64_t(40) << 20, kWorthPrompts = int64_t(96) << 20;
 
 struct PageAttnPlan {
   bool wide;       // page_tile_kernel
@@ -1562,7 +1566,7 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
 
 // Attention of groups: a launch over the shared keys, one over the sequences' own, the join.
 struct SharedPlan {
-  bool apart;  // false: every sequence by itself is less work than the parts and their join
+  bool apart;  // in parts; false: every sequence by itself is less work than those and their join
   PageAttnPlan whole, shared, own;
   size_t off_ml, off_shared, off_own, bytes;
 };
@@ -1575,7 +1579,8 @@ SharedPlan make_shared_plan(const ckv_page_pool* pool, const ckv_page_batch* b, 
   const int64_t most = most_tokens(b->max_tokens, b->n_tokens, b->n_seqs);
   const int64_t saved = ((int64_t)b->n_seqs - g->n_groups) * shared_len * 2 * pool->n_kv_heads * pool->head_dim *
                         page_elem_bytes(pool->dtype);
-  p.apart = g->n_groups > 0 && saved >= kWorthParts;
+  const bool prompts = pool->dtype != CKV_DTYPE_F32 && most * G > kFewRows;
+  p.apart = g->n_groups > 0 && saved >= (prompts ? kWorthPrompts : kWorthParts);
   if (!p.apart) {
     // A few short sequences: a step for each of a workgroup's 8 waves where that is a workgroup per CU
     // at most (15 sequences of 1,100 keys in fp32, splits of 16 steps 14.2 us, of 8 11.3; two of 4,000 in
