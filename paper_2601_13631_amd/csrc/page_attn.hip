@@ -77,8 +77,10 @@ struct PageAttnArgs {
 
 // What a launch attends over: whole sequences; or, where groups of them share a prefix, in one
 // launch the shared keys for all rows of a group, in another each sequence's own keys behind
-// them.  The parts meet in the join of the splits.
-enum Part { kWhole, kShared, kOwn };
+// them.  The parts meet in the join of the splits.  kAlone: whole sequences in fp32, their
+// exponents as those of the parts (rows_part).
+enum Part { kWhole, kShared, kOwn, kAlone };
+constexpr bool is_whole(int part) { return part == kWhole || part == kAlone; }
 
 // The rows and keys of one unit of a launch's work: a sequence, or a group (kShared), whose
 // rows are those of its sequences.
@@ -127,7 +129,7 @@ __device__ __forceinline__ Unit unit_of(const PageAttnArgs& a, int u) {
 // rows' zeros; a part that another one completes has none.
 template <int P>
 __device__ __forceinline__ int parts_of(const PageAttnArgs& a, const Unit& x, int steps, int slice) {
-  const int least = P == kWhole || (P == kOwn && x.first == 0) ? 1 : 0;
+  const int least = is_whole(P) || (P == kOwn && x.first == 0) ? 1 : 0;
   return min(max((steps + slice - 1) / slice, least), a.n_splits);
 }
 // Steps of a split of shared keys, so that the groups' splits together are a.n_wgs at most (for
@@ -329,6 +331,10 @@ __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, ui
   using QT = typename E::Q;
   constexpr bool kF32 = T == CKV_DTYPE_F32, kE4 = T == CKV_DTYPE_E4M3;
   static_assert(kBlocks == 1 || !kF32);
+  // In fp32, but for ckv_page_attn, an exponent s c1 - m is rounded once, so that keys near the
+  // maximum, which count, lose nothing to the size of s c1, and a logit is the sum of four parts:
+  // 12 cases of logits around 10 are 1.8e-7 to 5.8e-7 off 64 bits, 2.9e-7 to 1.3e-6 without.
+  constexpr bool kFused = kF32 && P != kWhole;
   constexpr int kVec = D / 16;                    // elements of a V row per lane, and products of O
   constexpr int kRow = D * E::kBytes;             // bytes of a K row in LDS
   constexpr int kPieces = kRow / 64;              // 16-byte pieces of a K row per lane
@@ -354,7 +360,7 @@ __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, ui
   // this sequence's own number of splits, by its length
   const int all_steps = steps_of<P>(a, p_base, p_base + sp.count - 1, unit.first, kv_end).n;
   const int n_parts = parts_of<P>(a, unit, all_steps, P == kShared ? shared_slice(a) : a.slice);
-  if ((P != kWhole || a.n_splits > 1) && split == 0 && g == 0 && by == 0)
+  if ((!is_whole(P) || a.n_splits > 1) && split == 0 && g == 0 && by == 0)
     for (int i = threadIdx.x; i < sp.count; i += 64 * kWaves) a.n_parts[sp.first + i] = parts_note<P>(unit, n_parts);
   if (split >= n_parts) return;
 
@@ -541,7 +547,24 @@ __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, ui
       for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
         for (int i = 0; i < 2; ++i) s[k][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (kF32) {
+      if constexpr (kFused) {
+        // (a sum for each quarter of the products: half the roundings in a row, and no product waits
+        // for the one before)
+        f32x4 part[kPieces][2];
+#pragma unroll
+        for (int y = 0; y < kPieces; ++y)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) part[y][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+#pragma unroll
+          for (int y = 0; y < kPieces; ++y)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              part[y][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[i][y][z]), qf[y][z], part[y][i], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s[0][i] = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
+      } else if constexpr (kF32) {
 #pragma unroll
         for (int y = 0; y < kPieces; ++y)
 #pragma unroll
@@ -604,8 +627,12 @@ __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, ui
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            s[k][i][y] *= a.c1;
-            mx = fmaxf(mx, s[k][i][y]);
+            if constexpr (kFused) {
+              mx = fmaxf(mx, s[k][i][y] * a.c1);
+            } else {
+              s[k][i][y] *= a.c1;
+              mx = fmaxf(mx, s[k][i][y]);
+            }
           }
         if (__any(mx > ref[k] + kSlack)) {
           mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -620,7 +647,7 @@ __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, ui
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            s[k][i][y] = __builtin_amdgcn_exp2f(s[k][i][y] - ref[k]);
+            s[k][i][y] = __builtin_amdgcn_exp2f(kFused ? fmaf(s[k][i][y], a.c1, -ref[k]) : s[k][i][y] - ref[k]);
             if constexpr (kF32) l[k] += s[k][i][y];
           }
         if constexpr (!kF32)
@@ -1653,7 +1680,7 @@ ckv_status launch_units(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) 
   if (p.wide) {
     if constexpr (T != CKV_DTYPE_F32)
       hipLaunchKernelGGL((page_tile_kernel<D, T, P>), dim3((unsigned)g.x), dim3(256), 0, st, a);
-  } else if constexpr (P == kWhole) {
+  } else if constexpr (is_whole(P)) {
     // A launch of at most a workgroup per CU has 8 waves in each, whose fewer steps follow
     // one another (16 sequences of 4 tokens: 13.1 -> 11.7 us, fp32 prompts 8.7 -> 8.0); where
     // there are more, 4 (48 sequences: 80 us, with 8: 94).
@@ -1707,9 +1734,9 @@ ckv_status launch_join(const PageAttnArgs& a, hipStream_t st) {
   return CKV_OK;
 }
 
-template <int D, int T>
+template <int D, int T, int P>
 ckv_status launch_page_attn(PageAttnArgs& a, const PageAttnPlan& p, hipStream_t st) {
-  if (ckv_status s = launch_units<D, T, kWhole>(a, p, st); s != CKV_OK) return s;
+  if (ckv_status s = launch_units<D, T, P>(a, p, st); s != CKV_OK) return s;
   return a.n_splits > 1 ? launch_join<D, T, false>(a, st) : CKV_OK;
 }
 
@@ -1835,7 +1862,7 @@ ckv_status ckv_page_attn(const ckv_page_pool* pool, const ckv_page_batch* batch,
   set_plan(a, p, ws);
   a.window = window;
   a.sinks = window > 0 ? n_sinks : 0;
-  return for_pool(pool, [&](auto d, auto t) { return launch_page_attn<d, t>(a, p, (hipStream_t)stream); });
+  return for_pool(pool, [&](auto d, auto t) { return launch_page_attn<d, t, kWhole>(a, p, (hipStream_t)stream); });
 }
 
 size_t ckv_page_attn_shared_workspace_bytes(const ckv_page_pool* pool, const ckv_page_batch* batch,
@@ -1860,7 +1887,9 @@ ckv_status ckv_page_attn_shared(const ckv_page_pool* pool, const ckv_page_batch*
   PageAttnArgs a = attn_args(pool, batch, q, n_q_heads, sm_scale, out);
   if (!p.apart) {
     set_plan(a, p.whole, ws);
-    return for_pool(pool, [&](auto d, auto t) { return launch_page_attn<d, t>(a, p.whole, (hipStream_t)stream); });
+    return for_pool(pool, [&](auto d, auto t) {
+      return launch_page_attn<d, t, t == CKV_DTYPE_F32 ? kAlone : kWhole>(a, p.whole, (hipStream_t)stream);
+    });
   }
   a.grp_off = groups->grp_off;
   a.shared = groups->shared;
