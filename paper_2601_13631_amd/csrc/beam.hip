@@ -224,12 +224,17 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_scan_kernel(BeamArgs a) {
 #pragma unroll
     for (int e = 0; e < kPieces * kPer; e += 2) mx = max3(mx, v[e], v[e + 1]);
     if (__any(mx > top)) {
+      // (no product of this block may go into a fused step: sums are carried from the rounded c to the
+      // rounded next one, and what one unrounded would be off by grows with c: 8e-6 in the logarithm for
+      // logits around 500)
+#pragma clang fp contract(off)
       float to = mx;
 #pragma unroll
       for (int i = 1; i < 64; i <<= 1) to = fmaxf(to, __shfl_xor(to, i));
-      sum *= (double)__builtin_amdgcn_exp2f(careful ? (top - to) * kLog2e : c - to * kLog2e);
+      const float next = to * kLog2e;
+      sum *= (double)__builtin_amdgcn_exp2f(careful ? (top - to) * kLog2e : c - next);
       top = to;
-      c = to * kLog2e;
+      c = next;
     }
     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
