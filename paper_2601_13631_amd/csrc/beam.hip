@@ -413,6 +413,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void beam_join_kernel(BeamArgs a) 
         tokens[b * keep] = a.eos;
       }
     } else if (live) {
+      // (every lane is to have the same sum: a product fused into one lane's addition and rounded for the
+      // other's would part their scores by 2^-40 once in thousands of rows, and break ties)
+#pragma clang fp contract(off)
       double top = ref;
 #pragma unroll
       for (int i = 1; i < 64; i <<= 1) top = fmax(top, __shfl_xor(top, i));
