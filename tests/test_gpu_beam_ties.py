@@ -26,7 +26,7 @@ def test_equal_tokens_of_equal_beams(kind, reqs, vocab, calls):
     wrong = torch.zeros((), dtype=torch.long, device=DEV)
     for _ in range(calls):
         one = torch.randn(reqs, 1, vocab, generator=g, device=DEV)
-        one[:, :, lo] = one[:, :, hi] = 6.0
+        one[:, :, lo] = one[:, :, hi] = 9.0  # (6 is passed by one of 10^9 numbers)
         x.copy_(one)
         ckv.beam_select(x, scores, parent, token, best, ws)
         wrong += ((parent != first + torch.tensor([0, 0, 1, 1], dtype=torch.int32, device=DEV)) |
