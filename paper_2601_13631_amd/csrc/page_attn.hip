@@ -46,6 +46,10 @@ constexpr float kNone = -3.4028234663852886e38f;  // reference of a row that has
 // outputs stay below 2^8 times what the maximum itself would give, and a rescaling
 // of the outputs is rare.
 constexpr float kSlack = 8.f;
+// An exponent s c1 - m in one fused step leaves the maximum itself, whose m is rounded, at up to half a
+// step of m: a quarter below 2^23, powers of two that pass the range from 2^30 on.  Rows whose
+// reference is past this take s c1 as rounded too, which the maximum is then exactly.
+constexpr float kFar = 0x1p23f;
 
 struct PageAttnArgs {
   PageSeqs s;
@@ -331,8 +335,8 @@ __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, ui
   using QT = typename E::Q;
   constexpr bool kF32 = T == CKV_DTYPE_F32, kE4 = T == CKV_DTYPE_E4M3;
   static_assert(kBlocks == 1 || !kF32);
-  // In fp32, but for ckv_page_attn, an exponent s c1 - m is rounded once, so that keys near the
-  // maximum, which count, lose nothing to the size of s c1, and a logit is the sum of four parts:
+  // In fp32, but for ckv_page_attn, an exponent s c1 - m is rounded once (up to kFar), so that keys near
+  // the maximum, which count, lose nothing to the size of s c1, and a logit is the sum of four parts:
   // 12 cases of logits around 10 are 1.8e-7 to 5.8e-7 off 64 bits, 2.9e-7 to 1.3e-6 without.
   constexpr bool kFused = kF32 && P != kWhole;
   constexpr int kVec = D / 16;                    // elements of a V row per lane, and products of O
@@ -647,7 +651,13 @@ __device__ __forceinline__ void rows_part(const PageAttnArgs& a, uint32_t bx, ui
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            s[k][i][y] = __builtin_amdgcn_exp2f(kFused ? fmaf(s[k][i][y], a.c1, -ref[k]) : s[k][i][y] - ref[k]);
+            if constexpr (kFused) {
+              const bool far = fabsf(ref[k]) >= kFar;
+              s[k][i][y] = fmaf(far ? s[k][i][y] * a.c1 : s[k][i][y], far ? 1.f : a.c1, -ref[k]);
+            } else {
+              s[k][i][y] -= ref[k];
+            }
+            s[k][i][y] = __builtin_amdgcn_exp2f(s[k][i][y]);
             if constexpr (kF32) l[k] += s[k][i][y];
           }
         if constexpr (!kF32)
