@@ -48,7 +48,8 @@ constexpr float kNone = -3.4028234663852886e38f;  // reference of a row that has
 constexpr float kSlack = 8.f;
 // An exponent s c1 - m in one fused step leaves the maximum itself, whose m is rounded, at up to half a
 // step of m: a quarter below 2^23, powers of two that pass the range from 2^30 on.  Rows whose
-// reference is past this take s c1 as rounded too, which the maximum is then exactly.
+// reference is past this take s c1 as rounded too, which the maximum is then exactly (page_rows_kernel;
+// page_tile_kernel when it does a split again).
 constexpr float kFar = 0x1p23f;
 
 struct PageAttnArgs {
@@ -1114,14 +1115,17 @@ __device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, ui
       }
     }
   };
+  float c1;  // of the logits: a.c1, or 1 where they are scaled already
   // The reference follows the logits of a half.  `before`: the half whose numerators are
   // under way, pb where they go; of its groups of kE the last has only its exponents, the
   // one before it is not yet added or packed.
   auto follow = [&](const f32x16& s, f32x16* before, u32x4* pb) __attribute__((always_inline)) {
-    float mx = max16(s) * a.c1;
+    float mx = max16(s) * c1;
     if (!__any(mx > ref + kSlack)) return;
     mx = fmaxf(mx, partner_f(mx));
-    const float to = ref == kNone ? fmaxf(mx, kNone) : ref + fmaxf(ceilf(mx - ref), 0.f);
+    // (a rise of 2^23 and more is itself rounded, and leaves nothing of what was before)
+    const float rise = fmaxf(ceilf(mx - ref), 0.f);
+    const float to = ref == kNone ? fmaxf(mx, kNone) : rise < kFar ? ref + rise : mx;
     const float by = ref - to, f = __builtin_amdgcn_exp2f(by);
     ref = to;
     l[0] *= f;
@@ -1145,11 +1149,18 @@ __device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, ui
     }
   };
 
+  auto scale = [&](f32x16& s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] *= a.c1;
+  };
+
   // The reference is looked at in the first stage and in those where some row sees only a
   // part: the first keys that a row sees are in one of them.  In the others it is left: only
   // a logit 120 log2 units above all earlier ones does harm, which the sums then show, and
-  // the split is done again with every stage looked at.
+  // the split is done again with every stage looked at.  So it is where a reference is past kFar, the
+  // logits scaled and rounded before the exponents.
   for (bool look = false;; look = true) {
+    c1 = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(look ? 1.f : a.c1)));
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -1237,6 +1248,7 @@ __device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, ui
         if (check) {
           if constexpr (kE4)
             if (top) keep_finite(nk, nv);
+          if (look) scale(s0);
           mask(st, 0, there, up, low, s0);
           follow(s0, nullptr, nullptr);
         }
@@ -1245,10 +1257,11 @@ __device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, ui
           constexpr int kk = i / (D / 32), db = i % (D / 32);
           va[kk][db] = read_v<D>(lv, vo, 0, kk, db);
           s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[i], qf[i], s1, 0, 0, 0);
-          rounded_step<kE, i>(s0, a.c1, ref, l, p0b);
+          rounded_step<kE, i>(s0, c1, ref, l, p0b);
           __builtin_amdgcn_sched_barrier(0);
         });
         if (check) {
+          if (look) scale(s1);
           mask(st, 1, there, up, low, s1);
           follow(s1, &s0, p0b);
         }
@@ -1256,10 +1269,10 @@ __device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, ui
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
           constexpr int kk = i / (D / 32), db = i % (D / 32);
           vb[kk][db] = read_v<D>(lv, vo, 1, kk, db);
-          if constexpr (i < 2) rounded_step<kE, kG + i>(s0, a.c1, ref, l, p0b);
+          if constexpr (i < 2) rounded_step<kE, kG + i>(s0, c1, ref, l, p0b);
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[kk][db], __builtin_bit_cast(bf16x8, p0b[kk]),
                                                           o[db], 0, 0, 0);
-          rounded_step<kE, i>(s1, a.c1, ref, l, p1b);
+          rounded_step<kE, i>(s1, c1, ref, l, p1b);
           __builtin_amdgcn_sched_barrier(0);
         });
         if constexpr (kE4) {  // the next stage's rows are written; loads stay in flight
@@ -1274,7 +1287,7 @@ __device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, ui
         static_for<kG>([&](auto i) __attribute__((always_inline)) {
           constexpr int kk = i / (D / 32), db = i % (D / 32);
           ka[i] = read_k<D>(nk, ko, 0, i);  // (after the last stage: read and not used)
-          if constexpr (i < 2) rounded_step<kE, kG + i>(s1, a.c1, ref, l, p1b);
+          if constexpr (i < 2) rounded_step<kE, kG + i>(s1, c1, ref, l, p1b);
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[kk][db], __builtin_bit_cast(bf16x8, p1b[kk]),
                                                           o[db], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
@@ -1298,15 +1311,17 @@ __device__ __forceinline__ void tile_part(const PageAttnArgs& a, uint32_t bx, ui
       for (int v = 0; v < 16; ++v) any[v & 3] += o[db][v];
     const uint32_t total = __float_as_uint((any[0] + any[1]) + (any[2] + any[3]));
     const bool bad = (total & 0x7f800000u) == 0x7f800000u ||
-                     (__float_as_uint(l[0]) & 0x7fffffffu) > __float_as_uint(0x1p120f);
+                     (__float_as_uint(l[0]) & 0x7fffffffu) > __float_as_uint(0x1p120f) ||
+                     (fabsf(ref) >= kFar && ref != kNone);
     if (!__builtin_amdgcn_readfirstlane(__syncthreads_or(bad))) break;
   }
 
   // o[db][v] holds d = 32*db + 8*(v/4) + 4*half + v%4 of this lane's row
   if (P == kShared || n_parts > 1 || (P == kOwn && unit.first > 0)) {
     if (!row_ok) return;
-    // The sum in [1, 2), so that outputs are of V's size whatever the reference was.
-    const int e = l[0] > 0.f ? (int)(__float_as_uint(l[0]) >> 23) - 127 : 0;
+    // The sum in [1, 2), so that outputs are of V's size whatever the reference was; but for one past
+    // kFar, which has no room for the change and was followed to the maximum.
+    const int e = l[0] > 0.f && fabsf(ref) < kFar ? (int)(__float_as_uint(l[0]) >> 23) - 127 : 0;
     const float f = __uint_as_float((uint32_t)(127 - e) << 23);
     const int64_t prow = (int64_t)split * a.s.n_tokens * a.Hq + out_row;
     float* dst = a.o_part + prow * D + 4 * half;

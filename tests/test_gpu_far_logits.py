@@ -17,8 +17,16 @@ from pages_common import DEV, Cache, attend  # noqa: E402
 from shared_common import GroupCache, attend_shared  # noqa: E402
 
 H7, H05, HF = (28, 4, 128), (14, 2, 64), (4, 2, 64)
-SIZES = [1e3, 1e7, 1e8, 1.5e9, 3.75e9, 1e11, 1e15, 1e25]
+SIZES = [1e4, 5e6, 1.5e9, 3.75e9, 1e25]
 WIDE = 1 << 18
+
+
+def split(c, size):
+    """Parts of a logit's size that queries and keys have (8-bit keys none of it, and one scale)."""
+    if c.cache == "e4m3":
+        c.scale["k"].fill_(127)
+        return size, 1.0
+    return float(np.sqrt(size)), float(np.sqrt(size))
 
 
 def single_out(c, size, sign):
@@ -28,9 +36,9 @@ def single_out(c, size, sign):
     g = torch.Generator().manual_seed(17)
     G = c.hq // c.hkv
     u = (torch.randint(0, 2, (c.hkv, c.d), generator=g) * 2 - 1).float()  # (entries of one size: sums are exact)
-    root = float(np.sqrt(size))
+    in_q, in_k = split(c, size)
     t = 1 + torch.rand(c.tokens, c.hq, 1, generator=g)
-    c.q = (t * root * u.repeat_interleave(G, 0)[None]).to(c.q.dtype)
+    c.q = (t * in_q * u.repeat_interleave(G, 0)[None]).to(c.q.dtype)
     want = torch.zeros(c.tokens, c.hq, c.d, dtype=torch.double)
     v = torch.from_numpy(c.values("v"))
     lens, off = c.lens, c.off
@@ -40,12 +48,12 @@ def single_out(c, size, sign):
         see = int(lens[b] - c.new[b]) + 1
         pick = {"first": 0, "last": see - 1, "shared": getattr(c, "whole_pages", {}).get(b, see) - 1}[c.pick]
         for s in range(-(-int(lens[b]) // c.page)):
-            k[c.table[b, s]] = u[None] * (root * (-1.0 if sign > 0 else -5.0))
+            k[c.table[b, s]] = u[None] * (in_k * (-1.0 if sign > 0 else -5.0))
         at, row = c.table[b, pick // c.page], pick % c.page
         c.picked.append((at, row))
         want[off[b]:off[b + 1]] = v[at, row].repeat_interleave(G, 0)[None]
     for at, row in c.picked:
-        k[at, row] = u * root * (1.0 if sign > 0 else -1.0)
+        k[at, row] = u * in_k * (1.0 if sign > 0 else -1.0)
     c.raw["k"] = (k * (1.0 + 0.25 * torch.rand(c.hkv, 1, generator=g))).to(c.raw["k"].dtype)
     return want
 
@@ -79,10 +87,15 @@ GROUPS_FEW = [(64, [(1, 1), (1, 700)]), (333, [(1, 1), (1, 9), (1, 40)])]
 GROUPS_MANY = [(64, [(40, 40), (33, 64)]), (333, [(45, 45), (3, 9)])]
 LONG = [(1, 6000), (5, 3001)]
 GROUPS_LONG = [(4000, [(1, 7), (1, 40)]), (333, [(1, 1500), (1, 9)])]
-WHOLE = [("f32", HF, FEW), ("f32", HF, MANY)]
-SHARED = [("f32", HF, GROUPS_FEW), ("f32", HF, GROUPS_MANY)]
-LEVEL = WHOLE + [("f32", HF, LONG)]
-LEVEL_SHARED = SHARED + [("f32", HF, GROUPS_LONG)]
+ROWS = [(40, 6000), (33, 3001)]
+GROUPS_ROWS = [(4000, [(33, 40), (40, 70)]), (333, [(1, 1500), (5, 9)])]
+WHOLE = [("f32", HF, FEW), ("f32", HF, MANY), ("bf16", H7, FEW), ("bf16", H7, MANY), ("bf16", H05, MANY),
+         ("e4m3", H7, MANY), ("e4m3", H05, MANY)]
+SHARED = [("f32", HF, GROUPS_FEW), ("f32", HF, GROUPS_MANY), ("bf16", H7, GROUPS_FEW), ("bf16", H7, GROUPS_MANY),
+          ("bf16", H05, GROUPS_MANY), ("e4m3", H7, GROUPS_MANY), ("e4m3", H05, GROUPS_FEW)]
+LEVEL = WHOLE + [("f32", HF, LONG), ("bf16", H7, LONG), ("bf16", H7, ROWS), ("e4m3", H05, ROWS)]
+LEVEL_SHARED = SHARED + [("f32", HF, GROUPS_LONG), ("bf16", H7, GROUPS_LONG), ("bf16", H05, GROUPS_ROWS),
+                         ("e4m3", H7, GROUPS_ROWS)]
 
 
 @pytest.mark.parametrize("sign", [1, -1])
@@ -116,9 +129,10 @@ def level(c, size, sign):
     rows in 64 bits, and of their sizes."""
     g = torch.Generator().manual_seed(23)
     G = c.hq // c.hkv
-    u = (torch.randint(0, 2, (c.hkv, c.d), generator=g) * 2 - 1).float() * float(np.sqrt(size))
-    c.q = ((1 + torch.rand(c.tokens, c.hq, 1, generator=g)) * u.repeat_interleave(G, 0)[None]).to(c.q.dtype)
-    c.raw["k"] = (sign * u).expand(c.raw["k"].shape).to(c.raw["k"].dtype).contiguous()
+    u = (torch.randint(0, 2, (c.hkv, c.d), generator=g) * 2 - 1).float()
+    in_q, in_k = split(c, size)
+    c.q = ((1 + torch.rand(c.tokens, c.hq, 1, generator=g)) * in_q * u.repeat_interleave(G, 0)[None]).to(c.q.dtype)
+    c.raw["k"] = (sign * in_k * u).expand(c.raw["k"].shape).to(c.raw["k"].dtype).contiguous()
     mean, size = (torch.zeros(c.tokens, c.hq, c.d, dtype=torch.double) for _ in "ms")
     v = c.values("v")
     for b, (n, m) in enumerate(c.seqs):
