@@ -77,7 +77,8 @@ struct PageAttnArgs {
   int n_groups;
   int n_wgs;               // workgroups of few rows for the shared keys of one KV head, about
   const int32_t* shared_parts;  // the join: splits of the shared keys by token
-  int shared_splits;            //   and the places that they have
+  int shared_splits;            //   and the places that they have;
+  int first_places;             //   places up to which most rows have all of theirs
 };
 
 // What a launch attends over: whole sequences; or, where groups of them share a prefix, in one
@@ -1442,8 +1443,10 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
       x[k] = *reinterpret_cast<const f32x4*>(a.o_part + at * D + col);
     }
   };
-  // the first splits come together with the number of them (those past it hold anything)
-  load(grp, a.n_splits);
+  // the first splits come together with the number of them (those past it hold anything; of parts, the
+  // places that few rows have come after it)
+  const int usual = kParts ? a.first_places : a.n_splits;
+  load(grp, usual);
   const int first_tok = a.s.tok_off[0], end_tok = a.s.tok_off[a.s.n_seqs];
   int n_parts, n_shared = 0, own_from = 0;  // places [0, n_shared) and [own_from, n_parts) are this row's
   if constexpr (kParts) {
@@ -1460,7 +1463,7 @@ __global__ __launch_bounds__(256) void page_combine_kernel(PageAttnArgs a) {
   float M = kNone, L = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
   for (int s0 = grp; s0 < n_parts; s0 += kGroups * kJoinBatch) {
-    if (s0 != grp) load(s0, n_parts);
+    if (s0 != grp || (kParts && n_parts > usual)) load(s0, n_parts);
     float to = M;
 #pragma unroll
     for (int k = 0; k < kJoinBatch; ++k) {
@@ -1524,6 +1527,15 @@ constexpr int64_t kSharedBlocks = 416;
 // 2,000 (61 MB) 13.1, 15.5.  Prompts gain by fuller tiles only: 8 of 30 tokens on 4,000 (57 MB) 34.7, 39.6; 8
 // of 30 on 16,000 in 8 bits (114 MB) 73.9, 69.7; 16 of 8 on 16,000 (491 MB) 79.1, 45.2.
 constexpr int64_t kWorthParts = int64_t(40) << 20, kWorthPrompts = int64_t(96) << 20;
+
+// Own keys behind shared ones: places for the longest sequence as far as they are this many workgroups (those of
+// 128-row tiles fewer), from 16 steps a place on; the join loads the usual ones with the first round.  48 sequences
+// on 30,011 tokens beside one of 30,000 in no group, 28 heads on 4 in bf16: 199 us with the places of the others,
+// 113 with 512 workgroups, 71 with 1,024, 82 with 2,048, each by itself 163; without that one 49.7, 50.0, 50.5, 50.8.
+// 8 prompts of 48 on 32,768 in 8 bits beside two of 20,000: 580, with 256 of tiles 403, 384 347, 512 328, each by
+// itself 314; 8 of 30 on 16,000 in bf16 alone 82.4, 82.7, 82.7, 86.1.
+constexpr int64_t kOwnWorkgroups = 1024, kOwnTiles = 384;
+constexpr int kOwnSlice = 16;
 
 struct PageAttnPlan {
   bool wide;       // page_tile_kernel
@@ -1620,6 +1632,7 @@ PageAttnPlan make_plan(const ckv_page_pool* pool, const ckv_page_batch* b, int H
 struct SharedPlan {
   bool apart;  // in parts; false: every sequence by itself is less work than those and their join
   PageAttnPlan whole, shared, own;
+  int first_places;  // of the shared keys and, as most sequences have them, of the own ones
   size_t off_ml, off_shared, off_own, bytes;
 };
 
@@ -1652,13 +1665,22 @@ SharedPlan make_shared_plan(const ckv_page_pool* pool, const ckv_page_batch* b, 
   const auto blocks = [&](int units, int64_t most_of) {
     return std::min(b->n_tokens * G / tile::kBlockRows + units, units * ceil_div(most_of * G, tile::kBlockRows));
   };
-  // (own keys: what the longest sequence has behind the longest prefix, a page at least)
-  const int64_t own_len = std::max<int64_t>(len - shared_len, pool->page_size);
-  p.own = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most, own_len, blocks(b->n_seqs, most), 0, 0, kFewRows, false);
+  // The sequences' own keys: splits for what the longest sequence has behind the longest prefix (a page at
+  // least), and some more places for one whose keys are all its own: in no group, in one of a shorter prefix, or
+  // where it is not known how much is shared.
+  const int64_t own_len = std::max<int64_t>(len - shared_len, pool->page_size), own_blocks = blocks(b->n_seqs, most);
+  p.own = plan_units(pool, Hq, b->n_seqs, b->n_tokens, most, own_len, own_blocks, 0, 0, kFewRows, false);
+  const int64_t own_wgs = pool->n_kv_heads * (p.own.wide ? own_blocks : (int64_t)b->n_seqs * p.own.row_blocks);
+  const int own_usual = p.own.n_splits;
+  p.own.slice = std::max(p.own.slice, kOwnSlice);
+  p.own.n_splits = (int)std::max<int64_t>(
+      p.own.n_splits, std::min(ceil_div(ceil_div(len, p.own.wide ? tile::kTile : kTile), p.own.slice),
+                               (p.own.wide ? kOwnTiles : kOwnWorkgroups) / std::max<int64_t>(own_wgs, 1)));
   const int64_t most_group = most_tokens(g->max_tokens, b->n_tokens, g->n_groups);
   const int few_rows = p.own.wide ? 0 : pool->dtype == CKV_DTYPE_BF16 && pool->head_dim == 128 ? 32 : 48;
   p.shared = plan_units(pool, Hq, g->n_groups, b->n_tokens, most_group, shared_len, blocks(g->n_groups, most_group), 0, 0,
                         few_rows, true);
+  p.first_places = p.shared.n_splits + own_usual;
   const size_t rows = (size_t)b->n_tokens * Hq, places = (size_t)p.shared.n_splits + p.own.n_splits;
   p.off_ml = align_up(places * rows * pool->head_dim * sizeof(float), 256);
   p.off_shared = align_up(p.off_ml + places * rows * sizeof(float2), 256);
@@ -1802,6 +1824,7 @@ ckv_status launch_shared_attn(PageAttnArgs& a, const SharedPlan& p, char* ws, hi
   a.ml_part = ml_part;
   a.shared_parts = shared_parts;
   a.shared_splits = p.shared.n_splits;
+  a.first_places = p.first_places;
   a.n_splits = p.shared.n_splits + p.own.n_splits;
   return launch_join<D, T, true>(a, st);
 }
