@@ -799,8 +799,9 @@ typedef struct ckv_seq_rows {
  * table entries (-1 behind them), its length, its rows of the n_states states.  With a
  * parent outside [0, n_seqs) it is empty: no entries, length 0, the states' rows as they
  * were.  refs_out[p] = refs[p] + (children of b - 1) summed over the sequences b that
- * hold page p: who has no children gives its pages back.  Tables and lengths go to other
- * buffers than they come from. */
+ * hold page p: who has no children gives its pages back.  What is written goes to other
+ * buffers than what is read, but for refs_out, which may be refs: CKV_EINVAL where arrays share a
+ * byte (rows of one may lie between those of another). */
 ckv_status ckv_page_fork(const ckv_page_tables* tables, const int32_t* parents,
                          const ckv_seq_rows* states, int32_t n_states, void* stream);
 
@@ -831,8 +832,10 @@ typedef struct ckv_page_step {
  *           kind of refusal neither counts).  Its n_new becomes 0.
  *   lens_out gets the lengths with the new tokens, tok_off and the token arrays the
  *           rows: sequence after sequence, positions ascending.
- * n_out must be n_seqs; table_out, lens_out and refs_out may be table, lens and refs.
- * ws: ckv_page_extend_workspace_bytes(n_pages, n_seqs) bytes. */
+ * n_out must be n_seqs; table_out, lens_out and refs_out may be table, lens and refs; no other
+ * array that is written, ws included, shares a byte with another (CKV_EINVAL).
+ * ws: ckv_page_extend_workspace_bytes(n_pages, n_seqs) bytes; calls that share one must not
+ * overlap in time. */
 size_t ckv_page_extend_workspace_bytes(int64_t n_pages, int32_t n_seqs);
 ckv_status ckv_page_extend(const ckv_page_tables* tables, const int32_t* n_new,
                            const ckv_page_step* step, void* ws, size_t ws_bytes, void* stream);
@@ -847,8 +850,9 @@ ckv_status ckv_page_extend(const ckv_page_tables* tables, const int32_t* n_new,
  * nothing and add nothing; an infinity counts as the largest finite number.
  *   parent  r * n_beams + b; token; score; done (may be NULL): 1 for eos and for who was
  *           done.  Where fewer are offered: -1, -1, -inf, 0.  [n_reqs][keep], other buffers
- *           than the beams' own
- *   ws      ckv_beam_select_workspace_bytes(...) bytes for the same beams */
+ *           than each other, ws and the beams' own (CKV_EINVAL)
+ *   ws      ckv_beam_select_workspace_bytes(...) bytes for the same beams; calls that share one
+ *           must not overlap in time */
 typedef struct ckv_beams {
   const void* logits;    /* device, rows r * n_beams + b of vocab elements, aligned to one */
   const float* scores;   /* device, [n_reqs][n_beams]                                     */

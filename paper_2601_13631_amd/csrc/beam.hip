@@ -14,7 +14,7 @@
 
 #include <type_traits>
 
-#include "ckv_internal.h"
+#include "pages_internal.h"
 
 namespace ckv {
 namespace {
@@ -543,6 +543,20 @@ ckv_status ckv_beam_select(const ckv_beams* beams, int32_t* parent, int32_t* tok
   const BeamPlan p = make_beam_plan(beams);
   if (ws_bytes < p.bytes) CKV_FAIL(CKV_EINVAL, "workspace too small: %zu < %zu", ws_bytes, p.bytes);
   if (!aligned16(ws)) CKV_FAIL(CKV_EINVAL, "pointers must be 16-byte aligned");
+  {
+    const int64_t rows = (int64_t)beams->n_reqs * beams->n_beams, kept = (int64_t)beams->n_reqs * beams->keep;
+    const int bytes = elem_bytes(beams->dtype);
+    const MemRows reads[3] = {
+        MemRows{beams->logits, rows, (int64_t)beams->vocab * bytes,
+                (beams->row_stride ? beams->row_stride : beams->vocab) * bytes},
+        mem_array(beams->scores, rows * (int64_t)sizeof(float)), mem_array(beams->done, rows)};
+    const MemRows writes[5] = {mem_array(parent, kept * (int64_t)sizeof(int32_t)),
+                               mem_array(token, kept * (int64_t)sizeof(int32_t)),
+                               mem_array(score, kept * (int64_t)sizeof(float)), mem_array(done, kept),
+                               mem_array(ws, (int64_t)p.bytes)};
+    if (writes_overlap(writes, 5, reads, 3))
+      CKV_FAIL(CKV_EINVAL, "the outputs must be other buffers than each other and the beams'");
+  }
   char* const w = static_cast<char*>(ws);
   const BeamArgs a{static_cast<const char*>(beams->logits), beams->scores, beams->done,
                    beams->row_stride ? beams->row_stride : beams->vocab, beams->n_reqs, beams->n_beams,

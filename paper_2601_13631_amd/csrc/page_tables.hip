@@ -561,6 +561,11 @@ ckv_status check_tables(const ckv_page_tables* t, Tables& x) {
   return CKV_OK;
 }
 
+constexpr int kInt = sizeof(int32_t);
+MemRows table_rows(const int32_t* at, int64_t n, const Tables& t, int64_t stride) {
+  return MemRows{at, n, (int64_t)t.max_pages * kInt, stride * kInt};
+}
+
 }  // namespace
 }  // namespace ckv
 
@@ -635,6 +640,21 @@ ckv_status ckv_page_fork(const ckv_page_tables* tables, const int32_t* parents, 
     x.pieces = (int32_t)ceil_div(r.row_bytes, kRowPiece);
     a.state_blocks += (int64_t)x.pieces * a.t.n_out;
   }
+  // Workgroups read what others write, in no order: only the counts may be in place.
+  MemRows reads[4 + CKV_MAX_SEQ_ROWS] = {table_rows(a.t.table, a.t.n_seqs, a.t, a.t.table_stride),
+                                         mem_array(a.t.lens, (int64_t)a.t.n_seqs * kInt),
+                                         mem_array(parents, (int64_t)a.t.n_out * kInt),
+                                         mem_array(a.t.refs_out == a.t.refs ? nullptr : a.t.refs, a.t.n_pages * kInt)};
+  MemRows writes[3 + CKV_MAX_SEQ_ROWS] = {table_rows(a.t.table_out, a.t.n_out, a.t, a.t.table_out_stride),
+                                          mem_array(a.t.lens_out, (int64_t)a.t.n_out * kInt),
+                                          mem_array(a.t.refs_out, a.t.n_pages * kInt)};
+  for (int i = 0; i < n_states; ++i) {
+    const StateRows& x = a.states[i];
+    reads[4 + i] = MemRows{x.src, x.src ? a.t.n_seqs : 0, x.row_bytes, x.src_stride};
+    writes[3 + i] = MemRows{x.dst, x.dst ? a.t.n_out : 0, x.row_bytes, x.dst_stride};
+  }
+  CKV_REQUIRE(!writes_overlap(writes, 3 + n_states, reads, 4 + n_states),
+              "an array that is written overlaps another one (only refs_out may be refs)");
   const int64_t ref_blocks = a.t.refs_out != a.t.refs ? ceil_div(a.t.n_pages, kPiece) : 0;
   const int64_t grid = a.table_blocks + a.state_blocks + ref_blocks, counts = (int64_t)a.t.n_seqs * a.table_pieces;
   if (grid >= kMaxGrid || counts >= kMaxGrid) CKV_FAIL(CKV_EUNSUPPORTED, "batch too large");
@@ -671,6 +691,26 @@ ckv_status ckv_page_extend(const ckv_page_tables* tables, const int32_t* n_new, 
   const ExtendLayout l = extend_layout(a.t.n_pages, a.t.n_seqs);
   CKV_REQUIRE(ws_bytes >= l.bytes, "workspace too small: %zu < %zu", ws_bytes, l.bytes);
   CKV_REQUIRE(aligned16(ws), "pointers must be 16-byte aligned");
+  {
+    const int64_t n = (int64_t)a.t.n_seqs * kInt;
+    const MemRows reads[4] = {
+        table_rows(a.t.table, a.t.table_out == a.t.table ? 0 : a.t.n_seqs, a.t, a.t.table_stride),
+        mem_array(a.t.lens_out == a.t.lens ? nullptr : a.t.lens, n),
+        mem_array(a.t.refs_out == a.t.refs ? nullptr : a.t.refs, a.t.n_pages * kInt), mem_array(n_new, n)};
+    const MemRows writes[11] = {table_rows(a.t.table_out, a.t.n_out, a.t, a.t.table_out_stride),
+                                mem_array(a.t.lens_out, n),
+                                mem_array(a.t.refs_out, a.t.n_pages * kInt),
+                                mem_array(step->tok_off, n + kInt),
+                                mem_array(step->copy_src, n),
+                                mem_array(step->copy_dst, n),
+                                mem_array(step->counts, 4 * kInt),
+                                mem_array(step->slots, step->n_tokens * (int64_t)sizeof(int64_t)),
+                                mem_array(step->positions, step->n_tokens * kInt),
+                                mem_array(step->seqs, step->n_tokens * kInt),
+                                mem_array(ws, (int64_t)l.bytes)};
+    CKV_REQUIRE(!writes_overlap(writes, 11, reads, 4),
+                "an array that is written overlaps another one (only the table, lengths and counts may be in place)");
+  }
   auto at = [&](size_t off) { return reinterpret_cast<int32_t*>(static_cast<char*>(ws) + off); };
   a.n_new = n_new;
   a.o = *step;

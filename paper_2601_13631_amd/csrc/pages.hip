@@ -11,6 +11,58 @@
 
 namespace ckv {
 
+namespace {
+using Wide = __int128;  // (rows times strides pass 64 bits)
+Wide floor_div(Wide a, Wide b) { return a / b - (a % b < 0 ? 1 : 0); }  // b > 0
+Wide begin_of(const MemRows& x) { return (Wide) reinterpret_cast<uintptr_t>(x.at); }
+// Whether bytes [lo, hi) meet a row of x.
+bool meets(Wide lo, Wide hi, const MemRows& x) {
+  // rows j with j stride + bytes > lo and j stride < hi, from x's begin
+  const Wide from = std::max<Wide>(floor_div(lo - begin_of(x) - x.bytes, x.stride) + 1, 0);
+  const Wide upto = std::min<Wide>(floor_div(hi - 1 - begin_of(x), x.stride), x.n - 1);
+  return from <= upto;
+}
+// Whether arrays whose bytes from the first to the last meet share one.
+bool rows_overlap(const MemRows& a, const MemRows& b) {
+  const MemRows &few = a.n <= b.n ? a : b, &many = a.n <= b.n ? b : a;
+  if (few.n > 1 && few.stride == many.stride) {
+    // Row i of `few` begins `off` bytes into a step of `many`, alike for all i.
+    const Wide d = begin_of(few) - begin_of(many), off = d - floor_div(d, few.stride) * few.stride;
+    if (off >= many.bytes && off + few.bytes <= few.stride) return false;
+  }
+  for (int64_t i = 0; i < few.n; ++i) {
+    const Wide lo = begin_of(few) + (Wide)i * few.stride;
+    if (meets(lo, lo + few.bytes, many)) return true;
+  }
+  return false;
+}
+// The address behind the last byte; the first one's of an empty array.
+uint64_t end_of(const MemRows& x) {
+  const uint64_t at = reinterpret_cast<uintptr_t>(x.at);
+  if (x.n <= 0 || x.bytes <= 0) return at;
+  const Wide end = (Wide)at + (Wide)(x.n - 1) * x.stride + x.bytes;
+  return end < (Wide)UINT64_MAX ? (uint64_t)end : UINT64_MAX;
+}
+}  // namespace
+
+bool writes_overlap(const MemRows* writes, int n_writes, const MemRows* reads, int n_reads) {
+  // (mostly no two come near each other: an allocation each)
+  uint64_t read_end[kMostArrays], write_end[kMostArrays];
+  for (int k = 0; k < n_reads; ++k) read_end[k] = end_of(reads[k]);
+  for (int k = 0; k < n_writes; ++k) write_end[k] = end_of(writes[k]);
+  const auto meet = [](const MemRows& a, uint64_t a1, const MemRows& b, uint64_t b1) {
+    const uint64_t a0 = reinterpret_cast<uintptr_t>(a.at), b0 = reinterpret_cast<uintptr_t>(b.at);
+    return a0 < b1 && b0 < a1 && a0 < a1 && b0 < b1 && rows_overlap(a, b);
+  };
+  for (int i = 0; i < n_writes; ++i) {
+    for (int k = 0; k < n_reads; ++k)
+      if (meet(writes[i], write_end[i], reads[k], read_end[k])) return true;
+    for (int k = i + 1; k < n_writes; ++k)
+      if (meet(writes[i], write_end[i], writes[k], write_end[k])) return true;
+  }
+  return false;
+}
+
 ckv_status check_pool(const ckv_page_pool* p, bool with_pointers) {
   if (!p) CKV_FAIL(CKV_EINVAL, "pool is NULL");
   if (p->dtype != CKV_DTYPE_F32 && p->dtype != CKV_DTYPE_BF16 && p->dtype != CKV_DTYPE_E4M3)

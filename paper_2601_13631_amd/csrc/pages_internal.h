@@ -15,6 +15,17 @@ inline int64_t page_stride_bytes(const ckv_page_pool* p) {
   return p->page_stride ? p->page_stride * page_elem_bytes(p->dtype) : page_bytes_of(p);
 }
 
+// An array of a call: `n` rows of `bytes` bytes each, `stride` bytes apart.
+struct MemRows {
+  const void* at;
+  int64_t n, bytes, stride;
+};
+inline MemRows mem_array(const void* at, int64_t bytes) { return MemRows{at, at ? 1 : 0, bytes, bytes}; }
+// Whether an array that is written shares a byte with one that is read, or with another that is written
+// (rows of one may lie between those of another); up to kMostArrays of each.
+constexpr int kMostArrays = 16;
+bool writes_overlap(const MemRows* writes, int n_writes, const MemRows* reads, int n_reads);
+
 // A launch has fewer than 2^32 threads along x: workgroups of 256 threads at most.
 constexpr int64_t kMaxGrid = int64_t(1) << 24;
 

@@ -6,7 +6,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 from pages_common import DEV  # noqa: E402
-from shared_common import extend_model  # noqa: E402
+from shared_common import extend_model, fork_model, select_model  # noqa: E402
 from test_gpu_page_tables import dev, run_extend, tables  # noqa: E402
 
 
@@ -53,3 +53,62 @@ def test_some_arrays_in_place(mix, kind):
         assert (x.cpu().numpy() == np.asarray(want[k])).all(), k
     for x, before, place in ((t, table, 1), (l, lens, 2), (r, refs, 4)):
         assert mix & place or (x.cpu().numpy() == before).all()
+
+
+def test_arrays_of_one_buffer():
+    """Two tables in the halves of wider rows, lengths, counts, parents and a state's rows side by side: a fork
+    there and back, a step on the second."""
+    import paper_2601_13631_amd as ckv
+    n, width, n_pages, page = 70, 33, 3000, 16
+    rng = np.random.default_rng(5)
+    table, lens, refs = tables(rng, n, width, n_pages, page)
+    both = torch.full((n, 2 * width), -77, dtype=torch.int32, device=DEV)
+    a, b = both[:, :width], both[:, width:]
+    a.copy_(dev(table))
+    ints = torch.zeros(3 * n + 2 * n_pages, dtype=torch.int32, device=DEV)
+    la, lb, parents, ra, rb = ints.split([n, n, n, n_pages, n_pages])
+    la.copy_(dev(lens))
+    ra.copy_(dev(refs))
+    p = rng.integers(-1, n, n)
+    parents.copy_(dev(p))
+    state = torch.zeros(n, 2, 50, dtype=torch.int32, device=DEV)
+    state[:, 0] = torch.arange(50 * n, device=DEV).view(n, 50)
+    ckv.page_fork(ckv.PageFork(page, a, b, la, lb, ra, rb, states=[(state[:, 0], state[:, 1])]), parents)
+    want = fork_model(page, table, lens, refs, p)
+    for x, y in zip((b, lb, rb), want):
+        assert (x.cpu().numpy() == y).all()
+    there = torch.from_numpy(p >= 0).to(DEV)
+    assert (state[there, 1] == state[parents.long()[there], 0]).all() and (a.cpu().numpy() == table).all()
+    n_new = rng.integers(0, 40, n)
+    total = int(n_new.sum())
+    out = torch.zeros(3 * n + 1 + 4 + 2 * total, dtype=torch.int32, device=DEV)
+    off, src, dst, counts, pos, seqs = out.split([n + 1, n, n, 4, total, total])
+    step = ckv.PageStep(page, b, a, lb, la, rb, rb, dev(n_new), off, src, dst, counts, positions=pos, seqs=seqs)
+    ckv.page_extend(step, torch.zeros(ckv.page_extend_workspace_bytes(n_pages, n), dtype=torch.uint8, device=DEV))
+    more = extend_model(page, *want, n_new, total)
+    for k, x in {"table": a, "lens": la, "refs": rb, "tok_off": off, "copy_src": src, "copy_dst": dst, "counts": counts,
+                 "positions": pos, "seqs": seqs}.items():
+        assert (x.cpu().numpy() == np.asarray(more[k])).all(), k
+    with pytest.raises(ckv.CkvError, match="overlap"):
+        ckv.page_fork(ckv.PageFork(page, both[:, 1:width + 1], both[:, width:], la, lb, ra, rb), parents)
+    with pytest.raises(ckv.CkvError, match="overlap"):
+        ckv.page_fork(ckv.PageFork(page, a, b, la, lb, ints[3 * n:3 * n + n_pages], ints[3 * n + 1:3 * n + 1 + n_pages]), parents)
+
+
+def test_a_selection_of_one_buffer():
+    import paper_2601_13631_amd as ckv
+    g = torch.Generator().manual_seed(8)
+    logits = torch.randn(5, 3, 700, generator=g)
+    scores = -torch.rand(5, 3, generator=g)
+    out = torch.zeros(3 * 5 * 4 + 5 * 3, device=DEV)
+    parent, token, best, given = out.split([20, 20, 20, 15])
+    given.copy_(scores.reshape(-1))
+    parent, token = (x.view(torch.int32).view(5, 4) for x in (parent, token))
+    x = logits.to(DEV)
+    ws = torch.empty(ckv.beam_select_workspace_bytes(x, 4), dtype=torch.uint8, device=DEV)
+    ckv.beam_select(x, given.view(5, 3), parent, token, best.view(5, 4), ws)
+    want = select_model(logits.numpy(), scores.numpy(), None, 4, -1)
+    assert (parent.cpu().numpy() == want[0]).all() and (token.cpu().numpy() == want[1]).all()
+    for bad in ((out[50:70], given), (out[40:60], out[59:74])):
+        with pytest.raises(ckv.CkvError, match="buffers"):
+            ckv.beam_select(x, bad[1].view(5, 3), parent, token, bad[0].view(5, 4), ws)
