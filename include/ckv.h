@@ -829,7 +829,8 @@ typedef struct ckv_page_step {
  *   refusal A sequence is refused, and stays as it is, if its length would pass its
  *           table; or if those that need pages up to and with it, refused ones too, need
  *           more than are free; or their n_new more than n_tokens rows (of the former
- *           kind of refusal neither counts).  Its n_new becomes 0.
+ *           kind of refusal neither counts).  Its n_new becomes 0.  So a prompt that is too
+ *           large refuses what needs pages behind it: prompts go last.
  *   lens_out gets the lengths with the new tokens, tok_off and the token arrays the
  *           rows: sequence after sequence, positions ascending.
  * n_out must be n_seqs; table_out, lens_out and refs_out may be table, lens and refs; no other
