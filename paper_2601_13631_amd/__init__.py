@@ -821,7 +821,8 @@ class PageFork:
     sequences as they are, ``table_out`` [n_out, max_pages], ``lens_out`` [n_out] and ``refs_out`` (which
     may be ``refs``) those after the call.  ``states``: pairs of tensors [n_seqs, ...] and
     [n_out, ...] of one type whose rows follow the sequences, up to eight; a row is
-    contiguous, rows may lie apart.  Keeps the tensors alive; make it once per pair of buffers.
+    contiguous, rows may lie apart.  What is written shares no memory with the rest, but ``refs_out`` with
+    ``refs``.  Keeps the tensors alive; make it once per pair of buffers.
     """
 
     def __init__(self, page_size: int, table, table_out, lens, lens_out, refs, refs_out, states=()):
@@ -870,7 +871,8 @@ class PageStep:
     ``refs_out`` may be the same tensors.  ``n_new`` [n_seqs]: the tokens that each sequence
     gets.  Written: ``tok_off`` [n_seqs + 1], ``copy_src`` and ``copy_dst`` [n_seqs], ``counts`` [4], and, each
     of as many rows as the call's token tensors, ``slots`` (int64), ``positions`` and ``seqs`` (int32; any
-    of these may be None).  ``n_tokens``: those rows, where all three are None.
+    of these may be None).  ``n_tokens``: those rows, where all three are None.  What is written shares no
+    memory with the rest, but for the three that may be the same.
     Keeps the tensors alive; one handle serves every step on the same tensors.
     """
 

@@ -1524,8 +1524,9 @@ constexpr int64_t kSharedBlocks = 416;
 // Bytes of shared pages read again and again that are worth the parts' launch and join.  Decoding, 28 heads
 // on 4 in bf16: 4 sequences on 4,000 tokens (25 MB) apart 12.7 us, in parts 14.7; 2 groups of 2 on 8,000 in 8
 // bits, 40 heads on 8 (33 MB) 18.6, 17.2; 4 on 8,000 (49 MB) 18.6, 15.1; 8 on 4,000 (57 MB) 18.7, 15.2; but 16 on
-// 2,000 (61 MB) 13.1, 15.5: bytes alone do not part many short sequences from these.  Prompts gain by fuller tiles only: 8 of 30 tokens on 4,000 (57 MB) 34.7, 39.6; 8
-// of 30 on 16,000 in 8 bits (114 MB) 73.9, 69.7; 16 of 8 on 16,000 (491 MB) 79.1, 45.2.
+// 2,000 (61 MB) 13.1, 15.5: bytes alone do not part many short sequences from these.  Prompts gain by fuller
+// tiles only: 8 of 30 tokens on 4,000 (57 MB) 34.7, 39.6; 8 of 30 on 16,000 in 8 bits (114 MB) 73.9, 69.7; 16 of 8
+// on 16,000 (491 MB) 79.1, 45.2.
 constexpr int64_t kWorthParts = int64_t(40) << 20, kWorthPrompts = int64_t(96) << 20;
 
 // Own keys behind shared ones: places for the longest sequence as far as they are this many workgroups (those of

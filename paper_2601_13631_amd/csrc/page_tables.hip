@@ -563,7 +563,7 @@ ckv_status check_tables(const ckv_page_tables* t, Tables& x) {
 
 constexpr int kInt = sizeof(int32_t);
 MemRows table_rows(const int32_t* at, int64_t n, const Tables& t, int64_t stride) {
-  return MemRows{at, n, (int64_t)t.max_pages * kInt, stride * kInt};
+  return MemRows{at, n, (int64_t)t.max_pages * kInt, std::min(stride, INT64_MAX / kInt) * kInt};
 }
 
 }  // namespace

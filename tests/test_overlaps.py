@@ -95,6 +95,16 @@ def test_rows_between_rows():
         assert fork(at, rows) == status, rows
 
 
+@pytest.mark.parametrize("stride", [1 << 60, 1 << 61, 1 << 62, (1 << 63) - 1])
+def test_strides_past_the_address_space(stride):
+    """Only the first rows are anywhere."""
+    at = places()
+    wide = dict(table_stride=stride, table_out_stride=stride)
+    for run in (fork, extend):
+        assert run(at, **wide) == ckv.EUNSUPPORTED
+        assert run(places(table_out=at["table"] + 4), **wide) == ckv.EINVAL and "overlap" in ckv.last_error()
+
+
 @pytest.mark.parametrize("seed", range(20))
 def test_overlaps_by_bytes(seed):
     """Random rows of few bytes, against the bytes themselves."""
